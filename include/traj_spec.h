@@ -24,6 +24,10 @@
  *                               traj_refresh_layer, the same layer over whole sequences that
  *                               refreshes the dual cache at a block boundary, and traj_linear,
  *                               the projection GEMM on its own.
+ *   7. traj_paged_append, traj_paged_attn -- a key-value cache in pages for sequences of different
+ *                               lengths: new tokens' keys rotated and written, and attention of the
+ *                               new tokens over it.
+ *   8. traj_confidence_topk_adjusted -- call 2 under each request's penalties, biases and grammar.
  *
  * Conventions shared by every entry point
  *   - Array arguments are DEVICE pointers owned by the caller, on the device that is
@@ -72,6 +76,10 @@ typedef enum { TRAJ_BF16 = 0, TRAJ_F32 = 1 } traj_dtype;
 #define TRAJ_DEV_BAD_LEAF 0x2   /* traj_build_tree: a leaf outside [-1, n_prev): taken as -1 */
 #define TRAJ_DEV_BAD_BLOCK 0x4  /* some block_start[b] was outside [0, S]: clamped              */
 #define TRAJ_DEV_BAD_ROOT 0x8   /* traj_joint_peers: a root index outside its tree: taken as 0   */
+#define TRAJ_DEV_BAD_LENGTH 0x10  /* paged cache: a length or start outside its range: clamped, or its tokens skipped */
+#define TRAJ_DEV_BAD_PAGE 0x20    /* paged cache: a page number outside [0, num_pages): its tokens are skipped       */
+#define TRAJ_DEV_BAD_MASK 0x40    /* adjusted logits: a mask index outside [-1, n_masks): nothing is allowed         */
+#define TRAJ_DEV_BAD_HISTORY 0x80 /* adjusted logits: a history length outside [0, history_size]: clamped            */
 
 /* ------------------------------------------------------------------------------------
  * 1. Trajectory-masked verification attention  (Sec. 3.3; drafts packed as in Sec. 3.2
@@ -410,6 +418,108 @@ size_t traj_linear_workspace_size(int64_t M, int64_t K, int64_t N);
 
 traj_status traj_linear(const void* x, const void* w, void* y, int64_t M, int64_t K, int64_t N, int32_t accumulate,
                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * 7. Paged key-value cache
+ *
+ * The keys and values of many sequences of different lengths in pages of one pool.  Token s of
+ * sequence b lies in row s % page_size of page page_table[b][s / page_size]; its kv head g, value d
+ * is k_pages[page * page_stride + row * token_stride + g * head_stride + d] (bf16), v_pages likewise
+ * with the same strides.  So pools [num_pages, page_size, Hkv, D] and [num_pages, Hkv, page_size, D]
+ * both serve, and a contiguous cache [B, S, Hkv, D] is a pool of B pages of S tokens.
+ * page_table: int32, max_pages columns, table_stride elements from row to row; entries behind a
+ * sequence's last page are never read.  Sequences may share pages that neither writes.
+ * Limits (all entry points): B >= 0 and T >= 0 (0 = no-op) with B <= 65535; D in {64, 128};
+ *   Hq % Hkv == 0; num_pages, page_size, max_pages >= 1 with max_pages * page_size < 2^31 - 256;
+ *   strides positive multiples of 8 with token_stride <= 2^26; pools and q / k / v rows 16-byte
+ *   aligned; table_stride >= max_pages.
+ * ------------------------------------------------------------------------------------ */
+typedef struct {
+    int32_t B, T; /* sequences; new tokens per sequence (at most) */
+    int32_t Hq, Hkv, D;
+    int32_t num_pages, page_size, max_pages;
+    int64_t table_stride, page_stride, token_stride, head_stride; /* elements */
+} traj_paged_shape;
+
+/* Appends new tokens: for t < n_new[b] (n_new NULL: T), with position p = pos0[b] + t (pos0 NULL:
+ * start[b] + t) and cache index s = start[b] + t,
+ *     page row s of sequence b  <- rotate(k[b,t], p), v[b,t];   q_out[b,t] <- rotate(q[b,t], p),
+ * rotate: pairs (d, d + D/2) of each head by p * rope_theta^(-2d/D), the angle reduced in 64 bits, the
+ * products in fp32, the result rounded to bf16; rope_theta == 0 stores q and k as they are.
+ * q [B, T, Hq, D], k, v [B, T, Hkv, D]: token rows of contiguous heads, q_stride / k_stride / v_stride
+ * elements apart (multiples of 8, at least the row), e.g. the parts of a projection's [q | k | v] rows.
+ * q and q_out may both be NULL; q_out [B, T, Hq, D] contiguous, may be q itself if q_stride == Hq * D.
+ * Rows t >= n_new[b] of q_out and all other rows of the pools are left as they are.  start, n_new,
+ * pos0: [B] int32 (device).  n_new[b] outside [0, T] is clamped, tokens whose cache index lies outside
+ * [0, max_pages * page_size) are not stored (TRAJ_DEV_BAD_LENGTH), nor are those of a page outside the
+ * pool (TRAJ_DEV_BAD_PAGE); their q_out is written.  No two tokens of a call may share a cache row. */
+traj_status traj_paged_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, void* q_out, void* k_pages, void* v_pages,
+                              const int32_t* page_table, const int32_t* start, const int32_t* n_new,
+                              const int32_t* pos0, const traj_paged_shape* shape, float rope_theta, void* stream);
+
+/* Attention of T new tokens per sequence over its cached keys (its own, once appended, among them):
+ *     out[b,t,h,:] = softmax_s( scale * q[b,t,h,:] . key_s ) * value_s,   g = h / (Hq / Hkv),
+ * over s < lens[b], or with causal != 0 over s < lens[b] - T + t + 1 (the new tokens are the sequence's
+ * last T).  A row that sees no key is 0.  Softmax and accumulation in fp32, weights rounded to bf16 for the
+ * matrix product, out rounded to bf16.  q, out: [B, T, Hq, D] bf16, contiguous, 16-byte aligned.
+ * lens [B] int32 (device); a length outside [0, max_pages * page_size] is clamped (TRAJ_DEV_BAD_LENGTH),
+ * keys of a page outside the pool are not visible (TRAJ_DEV_BAD_PAGE).  Rows of a page behind lens[b]
+ * may hold anything.  scale <= 0 selects 1/sqrt(D).
+ * workspace: traj_paged_attn_workspace_size() bytes, 16-byte aligned, for the partial results of
+ * sequences whose keys are split over workgroups (0: the shape is never split).  With NULL nothing is
+ * split.  Calls that may run at the same time (graphs among them) need workspaces of their own.
+ * Deterministic: the ranges follow from the lengths alone, their results are joined in order. */
+size_t traj_paged_attn_workspace_size(const traj_paged_shape* shape);
+
+traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                            const int32_t* lens, void* out, const traj_paged_shape* shape, float scale,
+                            int32_t causal, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * 8. Confidence and candidates of adjusted logits
+ *
+ * traj_confidence_topk of x instead of the logits l, with, for row r, its sequence q = r / rows_per_seq
+ * and c = number of times v occurs in history[q, 0 .. history_len[q]-1]:
+ *     x = l,  or where c > 0:  (l > 0 ? l / repetition[q] : l * repetition[q]);
+ *     x = x + (y - z),  y = sum of bias[q, j] with bias_ids[q, j] == v in order of j,
+ *                       z = frequency[q] * c + presence[q] where c > 0, else 0;
+ *     x = -inf where bit v % 32 of mask[m, v / 32] is 0,   m = mask_index[r],
+ * each operation in fp32.  A value of -inf is never a candidate: a row's slots without one hold idx -1 and conf 0 (all of
+ * them where nothing is allowed).  Logits of forbidden tokens may hold anything; the others no NaN or +inf.
+ * Ids outside [0, vocab) in history and bias_ids are padding.
+ * history [n_seq, history_size] int32, history_len [n_seq] (NULL: history_size), repetition (> 0), frequency,
+ * presence [n_seq] float32 (each NULL: 1, 0, 0), bias_ids / bias [n_seq, bias_size] int32 / float32 (finite or
+ * -inf), mask [n_masks, mask_stride] uint32, mask_index [rows] int32 (NULL: m = r; -1: every token is allowed;
+ * any other value outside [0, n_masks): none is, TRAJ_DEV_BAD_MASK); n_seq = ceil(rows / rows_per_seq).
+ * history_size == 0 / bias_size == 0 / mask == NULL leave that part out.
+ * Limits: those of traj_confidence_topk; vocab <= 2^20 (else TRAJ_E_UNSUPPORTED); rows_per_seq >= 1;
+ *   history_size, bias_size >= 0, their sum < 2^30; mask_stride >= ceil(vocab / 32); without mask_index
+ *   n_masks >= rows.
+ * workspace: traj_confidence_topk_adjusted_workspace_size() bytes, 16-byte aligned; one sized for more rows
+ * of the same kind serves too.  TRAJ_E_WORKSPACE where the sequences' records don't fit.
+ * ------------------------------------------------------------------------------------ */
+typedef struct {
+    int32_t rows_per_seq;
+    int32_t history_size, bias_size, n_masks;
+    const int32_t* history;
+    const int32_t* history_len;
+    const float* repetition;
+    const float* frequency;
+    const float* presence;
+    const int32_t* bias_ids;
+    const float* bias;
+    const uint32_t* mask;
+    const int32_t* mask_index;
+    int64_t mask_stride;
+} traj_logit_adjust;
+
+size_t traj_confidence_topk_adjusted_workspace_size(const traj_logits_shape* shape, int32_t k,
+                                                    const traj_logit_adjust* adjust);
+
+traj_status traj_confidence_topk_adjusted(const void* logits, int32_t k, float* conf, int32_t* idx,
+                                          const traj_logits_shape* shape, const traj_logit_adjust* adjust,
+                                          void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------
  * Utilities

@@ -20,6 +20,10 @@ Decoding for Diffusion LLMs):
 * :mod:`oracle.layer`      -- one verification decoder layer around the attention
   (RMSNorm, projections, rotary positions, SwiGLU MLP) with bf16 storage, and the
   same layer over whole sequences that refreshes the dual cache (App. A).
+* :mod:`oracle.paged`      -- appending rotated keys to a paged key-value cache, and
+  attention over it.
+* :mod:`oracle.adjust`     -- confidences and candidates of logits under penalties,
+  biases and masks.
 * :mod:`oracle.brute`      -- scalar-loop re-derivations used only to pin the
   functions above on tiny inputs.
 
@@ -48,6 +52,8 @@ from .accept import (  # noqa: E402
 from .tree import build_tree, build_tree_batch, gather_state_scores, level_widths  # noqa: E402
 from .layer import bf16_round, full_attention, linear, refresh_layer, verify_layer  # noqa: E402
 from .interblock import block_top1_confidence, interblock_trigger, interblock_trigger_batch, joint_peers  # noqa: E402
+from .paged import paged_append, paged_attention, rotate  # noqa: E402
+from .adjust import adjust_logits, confidence_topk_adjusted  # noqa: E402
 
 __all__ = [
     "MASK",
@@ -71,4 +77,9 @@ __all__ = [
     "joint_peers",
     "bf16_round",
     "verify_layer",
+    "rotate",
+    "paged_append",
+    "paged_attention",
+    "adjust_logits",
+    "confidence_topk_adjusted",
 ]

@@ -26,10 +26,21 @@ and :func:`verify_layer`, a whole decoder layer of the verification forward pass
 attention (norms, projections on the library's MFMA GEMM, RoPE, SwiGLU MLP), and
 :func:`linear`, that GEMM on its own; :func:`refresh_layer` runs the same layer over whole
 sequences at a block boundary and refreshes the dual cache (App. A).
+
+For serving sequences of different lengths and requests with their own rules:
+
+* :func:`paged_append` -- new tokens' keys rotated by position and written, with the values, into a
+  paged key-value cache; :func:`paged_attn` attends to it.
+* :func:`confidence_topk_adjusted` -- :func:`confidence_topk` under penalties for repeated tokens,
+  biases and grammar masks.
 """
 
 from ._lib import (  # noqa: F401
     DEV_BAD_BLOCK,
+    DEV_BAD_HISTORY,
+    DEV_BAD_LENGTH,
+    DEV_BAD_MASK,
+    DEV_BAD_PAGE,
     DEV_BAD_ROOT,
     DEV_BAD_LEAF,
     DEV_BAD_PARENT,
@@ -40,6 +51,8 @@ from ._lib import (  # noqa: F401
     built_digest,
     check_build,
     confidence_topk,
+    confidence_topk_adjusted,
+    confidence_topk_adjusted_workspace_size,
     confidence_topk_noalloc,
     confidence_topk_workspace_size,
     device_status,
@@ -52,6 +65,9 @@ from ._lib import (  # noqa: F401
     refresh_layer_workspace_size,
     verify_layer,
     load,
+    paged_append,
+    paged_attn,
+    paged_attn_workspace_size,
     tree_max_nodes,
     verify_attn,
     verify_attn_workspace_size,

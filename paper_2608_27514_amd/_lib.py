@@ -23,6 +23,10 @@ DEV_BAD_PARENT = 0x1
 DEV_BAD_LEAF = 0x2
 DEV_BAD_BLOCK = 0x4
 DEV_BAD_ROOT = 0x8
+DEV_BAD_LENGTH = 0x10
+DEV_BAD_PAGE = 0x20
+DEV_BAD_MASK = 0x40
+DEV_BAD_HISTORY = 0x80
 
 
 class TrajSpecError(RuntimeError):
@@ -74,6 +78,17 @@ class LayerWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")]
 
 
+class PagedShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "Hq", "Hkv", "D", "num_pages", "page_size", "max_pages")] + \
+               [(n, ctypes.c_int64) for n in ("table_stride", "page_stride", "token_stride", "head_stride")]
+
+
+class LogitAdjust(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows_per_seq", "history_size", "bias_size", "n_masks")] + \
+               [(n, ctypes.c_void_p) for n in ("history", "history_len", "repetition", "frequency", "presence", "bias_ids",
+                                               "bias", "mask", "mask_index")] + [("mask_stride", ctypes.c_int64)]
+
+
 _LIB = None
 
 EXPORTS = {
@@ -110,6 +125,16 @@ EXPORTS = {
                     [ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "traj_build_tree": (ctypes.c_int32, [ctypes.c_void_p] * 6 + [ctypes.POINTER(TreeShape), ctypes.c_float]
                         + [ctypes.c_void_p] * 7),
+    "traj_paged_append": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p] * 7 +
+                          [ctypes.POINTER(PagedShape), ctypes.c_float, ctypes.c_void_p]),
+    "traj_paged_attn_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(PagedShape)]),
+    "traj_paged_attn": (ctypes.c_int32, [ctypes.c_void_p] * 6 + [ctypes.POINTER(PagedShape), ctypes.c_float, ctypes.c_int32,
+                                                                 ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "traj_confidence_topk_adjusted_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(LogitsShape), ctypes.c_int32,
+                                                                       ctypes.POINTER(LogitAdjust)]),
+    "traj_confidence_topk_adjusted": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
+                                                       ctypes.POINTER(LogitsShape), ctypes.POINTER(LogitAdjust),
+                                                       ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "traj_status_string": (ctypes.c_char_p, [ctypes.c_int32]),
     "traj_version": (ctypes.c_char_p, []),
     "traj_get_device_status": (ctypes.c_int32, [ctypes.POINTER(ctypes.c_int32), ctypes.c_int32, ctypes.c_void_p]),
@@ -540,6 +565,225 @@ def linear(x, w, y=None, accumulate=False, workspace=None, stream=None):
     _check(_lib().traj_linear(_ptr(x), _ptr(w), _ptr(y), M, K, N, 1 if accumulate else 0, _ptr(workspace), ws_bytes,
                               _stream(stream)), "traj_linear")
     return y
+
+
+# ---------------------------------------------------------------- paged cache
+def _here(t, name):
+    """The library launches on the current device: a tensor of another one is refused."""
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory for a call on ``stream``: taken from that stream's pool, so that nothing frees or reuses it early."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _paged_shape(B, T, Hq, k_pages, v_pages, page_table):
+    """The shape of a paged call; checks the pools and the table."""
+    for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{n} must be a CUDA (HIP) tensor")
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"{n} must be {torch.bfloat16}, got {t.dtype}")
+        if t.dim() != 4 or t.stride(3) != 1:
+            raise ValueError(f"{n} must be [pages, page_size, Hkv, D] with a contiguous last dimension")
+    if k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride():
+        raise ValueError("k_pages and v_pages must have the same shape and strides")
+    if not isinstance(page_table, torch.Tensor) or not page_table.is_cuda or page_table.dtype != torch.int32:
+        raise TypeError("page_table must be a CUDA (HIP) tensor of torch.int32")
+    if page_table.dim() != 2 or page_table.shape[0] != B or page_table.stride(1) != 1 and page_table.shape[1] > 1:
+        raise ValueError("page_table must be [B, max_pages] with contiguous rows")
+    _here(k_pages, "k_pages")
+    pages, page_size, Hkv, D = k_pages.shape
+    st = k_pages.stride()
+    cols = page_table.shape[1]
+    # a dimension of one entry has no stride that matters
+    return PagedShape(B, T, Hq, Hkv, D, pages, page_size, cols, max(page_table.stride(0), cols) if B <= 1 else page_table.stride(0),
+                      st[0] if pages > 1 else 8, st[1] if page_size > 1 else 8, st[2] if Hkv > 1 else 8)
+
+
+def _token_rows(t, name, B, T, heads, D):
+    """Checks a [B, T, heads, D] tensor whose token rows hold their heads side by side; returns (address, row stride)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    _expect_shape(t, name, (B, T, heads, D))
+    sb, st, sh, sd = t.stride()
+    row = st if T > 1 else sb if B > 1 else heads * D
+    if sd != 1 or (heads > 1 and sh != D) or (B > 1 and T > 1 and sb != T * st):
+        raise ValueError(f"{name} must have evenly spaced token rows of contiguous heads")
+    return t.data_ptr() if t.numel() > 0 else None, row
+
+
+def _per_seq(t, name, B, dtype=torch.int32):
+    if t is None:
+        return None
+    p = _dev(t, name, dtype)
+    _expect_shape(t, name, (B,))
+    return p
+
+
+def paged_append(k, v, k_pages, v_pages, page_table, start, q=None, q_out=None, n_new=None, pos0=None,
+                 rope_theta=500000.0, stream=None):
+    """Rotates the new tokens' keys (and queries) by position and writes keys and values into the pages.
+
+    k, v [B,T,Hkv,D] and q [B,T,Hq,D] (bf16) may be views into a projection's rows; k_pages / v_pages
+    [pages, page_size, Hkv, D] with any strides but the last dimension's; page_table [B, max_pages] int32; start,
+    n_new (None: T each) and pos0 (None: start) [B] int32.  Token t of sequence b gets cache index start[b] + t and
+    position pos0[b] + t; rows t >= n_new[b] are padding and left alone.  Returns q_out [B,T,Hq,D] (allocated when
+    None; its padding rows are then zero), or None without q."""
+    B, T, Hkv, D = k.shape
+    Hq = q.shape[2] if q is not None else Hkv
+    sh = _paged_shape(B, T, Hq, k_pages, v_pages, page_table)
+    if (sh.Hkv, sh.D) != (Hkv, D):
+        raise ValueError(f"k has {Hkv} heads of {D}, the pages {sh.Hkv} of {sh.D}")
+    kp, ks = _token_rows(k, "k", B, T, Hkv, D)
+    vp, vs = _token_rows(v, "v", B, T, Hkv, D)
+    qp, qs, qop = None, 0, None
+    if q is not None:
+        qp, qs = _token_rows(q, "q", B, T, Hq, D)
+        if q_out is None:
+            if n_new is None:
+                q_out = _empty((B, T, Hq, D), torch.bfloat16, q.device, stream)
+            else:
+                with torch.cuda.stream(stream):  # None: the current one
+                    q_out = torch.zeros((B, T, Hq, D), dtype=torch.bfloat16, device=q.device)
+        qop = _dev(q_out, "q_out", torch.bfloat16)
+        _expect_shape(q_out, "q_out", (B, T, Hq, D))
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    st = _lib().traj_paged_append(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
+                                  _per_seq(start, "start", B), _per_seq(n_new, "n_new", B), _per_seq(pos0, "pos0", B),
+                                  ctypes.byref(sh), float(rope_theta), _stream(stream))
+    _check(st, "traj_paged_append")
+    return q_out
+
+
+def paged_attn_workspace_size(q, k_pages, v_pages, page_table):
+    return int(_lib().traj_paged_attn_workspace_size(ctypes.byref(_paged_shape(*q.shape[:3], k_pages, v_pages, page_table))))
+
+
+def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causal=False, workspace=None, stream=None):
+    """Attention of T new tokens per sequence, q [B,T,Hq,D] (bf16), over the first lens[b] cached keys of each
+    (causal: the new tokens are the last T of them and see those up to themselves).  Pages and table as
+    :func:`paged_append`; lens [B] int32.  Returns ``out`` [B,T,Hq,D]; a row that sees no key is zero."""
+    B, T, Hq, D = q.shape
+    qp = _dev(q, "q", torch.bfloat16)
+    sh = _paged_shape(B, T, Hq, k_pages, v_pages, page_table)
+    if sh.D != D:
+        raise ValueError(f"q has heads of {D}, the pages of {sh.D}")
+    if out is None:
+        out = _empty((B, T, Hq, D), torch.bfloat16, q.device, stream)
+    else:
+        _expect_shape(out, "out", (B, T, Hq, D))
+    outp = _dev(out, "out", torch.bfloat16)
+    lib = _lib()
+    if workspace is None:
+        need = lib.traj_paged_attn_workspace_size(ctypes.byref(sh))
+        if need > 0:
+            workspace = _empty(need, torch.uint8, q.device, stream)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = lib.traj_paged_attn(qp, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), _per_seq(lens, "lens", B), outp,
+                             ctypes.byref(sh), float(scale), 1 if causal else 0, _ptr(workspace), ws_bytes, _stream(stream))
+    _check(st, "traj_paged_attn")
+    return out
+
+
+# ---------------------------------------------------------------- adjusted logits
+def _logit_adjust(logits, rows_per_seq, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index):
+    R, V = logits.shape
+    per = int(rows_per_seq)
+    if per < 1:
+        raise ValueError("rows_per_seq must be at least 1")
+    n = -(-R // per)
+    a = LogitAdjust(rows_per_seq=per)
+    f32, i32 = torch.float32, torch.int32
+    if history is not None:
+        a.history = _dev(history, "history", i32)
+        _expect_shape(history, "history", (n, history.shape[-1]))
+        a.history_size = history.shape[-1]
+    for name, t, dt in (("history_len", history_len, i32), ("repetition", repetition, f32), ("frequency", frequency, f32),
+                        ("presence", presence, f32)):
+        if t is not None:
+            if history is None:
+                raise ValueError(f"{name} needs history")
+            setattr(a, name, _per_seq(t, name, n, dt))
+    if (bias_ids is None) != (bias is None):
+        raise ValueError("bias_ids and bias go together")
+    if bias is not None:
+        a.bias_ids, a.bias = _dev(bias_ids, "bias_ids", i32), _dev(bias, "bias", f32)
+        _expect_shape(bias, "bias", (n, bias.shape[-1]))
+        _expect_shape(bias_ids, "bias_ids", bias.shape)
+        a.bias_size = bias.shape[-1]
+    if mask is not None:
+        a.mask = _dev(mask, "mask", i32)
+        if mask.dim() != 2 or mask.shape[0] < 1 or mask.shape[1] < -(-V // 32):
+            raise ValueError(f"mask must be [n_masks, at least {-(-V // 32)}] words")
+        a.n_masks, a.mask_stride = mask.shape
+        if mask_index is None and mask.shape[0] < R:
+            raise ValueError("mask must have a row for every row of logits, or mask_index one entry")
+    if mask_index is not None:
+        if mask is None:
+            raise ValueError("mask_index needs mask")
+        a.mask_index = _per_seq(mask_index, "mask_index", R)
+    return a
+
+
+def _logit_rows(logits):
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise TypeError("logits must be a CUDA (HIP) tensor")
+    if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] > 1:
+        raise ValueError("logits must be 2-D with a contiguous last dimension")
+    sh = logits_shape(logits)
+    if sh.rows <= 1:
+        sh.row_stride = max(sh.row_stride, sh.vocab)
+    return sh
+
+
+def confidence_topk_adjusted_workspace_size(logits, k, rows_per_seq, history=None, bias=None):
+    """Bytes for a call with these logits and lists (their sizes count)."""
+    a = LogitAdjust(rows_per_seq=int(rows_per_seq), history_size=0 if history is None else history.shape[-1],
+                    bias_size=0 if bias is None else bias.shape[-1])
+    return int(_lib().traj_confidence_topk_adjusted_workspace_size(ctypes.byref(_logit_rows(logits)), int(k), ctypes.byref(a)))
+
+
+def confidence_topk_adjusted(logits, k, rows_per_seq, history=None, history_len=None, repetition=None, frequency=None,
+                             presence=None, bias_ids=None, bias=None, mask=None, mask_index=None, conf=None, idx=None,
+                             workspace=None, stream=None):
+    """:func:`confidence_topk` of the logits under each request's penalties, biases and grammar (the adjusted logits
+    are written nowhere).  Row r belongs to sequence r // rows_per_seq.  Per sequence: history [n, H] int32 with
+    history_len [n] (ids outside the vocabulary are padding, a masked position's -1 among them), repetition, frequency
+    and presence penalties [n] float32, bias_ids / bias [n, NB]; mask [n_masks, words] int32 holds a bit per token
+    (bit v % 32 of word v // 32; 0 forbids) and mask_index [R] int32 each row's mask (-1: none; without it row r takes
+    mask r).  Slots without an allowed token hold confidence 0 and index -1."""
+    sh = _logit_rows(logits)
+    _here(logits, "logits")
+    a = _logit_adjust(logits, rows_per_seq, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index)
+    R, k = logits.shape[0], int(k)
+    dev = logits.device
+    if conf is None:
+        conf = _empty((R, k), torch.float32, dev, stream)
+    if idx is None:
+        idx = _empty((R, k), torch.int32, dev, stream)
+    _dev(conf, "conf", torch.float32)
+    _dev(idx, "idx", torch.int32)
+    _expect_shape(conf, "conf", (R, k))
+    _expect_shape(idx, "idx", (R, k))
+    lib = _lib()
+    if workspace is None:
+        need = lib.traj_confidence_topk_adjusted_workspace_size(ctypes.byref(sh), k, ctypes.byref(a))
+        if need > 0:
+            workspace = _empty(need, torch.uint8, dev, stream)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = lib.traj_confidence_topk_adjusted(_ptr(logits), k, _ptr(conf), _ptr(idx), ctypes.byref(sh), ctypes.byref(a),
+                                           _ptr(workspace), ws_bytes, _stream(stream))
+    _check(st, "traj_confidence_topk_adjusted")
+    return conf, idx
 
 
 def device_status(reset=True, stream=None):

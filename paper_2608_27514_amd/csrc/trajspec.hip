@@ -10,11 +10,13 @@
 
 #include "../../include/traj_spec.h"
 #include "accept.hpp"
+#include "adjust.hpp"
 #include "common.hpp"
 #include "conf_topk.hpp"
 #include "gemm.hpp"
 #include "interblock.hpp"
 #include "layer.hpp"
+#include "paged.hpp"
 #include "tree.hpp"
 #include "verify_attn.hpp"
 #include "verify_attn16.hpp"
@@ -547,6 +549,139 @@ traj_status run_layer(uint16_t* xs, const traj_layer_weights* w, const traj_laye
     return gemm(buf(plan.act), static_cast<const uint16_t*>(w->w_down), xs, T, hidden, inter, kEpiAccumulate, split, split_bytes, s);
 }
 
+// ------------------------------------------------------------------ paged cache
+traj_status check_paged(const traj_paged_shape* sh) {
+    if (sh->B < 0 || sh->B > 65535 || sh->T < 0 || sh->Hq < 1 || sh->Hkv < 1 || sh->Hq % sh->Hkv != 0) return TRAJ_E_SHAPE;
+    if (sh->num_pages < 1 || sh->page_size < 1 || sh->max_pages < 1) return TRAJ_E_SHAPE;
+    if ((int64_t)sh->max_pages * sh->page_size >= (1ll << 31) - 256 || sh->table_stride < sh->max_pages) return TRAJ_E_SHAPE;
+    for (int64_t s : {sh->page_stride, sh->token_stride, sh->head_stride})
+        if (s < 8 || s % 8 != 0 || s > (1ll << 40)) return TRAJ_E_SHAPE;
+    if ((int64_t)sh->T * (sh->Hq / sh->Hkv) > (1 << 30) || sh->table_stride > (1ll << 40)) return TRAJ_E_SHAPE;
+    if ((sh->D != 64 && sh->D != 128) || sh->token_stride > (1 << 26)) return TRAJ_E_UNSUPPORTED;
+    return TRAJ_OK;
+}
+
+FastDiv fast_div(int64_t d) {
+    int s = 0;
+    while ((1ll << s) < d) ++s;
+    return FastDiv{(uint32_t)((((uint64_t)1 << (31 + s)) + (uint64_t)d - 1) / (uint64_t)d), 31 + s};
+}
+
+PagedCache paged_cache(const traj_paged_shape* sh, const void* k, const void* v, const int32_t* table) {
+    PagedCache c{};
+    c.k = static_cast<uint16_t*>(const_cast<void*>(k));
+    c.v = static_cast<uint16_t*>(const_cast<void*>(v));
+    c.table = table;
+    c.table_stride = sh->table_stride;
+    c.page_stride = sh->page_stride;
+    c.token_stride = sh->token_stride;
+    c.head_stride = sh->head_stride;
+    c.num_pages = sh->num_pages;
+    c.page_size = sh->page_size;
+    c.capacity = sh->max_pages * sh->page_size;
+    c.by_page = fast_div(sh->page_size);
+    return c;
+}
+
+// Row tiles of one or two 16-row fragments, and the slots that the device's split can come to: chunks of the batch's
+// keys over the target, and a last, short one per sequence.
+struct PagedPlan {
+    int frags, tiles, units;
+    int64_t slots;
+    size_t workspace;  // 0: no sequence can be split
+};
+
+PagedPlan plan_paged(const traj_paged_shape* sh) {
+    PagedPlan p{};
+    const int rows = sh->T * (sh->Hq / sh->Hkv);
+    p.frags = rows <= 16 ? 1 : 2;
+    p.tiles = (rows + 16 * p.frags - 1) / (16 * p.frags);
+    const int64_t units = (int64_t)sh->Hkv * p.tiles;
+    p.units = units > INT_MAX ? INT_MAX : (int)units;
+    const int64_t cap = (int64_t)sh->max_pages * sh->page_size;
+    p.slots = std::min<int64_t>((kPagedTargetWgs + units - 1) / units + sh->B, sh->B * ((cap + kPagedChunkMin - 1) / kPagedChunkMin));
+    p.workspace = cap <= kPagedChunkMin ? 0 : (size_t)p.slots * (size_t)units * 16 * p.frags * (sh->D + 2) * sizeof(float);
+    return p;
+}
+
+template <int D, int NR>
+void launch_paged(const PagedAttnParams& p, int64_t wgs, bool uniform, hipStream_t st) {
+    hipLaunchKernelGGL((uniform ? paged_attn_kernel<D, NR, true> : paged_attn_kernel<D, NR, false>), dim3((unsigned)wgs),
+                       dim3(kPagedThreads), 0, st, p);
+    if (!p.single)
+        hipLaunchKernelGGL((paged_join_kernel<D, NR>), dim3((unsigned)((int64_t)p.B * p.T * p.Hq)), dim3(kPagedThreads), 0, st, p);
+}
+
+// ------------------------------------------------------------------ adjusted logits
+traj_status check_adjust(const traj_logits_shape* sh, int32_t k, const traj_logit_adjust* a) {
+    const traj_status st = check_logits(sh, k);
+    if (st != TRAJ_OK) return st;
+    if (sh->vocab > kAdjustMaxVocab) return TRAJ_E_UNSUPPORTED;
+    if (a->rows_per_seq < 1 || a->history_size < 0 || a->bias_size < 0) return TRAJ_E_SHAPE;
+    if ((int64_t)a->history_size + a->bias_size >= 1 << 30) return TRAJ_E_SHAPE;
+    if (a->mask != nullptr && (a->n_masks < 1 || a->mask_stride < (sh->vocab + 31) / 32 || a->mask_stride > (1ll << 40) ||
+                               (a->mask_index == nullptr && a->n_masks < sh->rows)))
+        return TRAJ_E_SHAPE;
+    return TRAJ_OK;
+}
+
+// The workspace's parts: the sequences' bitmaps, record counts and records; then the split records.
+struct AdjustPlan {
+    TopkPlan topk;
+    int64_t n_seq;
+    int max_records;
+    size_t counts, records, partial, total;  // `partial`: what has to fit
+};
+
+AdjustPlan plan_adjust_call(const traj_logits_shape* sh, const traj_logit_adjust* a) {
+    AdjustPlan p{};
+    p.topk = plan_adjust(sh->rows, sh->vocab, vec_of(sh->dtype));
+    p.max_records = (int)std::min<int64_t>(sh->vocab, (int64_t)a->history_size + a->bias_size);
+    if (p.max_records > 0) {
+        p.n_seq = (sh->rows + a->rows_per_seq - 1) / a->rows_per_seq;
+        p.counts = align256((size_t)p.n_seq * ((sh->vocab + 31) / 32) * 4);
+        p.records = p.counts + align256((size_t)p.n_seq * 4);
+        p.partial = p.records + align256((size_t)p.n_seq * p.max_records * sizeof(AdjustRecord));
+    }
+    p.total = p.partial + (p.topk.splits > 1 ? (size_t)sh->rows * p.topk.splits * kTopkRecord * sizeof(float) : 0);
+    return p;
+}
+
+template <typename T, int K, int THREADS, int U, int DEPTH>
+void launch_adjust_kernel(const AdjustParams& A, const void* lg, const traj_logits_shape* sh, int k, const TopkPlan& plan, float* conf,
+                          int32_t* idx, float* partial, hipStream_t st) {
+    const size_t lds = ((size_t)(plan.chunk + 31) / 32 + 1) * sizeof(uint32_t);
+    hipLaunchKernelGGL((adjust_topk_kernel<T, K, THREADS, U, DEPTH>), dim3((unsigned)(sh->rows * plan.splits)), dim3(THREADS), lds, st, A,
+                       static_cast<const T*>(lg), sh->row_stride, k, plan.splits, plan.chunk, conf, idx, partial);
+}
+
+template <typename T, int K>
+traj_status launch_adjust_k(const AdjustParams& A, const void* lg, const traj_logits_shape* sh, int k, const TopkPlan& plan, float* conf,
+                            int32_t* idx, float* partial, hipStream_t st) {
+    if (plan.threads == 256)
+        launch_adjust_kernel<T, K, 256, 2, 2>(A, lg, sh, k, plan, conf, idx, partial, st);
+    else if (plan.unroll == 4)
+        launch_adjust_kernel<T, K, 512, 4, 2>(A, lg, sh, k, plan, conf, idx, partial, st);
+    else
+        launch_adjust_kernel<T, K, 512, 2, 2>(A, lg, sh, k, plan, conf, idx, partial, st);
+    const traj_status rs = launched();
+    if (rs != TRAJ_OK || plan.splits <= 1) return rs;
+    hipLaunchKernelGGL((adjust_merge_kernel<K>), dim3((unsigned)sh->rows), dim3(64), 0, st, partial, plan.splits, k, conf, idx);
+    return launched();
+}
+
+template <typename T>
+traj_status launch_adjust(const AdjustParams& A, const void* lg, const traj_logits_shape* sh, int k, const TopkPlan& plan, float* conf,
+                          int32_t* idx, float* partial, hipStream_t st) {
+    switch (k) {
+        case 1: return launch_adjust_k<T, 1>(A, lg, sh, k, plan, conf, idx, partial, st);
+        case 2: return launch_adjust_k<T, 2>(A, lg, sh, k, plan, conf, idx, partial, st);
+        case 3:
+        case 4: return launch_adjust_k<T, 4>(A, lg, sh, k, plan, conf, idx, partial, st);
+        default: return launch_adjust_k<T, 8>(A, lg, sh, k, plan, conf, idx, partial, st);
+    }
+}
+
 }  // namespace
 
 extern "C" {
@@ -808,6 +943,161 @@ traj_status traj_linear(const void* x, const void* w, void* y, int64_t M, int64_
     if (workspace != nullptr && (workspace_bytes < least || !aligned16(workspace))) return TRAJ_E_WORKSPACE;
     return gemm(static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w), static_cast<uint16_t*>(y), M, N, K,
                 accumulate != 0 ? kEpiAccumulate : kEpiStore, workspace, workspace_bytes, as_stream(stream));
+}
+
+traj_status traj_paged_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                              void* q_out, void* k_pages, void* v_pages, const int32_t* page_table, const int32_t* start,
+                              const int32_t* n_new, const int32_t* pos0, const traj_paged_shape* shape, float rope_theta, void* stream) {
+    if (shape == nullptr) return TRAJ_E_NULL;
+    const traj_status st = check_paged(shape);
+    if (st != TRAJ_OK) return st;
+    if (!(rope_theta >= 0.f) || std::isinf(rope_theta)) return TRAJ_E_ARG;
+    if (shape->B == 0 || shape->T == 0) return TRAJ_OK;
+    if (k == nullptr || v == nullptr || k_pages == nullptr || v_pages == nullptr || page_table == nullptr || start == nullptr ||
+        (q == nullptr) != (q_out == nullptr))
+        return TRAJ_E_NULL;
+    const int64_t kv_row = (int64_t)shape->Hkv * shape->D, q_row = (int64_t)shape->Hq * shape->D;
+    if (k_stride < kv_row || v_stride < kv_row || k_stride % 8 != 0 || v_stride % 8 != 0 || k_stride > (1ll << 40) || v_stride > (1ll << 40))
+        return TRAJ_E_SHAPE;
+    if (q != nullptr && (q_stride < q_row || q_stride % 8 != 0 || q_stride > (1ll << 40) || !aligned16(q) || !aligned16(q_out))) return TRAJ_E_SHAPE;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages)) return TRAJ_E_SHAPE;
+    AppendParams p{};
+    p.q = static_cast<const uint16_t*>(q);
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.q_row = q_stride;
+    p.k_row = k_stride;
+    p.v_row = v_stride;
+    p.q_out = static_cast<uint16_t*>(q_out);
+    p.cache = paged_cache(shape, k_pages, v_pages, page_table);
+    p.start = start;
+    p.n_new = n_new;
+    p.pos0 = pos0;
+    p.T = shape->T;
+    p.Hq = shape->Hq;
+    p.Hkv = shape->Hkv;
+    p.rotate = rope_theta > 0.f ? 1 : 0;
+    const int64_t per_token = ((q != nullptr ? (int64_t)shape->Hq : 0) + 2 * (int64_t)shape->Hkv) * (shape->D / 16);
+    if (per_token > (1 << 28)) return TRAJ_E_SHAPE;
+    p.per_token = (int)per_token;
+    p.by_token = fast_div(per_token);
+    if (p.rotate) {
+        const double step = std::pow((double)rope_theta, -2.0 / shape->D);
+        double turns = 0.15915494309189533577;  // 1 / 2 pi
+        for (int d = 0; d < shape->D / 2; ++d, turns *= step) p.turns[d] = turns;
+    }
+    const int tok = (int64_t)shape->B * shape->T < 1024 ? 1 : kAppendTokens;
+    const dim3 grid((unsigned)((shape->T + tok - 1) / tok), tok == 1 ? (unsigned)((per_token + kAppendThreads - 1) / kAppendThreads) : 1u,
+                    (unsigned)shape->B);
+    if (grid.y > 65535) return TRAJ_E_SHAPE;
+    auto kernel = shape->D == 128 ? (tok == 1 ? paged_append_kernel<128, 1> : paged_append_kernel<128, kAppendTokens>)
+                                  : (tok == 1 ? paged_append_kernel<64, 1> : paged_append_kernel<64, kAppendTokens>);
+    hipLaunchKernelGGL(kernel, grid, dim3(kAppendThreads), 0, as_stream(stream), p);
+    return launched();
+}
+
+size_t traj_paged_attn_workspace_size(const traj_paged_shape* shape) {
+    if (shape == nullptr || check_paged(shape) != TRAJ_OK) return 0;
+    return plan_paged(shape).workspace;
+}
+
+traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table, const int32_t* lens,
+                            void* out, const traj_paged_shape* shape, float scale, int32_t causal, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    if (shape == nullptr) return TRAJ_E_NULL;
+    const traj_status st = check_paged(shape);
+    if (st != TRAJ_OK) return st;
+    if (!(scale == scale) || std::isinf(scale)) return TRAJ_E_ARG;
+    if (shape->B == 0 || shape->T == 0) return TRAJ_OK;
+    if (q == nullptr || k_pages == nullptr || v_pages == nullptr || page_table == nullptr || lens == nullptr || out == nullptr) return TRAJ_E_NULL;
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return TRAJ_E_SHAPE;
+    const PagedPlan plan = plan_paged(shape);
+    if (workspace != nullptr && (workspace_bytes < plan.workspace || !aligned16(workspace))) return TRAJ_E_WORKSPACE;
+    PagedAttnParams p{};
+    p.q = static_cast<const uint16_t*>(q);
+    p.cache = paged_cache(shape, k_pages, v_pages, page_table);
+    p.lens = lens;
+    p.out = static_cast<uint16_t*>(out);
+    p.B = shape->B;
+    p.T = shape->T;
+    p.Hq = shape->Hq;
+    p.Hkv = shape->Hkv;
+    p.group = shape->Hq / shape->Hkv;
+    p.rows = p.T * p.group;
+    p.tiles = plan.tiles;
+    p.units = plan.units;
+    p.single = plan.workspace == 0 || workspace == nullptr;
+    p.causal = causal != 0;
+    p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)shape->D)) * 1.4426950408889634f;
+    const int64_t wgs = (p.single ? (int64_t)p.B : plan.slots) * ((int64_t)shape->Hkv * plan.tiles);
+    if (wgs > INT_MAX || (int64_t)p.B * p.T * p.Hq > INT_MAX) return TRAJ_E_SHAPE;
+    p.part_o = static_cast<float*>(workspace);
+    p.part_ml = p.part_o + (p.single ? 0 : (size_t)plan.slots * p.units * 16 * plan.frags * shape->D);
+    const bool uniform = shape->page_size % 16 == 0;
+    hipStream_t s = as_stream(stream);
+    if (shape->D == 128)
+        plan.frags == 1 ? launch_paged<128, 1>(p, wgs, uniform, s) : launch_paged<128, 2>(p, wgs, uniform, s);
+    else
+        plan.frags == 1 ? launch_paged<64, 1>(p, wgs, uniform, s) : launch_paged<64, 2>(p, wgs, uniform, s);
+    return launched();
+}
+
+size_t traj_confidence_topk_adjusted_workspace_size(const traj_logits_shape* shape, int32_t k, const traj_logit_adjust* adjust) {
+    if (shape == nullptr || adjust == nullptr || check_adjust(shape, k, adjust) != TRAJ_OK) return 0;
+    return plan_adjust_call(shape, adjust).total;
+}
+
+traj_status traj_confidence_topk_adjusted(const void* logits, int32_t k, float* conf, int32_t* idx, const traj_logits_shape* shape,
+                                          const traj_logit_adjust* adjust, void* workspace, size_t workspace_bytes, void* stream) {
+    if (shape == nullptr || adjust == nullptr) return TRAJ_E_NULL;
+    const traj_status st = check_adjust(shape, k, adjust);
+    if (st != TRAJ_OK) return st;
+    if (shape->rows == 0) return TRAJ_OK;
+    if (logits == nullptr || conf == nullptr || idx == nullptr) return TRAJ_E_NULL;
+    if (adjust->history_size > 0 && adjust->history == nullptr) return TRAJ_E_NULL;
+    if (adjust->bias_size > 0 && (adjust->bias_ids == nullptr || adjust->bias == nullptr)) return TRAJ_E_NULL;
+    if (reinterpret_cast<uintptr_t>(logits) % size_of(shape->dtype) != 0) return TRAJ_E_SHAPE;
+    AdjustPlan plan = plan_adjust_call(shape, adjust);
+    if (workspace != nullptr && !aligned16(workspace)) return TRAJ_E_WORKSPACE;
+    if (workspace == nullptr) workspace_bytes = 0;
+    if (workspace_bytes < plan.partial) return TRAJ_E_WORKSPACE;
+    if (workspace_bytes < plan.total) {  // no room for split records
+        plan.topk.splits = 1;
+        plan.topk.chunk = (int)shape->vocab;
+    }
+    char* ws = static_cast<char*>(workspace);
+    AdjustParams p{};
+    p.history = adjust->history;
+    p.history_len = adjust->history_len;
+    p.repetition = adjust->history_size > 0 ? adjust->repetition : nullptr;
+    p.frequency = adjust->frequency;
+    p.presence = adjust->presence;
+    p.bias_ids = adjust->bias_ids;
+    p.bias = adjust->bias;
+    p.H = adjust->history_size;
+    p.NB = adjust->bias_size;
+    p.rows_per_seq = adjust->rows_per_seq;
+    p.max_records = plan.max_records;
+    p.mask = adjust->mask;
+    p.mask_index = adjust->mask_index;
+    p.mask_stride = adjust->mask_stride;
+    p.n_masks = adjust->n_masks;
+    p.V = (int)shape->vocab;
+    p.words = (p.V + 31) / 32;
+    hipStream_t s = as_stream(stream);
+    if (plan.max_records > 0) {
+        p.special = reinterpret_cast<uint32_t*>(ws);
+        p.n_records = reinterpret_cast<int32_t*>(ws + plan.counts);
+        p.records = reinterpret_cast<AdjustRecord*>(ws + plan.records);
+        const int groups = (p.V + kAdjustGroup - 1) / kAdjustGroup;
+        const size_t lds = ((size_t)groups * (kAdjustGroup / 32 + 1) + 2 * kAdjustWindow) * 4;
+        hipLaunchKernelGGL(adjust_prepare_kernel, dim3((unsigned)plan.n_seq), dim3(kAdjustPrepThreads), lds, s, p);
+        const traj_status rs = launched();
+        if (rs != TRAJ_OK) return rs;
+    }
+    float* partial = plan.topk.splits > 1 ? reinterpret_cast<float*>(ws + plan.partial) : nullptr;
+    return shape->dtype == TRAJ_BF16 ? launch_adjust<uint16_t>(p, logits, shape, k, plan.topk, conf, idx, partial, s)
+                                     : launch_adjust<float>(p, logits, shape, k, plan.topk, conf, idx, partial, s);
 }
 
 // For the tests: the plan of a product with all the workspace it asks for, as tile rows and columns and k
