@@ -431,7 +431,7 @@ traj_status traj_linear(const void* x, const void* w, void* y, int64_t M, int64_
  * sequence's last page are never read.  Sequences may share pages that neither writes.
  * Limits (all entry points): B >= 0 and T >= 0 (0 = no-op) with B <= 65535; D in {64, 128};
  *   Hq % Hkv == 0; num_pages, page_size, max_pages >= 1 with max_pages * page_size < 2^31 - 256;
- *   strides positive multiples of 8 with token_stride <= 2^26; pools and q / k / v rows 16-byte
+ *   strides positive multiples of 8 with token_stride <= 2^25; pools and q / k / v rows 16-byte
  *   aligned; table_stride >= max_pages.
  * ------------------------------------------------------------------------------------ */
 typedef struct {

@@ -7,6 +7,8 @@
 //   paged_join_kernel     joins the partial results of sequences whose keys were split over workgroups
 #pragma once
 
+#include <type_traits>
+
 #include "layer.hpp"
 #include "verify_attn16.hpp"
 
@@ -125,21 +127,34 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(AppendPara
 // ------------------------------------------------------------------ attention
 // Work: a workgroup takes `16 NR` query rows of one (sequence, kv head) (row = new token * group + head in
 // group) and a range of the sequence's keys; its 4 waves take 32-key tiles of the range in turn, each with its own
-// running softmax state, merged through LDS at the end.  A step reads every cached key and value once and does
+// running softmax state, merged through LDS at the end.  The call reads every cached key and value once and does
 // T Hq / Hkv multiply-adds per element read, so up to some hundreds of rows the stream of K and V bounds it:
 // rows are padded to 16 for the matrix core, which idles either way.
 //   S^T = K Q^T with K fragments loaded straight from the pages into the A operand (no wave shares another's
 //   keys); V goes through the wave's own LDS tile for the transposing reads of O^T += V^T P^T (layouts of
-//   the 16-row verification kernel).  The next tile's K loads are issued behind the score MFMAs and its V
-//   loads behind the LDS writes, so one tile of each is always in flight; page numbers are fetched a tile earlier.
+//   the 16-row verification kernel).  DEPTH tiles are held in registers: a tile's K registers are requested anew
+//   behind its score MFMAs and its V registers behind the LDS writes; page numbers are requested a tile earlier.
 //
 // Splits: the device computes from the lengths how many keys a workgroup takes (`chunk`), so that the batch makes
 // about kPagedTargetWgs workgroups whatever the lengths are; slot = index of a (sequence, range) pair in order.
 constexpr int kPagedWaves = 4;
 constexpr int kPagedThreads = kPagedWaves * 64;
 constexpr int kPagedTile = 32;
-constexpr int kPagedChunkMin = kPagedWaves * kPagedTile;
-constexpr int kPagedTargetWgs = 1024;
+constexpr int kPagedGranule = kPagedWaves * kPagedTile;
+#ifndef X_TARGET
+#define X_TARGET 2048
+#endif
+#ifndef X_FILL
+#define X_FILL 512
+#endif
+#ifndef X_CHUNK
+#define X_CHUNK 512
+#endif
+#ifndef X_NT
+#define X_NT 1
+#endif
+constexpr int kPagedFillWgs = X_FILL, kPagedMostWgs = X_TARGET, kPagedChunk = X_CHUNK;
+constexpr int kPagedWhole = 256;
 
 struct PagedAttnParams {
     const uint16_t* q;
@@ -166,13 +181,13 @@ __device__ __forceinline__ int paged_length(const PagedAttnParams& P, int b, boo
     return len;
 }
 
-// Keys per workgroup: the batch's keys times units over the target, in whole rounds of the waves' tiles.
-// Every wave computes the same from the same lengths (whole numbers; the quotient by a power of two is exact).
+// Keys per workgroup.  Every wave computes the same from the same lengths (whole numbers, quotients by powers of two).
 __device__ __forceinline__ int paged_chunk(int64_t total, int units, int capacity) {
-    const double per = (double)total * (double)units / (double)(kPagedTargetWgs * kPagedChunkMin);
-    const double most = (double)(capacity / kPagedChunkMin + 1);
-    const int rounds = (int)ceil(per < most ? per : most);
-    return kPagedChunkMin * (rounds < 1 ? 1 : rounds);
+    const double work = (double)total * (double)units / kPagedGranule;  // of all workgroups together
+    double per = fmax(work / kPagedMostWgs, fmin(work / kPagedFillWgs, (double)(kPagedChunk / kPagedGranule)));
+    per = fmin(per, (double)(capacity / kPagedGranule + 1));
+    const int granules = (int)ceil(per);
+    return kPagedGranule * (granules < 1 ? 1 : granules);
 }
 
 // The range that `slot` stands for (by == false), or the ranges of sequence `slot` (by == true); false where
@@ -218,49 +233,60 @@ __device__ __forceinline__ bool paged_range(const PagedAttnParams& P, int slot, 
     return false;
 }
 
-// Where a tile's 32 keys lie.  UNIFORM (page_size % 16 == 0): each 16-key block within one page, so its base is
-// uniform; otherwise lane l holds the offset of key l % 32.  vis: visible keys (inside the range, on a good page).
+// Where a tile's 32 keys lie.  UNIFORM (page_size % 16 == 0): each 16-key block within one page, so its page
+// comes by a scalar load and its base is uniform; otherwise lane l holds the page and the offset of key l % 32.
+// vis: visible keys (inside the range, on a good page).
 template <bool UNIFORM>
-struct PagedTile;
-template <>
-struct PagedTile<true> {
-    int64_t base[2];
+struct PagedTile {
+    int64_t at[UNIFORM ? 2 : 1];
     uint32_t vis;
 };
-template <>
-struct PagedTile<false> {
-    int64_t off;
-    uint32_t vis;
+template <bool UNIFORM>
+struct PagedPages {
+    int page[UNIFORM ? 2 : 1];
 };
+typedef const __attribute__((address_space(4))) int32_t const_i32_t;  // read by scalar loads where uniform
 
+// Page numbers of the tile at key0: only requested here, looked at a tile later.  Keys at or behind `end`
+// take the place of `first`, which lies before it.
 template <bool UNIFORM>
-__device__ __forceinline__ PagedTile<UNIFORM> paged_tile(const PagedCache& C, const int32_t* row, int64_t head, int key0, int end) {
-    PagedTile<UNIFORM> t;
+__device__ __forceinline__ PagedPages<UNIFORM> paged_pages(const PagedCache& C, const int32_t* row, int key0, int first, int end) {
+    PagedPages<UNIFORM> p;
     if constexpr (UNIFORM) {
-        t.vis = 0;
+        const_i32_t* table = (const_i32_t*)(uintptr_t)row;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int key = key0 + 16 * j;
-            const int at = key < end ? key : key0;  // a block behind the end reads the first one's rows
-            const int col = C.by_page.div(at);
-            int page = __builtin_amdgcn_readfirstlane(row[col]);
-            const bool good = page >= 0 && page < C.num_pages;
-            if (!good) page = 0;
-            const int n = key < end && good ? (end - key < 16 ? end - key : 16) : 0;
-            t.vis |= ((1u << n) - 1u) << (16 * j);
-            if (!good && key < end && (threadIdx.x & 63) == 0) flag_device_status(kDevBadPage);
-            t.base[j] = page * C.page_stride + (at - col * C.page_size) * C.token_stride + head;
-        }
+        for (int j = 0; j < 2; ++j) p.page[j] = table[C.by_page.div(key0 + 16 * j < end ? key0 + 16 * j : first)];
     } else {
         const int key = key0 + (threadIdx.x & 31);
-        const int at = key < end ? key : key0;
-        const int col = C.by_page.div(at);
-        int page = row[col];
-        const bool good = page >= 0 && page < C.num_pages;
-        if (!good) page = 0;
-        if (!good && key < end) flag_device_status(kDevBadPage);
-        t.vis = (uint32_t)ballot64(good && key < end);
-        t.off = page * C.page_stride + (at - col * C.page_size) * C.token_stride + head;
+        p.page[0] = row[C.by_page.div(key < end ? key : first)];
+    }
+    return p;
+}
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+template <bool UNIFORM>
+__device__ __forceinline__ PagedTile<UNIFORM> paged_tile(const PagedCache& C, const PagedPages<UNIFORM>& p, int64_t head, int key0,
+                                                         int first, int end, bool& bad) {
+    PagedTile<UNIFORM> t;
+    t.vis = 0;
+#pragma unroll
+    for (int j = 0; j < (UNIFORM ? 2 : 1); ++j) {
+        const int key = UNIFORM ? key0 + 16 * j : key0 + (int)(threadIdx.x & 31);
+        const int at = key < end ? key : first;
+        const bool good = p.page[j] >= 0 && p.page[j] < C.num_pages;
+        bad |= !good && key < end;
+        if constexpr (UNIFORM) {
+            const int n = key < end && good ? (end - key < 16 ? end - key : 16) : 0;
+            t.vis |= ((1u << n) - 1u) << (16 * j);
+        } else {
+            t.vis = (uint32_t)ballot64(good && key < end);
+        }
+        t.at[j] = (good ? p.page[j] : 0) * C.page_stride + (at - C.by_page.div(at) * C.page_size) * C.token_stride + head;
+        if (UNIFORM) t.at[j] = uniform64(t.at[j]);
     }
     return t;
 }
@@ -269,15 +295,17 @@ template <int D, int NR>
 struct PagedGeom {
     static constexpr int kRows = 16 * NR;
     static constexpr int kRowF = D + 4;  // floats per row of the merge buffers: rows start 4 banks apart
-    static constexpr int kTileBytes = kPagedTile * D * 2;
+    static constexpr int kKRow = D + 8;   // elements per row of a K tile: the 16 rows of a fragment read start 4 banks apart
+    static constexpr int kVRow = D + 16;  // elements per row of a V tile: the 8 rows that half a wave reads of a transposing
+                                          // load start 8 banks apart (72 and 40 words a row) and each takes 8 of the 64
+    static constexpr int kTileBytes = kPagedTile * kVRow * 2;
     static constexpr int kMergeBytes = kRows * kRowF * 4;
     static constexpr int kWaveBytes = kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes;
 };
 
-template <int D, int NR, bool UNIFORM>
-__global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(PagedAttnParams P) {
+template <int D, int NR, bool UNIFORM, int DEPTH, bool ONCE>
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnParams P) {
     using G = PagedGeom<D, NR>;
-    using AG = AttnGeom<D, 16>;
     constexpr int KS = D / 32;       // k steps of the scores
     constexpr int NDB = D / 16;      // head-dim blocks of the output
     constexpr int RPI = 512 / D;     // V rows per wave-wide 16-byte load
@@ -287,11 +315,14 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(PagedAttnPara
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int q4 = lane >> 4, l16 = lane & 15;
-    const int id = xcd_logical_id(blockIdx.x, gridDim.x);
-    const int slot = id / P.units, unit = id - slot * P.units;
-    const int g = unit / P.tiles, tile_row = (unit - g * P.tiles) * G::kRows;
+    // Workgroup i runs on XCD i % 8.  The row tiles of one (slot, kv head) follow each other on one XCD, whose L2
+    // they share; the (slot, kv head) pairs go round the XCDs in order, so that slots without work, the last ones,
+    // leave none of them idle.
+    const int turn = blockIdx.x / 8 / P.tiles, row_tile = blockIdx.x / 8 - turn * P.tiles;
+    const int pair = turn * 8 + blockIdx.x % 8, slot = pair / P.Hkv, g = pair - slot * P.Hkv;
+    const int unit = g * P.tiles + row_tile, tile_row = row_tile * G::kRows;
     PagedRange r;
-    if (!paged_range(P, slot, false, id == 0, r)) return;
+    if (!paged_range(P, slot, false, blockIdx.x == 0, r)) return;
     const int b = r.b, len = r.len;
     const int begin = r.split * r.chunk, end = len - begin > r.chunk ? begin + r.chunk : len;
 
@@ -300,22 +331,21 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(PagedAttnPara
     int limit[NR];  // keys that the row sees
 #pragma unroll
     for (int f = 0; f < NR; ++f) {
-        const int row = tile_row + 16 * f + l16;
+        const int row = min(tile_row + 16 * f + l16, P.rows - 1);  // rows past the last repeat it and are not stored
         const int t = row / P.group, h = g * P.group + row - t * P.group;
         limit[f] = P.causal ? len - P.T + t + 1 : len;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            qf[f][ks] = bf16x8_t{};
-            if (row < P.rows) qf[f][ks] = __builtin_bit_cast(bf16x8_t, ldg16(P.q + (((int64_t)b * P.T + t) * P.Hq + h) * D + 32 * ks + 8 * q4));
-        }
+        for (int ks = 0; ks < KS; ++ks)
+            qf[f][ks] = __builtin_bit_cast(bf16x8_t, ldg16(P.q + (((int64_t)b * P.T + t) * P.Hq + h) * D + 32 * ks + 8 * q4));
     }
     const int min_limit = P.causal ? len - P.T + 1 : len;
 
     f32x4_t o[NR][NDB];
-    float m[NR], neg_mc[NR], lsum[NR];
+    float m[NR], thr[NR], neg_mc[NR], lsum[NR];
 #pragma unroll
     for (int f = 0; f < NR; ++f) {
         m[f] = kNegInf;
+        thr[f] = kNegInf;
         neg_mc[f] = 0.f;
         lsum[f] = 0.f;
 #pragma unroll
@@ -323,46 +353,45 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(PagedAttnPara
     }
 
     uint16_t* vt = reinterpret_cast<uint16_t*>(lds + wave * G::kWaveBytes);
-    int vq[NDB];
-    {
-        const int vr = 4 * q4 + (l16 >> 2);
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) {
-            const int chunk = 2 * db + ((l16 & 3) >> 1);
-            vq[db] = vr * D + ((chunk ^ AG::v_rot(vr)) << 3) + (l16 & 1) * 4;
-        }
-    }
+    const uint16_t* kread = vt + l16 * G::kKRow + 8 * q4;
+    const uint16_t* vread = vt + (4 * q4 + (l16 >> 2)) * G::kVRow + 4 * (l16 & 3);
     const int vrow = lane / (D / 8), vchunk = lane % (D / 8);  // of a V load
+    uint16_t* kwrite = vt + vrow * G::kKRow + 8 * vchunk;
+    uint16_t* vwrite = vt + vrow * G::kVRow + 8 * vchunk;
 
     const PagedCache& C = P.cache;
     const int32_t* row = C.table + b * C.table_stride;
     const int64_t head = g * C.head_stride;
-    const float c = P.scale_log2;
-    u32x4_t kr[2][KS], vr[NVL];
+    const float c = P.scale_log2, lazy = kLazyLog2 / c;
+    const int first = begin + wave * kPagedTile;
+    u32x4_t kr[DEPTH][NVL], vr[DEPTH][NVL];
+    uint32_t vis[DEPTH];
+    bool bad = false;
 
-    auto load_k = [&](const PagedTile<UNIFORM>& t) {
+    int voff[16 / RPI];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint16_t* p;
-            if constexpr (UNIFORM)
-                p = C.k + t.base[j] + (l16 * (int)C.token_stride + 8 * q4);
-            else
-                p = C.k + __shfl(t.off, 16 * j + l16) + 8 * q4;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) kr[j][ks] = ldg16(p + 32 * ks);
-        }
-    };
-    auto load_v = [&](const PagedTile<UNIFORM>& t) {
+    for (int i = 0; i < 16 / RPI; ++i) voff[i] = 2 * ((i * RPI + vrow) * (int)C.token_stride + 8 * vchunk);
+    // A tile's rows of K or V, whole 128-byte lines per load.  UNIFORM: a buffer of each block's visible rows with
+    // 32-bit lane offsets, so that rows behind its end read as 0.
+    auto load = [&](u32x4_t (&x)[NVL], const uint16_t* pool, const PagedTile<UNIFORM>& t) {
 #pragma unroll
         for (int i = 0; i < NVL; ++i) {
-            if constexpr (UNIFORM)
-                vr[i] = ldg16(C.v + t.base[i * RPI / 16] + (((i * RPI) % 16 + vrow) * (int)C.token_stride + 8 * vchunk));
-            else
-                vr[i] = ldg16(C.v + __shfl(t.off, i * RPI + vrow) + 8 * vchunk);
+            if constexpr (UNIFORM) {
+                const int j = i * RPI / 16, rows = __popc(t.vis >> (16 * j) & 0xffffu);
+                const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)(pool + t.at[j]), (short)0, rows * 2 * (int)C.token_stride, kBufferFlags);
+                x[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, voff[i % (16 / RPI)], 0, ONCE ? 2 : 0);
+            } else {
+                const u32x4_t* p = reinterpret_cast<const u32x4_t*>(pool + __shfl(t.at[0], i * RPI + vrow) + 8 * vchunk);
+                x[i] = ONCE ? __builtin_nontemporal_load(p) : *p;
+            }
         }
     };
-    // one tile; `next`: the tile whose loads it issues, if there is one
-    auto step = [&](int key0, uint32_t vis, bool more, const PagedTile<UNIFORM>& next) {
+    PagedPages<UNIFORM> pages;  // of the tile after those in flight
+    // The tile at key0, held in ring slot u; with `more` also the loads of the tile DEPTH rounds behind it.
+    auto step = [&](auto slot, int key0, bool more) {
+        constexpr int u = decltype(slot)::value;
+#pragma unroll
+        for (int i = 0; i < NVL; ++i) *reinterpret_cast<u32x4_t*>(kwrite + i * RPI * G::kKRow) = kr[u][i];
         f32x4_t s[NR][2];
 #pragma unroll
         for (int f = 0; f < NR; ++f)
@@ -371,35 +400,49 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(PagedAttnPara
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < 2; ++j) {
+                const bf16x8_t kf = lds16(kread + 16 * j * G::kKRow + 32 * ks);
 #pragma unroll
-                for (int f = 0; f < NR; ++f)
-                    s[f][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kr[j][ks]), qf[f][ks], s[f][j], 0, 0, 0);
-        if (more) load_k(next);
-        const bool whole = vis == 0xffffffffu && key0 + kPagedTile <= min_limit;
-        bf16x8_t pf[NR];
+                for (int f = 0; f < NR; ++f) s[f][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[f][ks], s[f][j], 0, 0, 0);
+            }
+        PagedTile<UNIFORM> next;
+        if (more) {
+            next = paged_tile<UNIFORM>(C, pages, head, key0 + DEPTH * kPagedGranule, first, end, bad);
+            pages = paged_pages<UNIFORM>(C, row, key0 + (DEPTH + 1) * kPagedGranule, first, end);
+            load(kr[u], C.k, next);
+        }
+        if (vis[u] != 0xffffffffu || key0 + kPagedTile > min_limit) {  // rare: a sequence's last tile
 #pragma unroll
-        for (int f = 0; f < NR; ++f) {
-            if (!whole) {
+            for (int f = 0; f < NR; ++f)
 #pragma unroll
                 for (int v = 0; v < 8; ++v) {
                     const int k = 16 * (v >> 2) + 4 * q4 + (v & 3);
-                    const bool seen = ((vis >> k) & 1u) != 0u && key0 + k < limit[f];
+                    const bool seen = ((vis[u] >> k) & 1u) != 0u && key0 + k < limit[f];
                     s[f][v >> 2][v & 3] = seen ? s[f][v >> 2][v & 3] : kNegInf;
                 }
-            }
-            float mx = kNegInf;
+            // V rows that are not visible may hold anything and count as 0 (a block's buffer ends before them)
+            if constexpr (!UNIFORM) {
 #pragma unroll
-            for (int v = 0; v < 8; ++v) mx = fmaxf(mx, s[f][v >> 2][v & 3]);
+                for (int i = 0; i < NVL; ++i)
+                    if (((vis[u] >> (i * RPI + vrow)) & 1u) == 0u) vr[u][i] = u32x4_t{};
+            }
+        }
+        bf16x8_t pf[NR];
+#pragma unroll
+        for (int f = 0; f < NR; ++f) {
+            float mx = s[f][0][0];
+#pragma unroll
+            for (int v = 1; v < 8; ++v) mx = __builtin_elementwise_maximum(mx, s[f][v >> 2][v & 3]);
             mx = quad_max(mx);
-            const bool up = mx > m[f];
-            if (ballot64(up) != 0ull) {
+            const bool up = mx > thr[f];
+            if (ballot64(up) != 0ull) {  // the reference follows the maximum in steps of at least 2^8
                 const float m_new = up ? mx : m[f];
-                const float alpha = up ? fast_exp2((m[f] - m_new) * c) : 1.0f;  // 0 from the first reference on
+                const float alpha = up ? fast_exp2((m[f] - m_new) * c) : 1.0f;  // 0 at the first reference
                 lsum[f] *= alpha;
 #pragma unroll
                 for (int db = 0; db < NDB; ++db) o[f][db] *= alpha;
                 m[f] = m_new;
+                thr[f] = m_new + lazy;
                 neg_mc[f] = m_new == kNegInf ? 0.f : -m_new * c;
             }
 #pragma unroll
@@ -409,40 +452,64 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(PagedAttnPara
                 pf[f][v] = (__bf16)p;
             }
         }
-        // V into the wave's tile; rows that are not visible may hold anything and count as 0
 #pragma unroll
         for (int i = 0; i < NVL; ++i) {
-            const int rr = i * RPI + vrow;
-            u32x4_t x = vr[i];
-            if (vis != 0xffffffffu && ((vis >> rr) & 1u) == 0u) x = u32x4_t{};
-            *reinterpret_cast<u32x4_t*>(vt + rr * D + ((vchunk ^ AG::v_rot(rr & 15)) << 3)) = x;
+            *reinterpret_cast<u32x4_t*>(vwrite + i * RPI * G::kVRow) = vr[u][i];
         }
-        if (more) load_v(next);
+        if (more) {
+            load(vr[u], C.v, next);
+            vis[u] = next.vis;
+        }
 #pragma unroll
         for (int db = 0; db < NDB; ++db) {
-            const bf16x4_t a0 = lds_read_tr(vt + vq[db]);
-            const bf16x4_t a1 = lds_read_tr(vt + vq[db] + 16 * D);
+            const bf16x4_t a0 = lds_read_tr(vread + 16 * db);
+            const bf16x4_t a1 = lds_read_tr(vread + 16 * db + 16 * G::kVRow);
             const bf16x8_t va = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
             for (int f = 0; f < NR; ++f) o[f][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[f], o[f][db], 0, 0, 0);
         }
     };
 
-    int key0 = begin + wave * kPagedTile;
-    if (key0 < end) {
-        PagedTile<UNIFORM> cur = paged_tile<UNIFORM>(C, row, head, key0, end);
-        load_k(cur);
-        load_v(cur);
-        PagedTile<UNIFORM> nxt = cur;
-        if (key0 + kPagedChunkMin < end) nxt = paged_tile<UNIFORM>(C, row, head, key0 + kPagedChunkMin, end);
-        while (key0 + kPagedChunkMin < end) {
-            const PagedTile<UNIFORM> now = cur;
-            cur = nxt;
-            if (key0 + 2 * kPagedChunkMin < end) nxt = paged_tile<UNIFORM>(C, row, head, key0 + 2 * kPagedChunkMin, end);
-            step(key0, now.vis, true, cur);
-            key0 += kPagedChunkMin;
+    int left = first < end ? (end - first + kPagedGranule - 1) / kPagedGranule : 0;  // tiles of this wave
+    if (left > 0) {
+        using Slot0 = std::integral_constant<int, 0>;
+        using Slot1 = std::integral_constant<int, DEPTH - 1>;
+        auto fetch = [&](int u) { return paged_pages<UNIFORM>(C, row, first + u * kPagedGranule, first, end); };
+        auto request = [&](auto slot, const PagedPages<UNIFORM>& p) {
+            constexpr int u = decltype(slot)::value;
+            const PagedTile<UNIFORM> t = paged_tile<UNIFORM>(C, p, head, first + u * kPagedGranule, first, end, bad);
+            vis[u] = t.vis;
+            load(kr[u], C.k, t);
+            load(vr[u], C.v, t);
+        };
+        const PagedPages<UNIFORM> p0 = fetch(0), p1 = fetch(DEPTH - 1);
+        pages = fetch(DEPTH);
+        int key0 = first;
+        // No load under a condition ahead of the loop: the compiler's waits count the loads that every path issued.
+        if constexpr (DEPTH == 1) {
+            request(Slot0{}, p0);
+            for (; left > 1; --left, key0 += kPagedGranule) step(Slot0{}, key0, true);
+            step(Slot0{}, key0, false);
+        } else if (left == 1) {
+            request(Slot0{}, p0);
+            step(Slot0{}, key0, false);
+        } else {
+            request(Slot0{}, p0);
+            request(Slot1{}, p1);
+            for (; left > 3; left -= 2, key0 += 2 * kPagedGranule) {
+                step(Slot0{}, key0, true);
+                step(Slot1{}, key0 + kPagedGranule, true);
+            }
+            if (left > 2) {
+                step(Slot0{}, key0, true);
+                step(Slot1{}, key0 + kPagedGranule, false);
+                step(Slot0{}, key0 + 2 * kPagedGranule, false);
+            } else {
+                step(Slot0{}, key0, false);
+                step(Slot1{}, key0 + kPagedGranule, false);
+            }
         }
-        step(key0, cur.vis, false, cur);
+        if (ballot64(bad) != 0ull && lane == 0) flag_device_status(kDevBadPage);
     }
 
     // waves -> workgroup
@@ -493,53 +560,73 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(PagedAttnPara
     }
 }
 
-// One workgroup per (sequence, new token, query head): 8 (D = 128) or 16 (D = 64) ranges at a time, each by D / 4
-// lanes, joined through LDS.  Sequences in one range were written by the attention itself.
-template <int D, int NR>
-__global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedAttnParams P) {
-    constexpr int LPR = D / 4, GR = kPagedThreads / LPR;
-    __shared__ f32x4_t sh_o[GR][LPR];
-    __shared__ float sh_w[kPagedWaves][2];
-    __shared__ float sh_l[GR];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t orow = blockIdx.x;
+// THREADS threads per (sequence, new token, query head): each range by D / 4 lanes, THREADS * 4 / D ranges at a time,
+// every group with its own running maximum, joined through LDS in the groups' order.  Sequences in one range were
+// written by the attention itself.
+template <int D, int NR, int THREADS>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void paged_join_kernel(PagedAttnParams P) {
+    constexpr int LPR = D / 4, GR = THREADS / LPR, ROWS = THREADS < 256 ? 256 / THREADS : 1, U = 4;
+    static_assert(THREADS >= 64, "a row's lanes of a wave have one sequence");
+    __shared__ f32x4_t sh_o[ROWS][GR][LPR];
+    __shared__ float sh_m[ROWS][GR], sh_l[ROWS][GR];
+    const int mine = threadIdx.x / THREADS, tid = threadIdx.x % THREADS;
+    const int64_t rows = (int64_t)P.B * P.T * P.Hq;
+    const int64_t orow = min((int64_t)blockIdx.x * ROWS + mine, rows - 1);
     const int h = (int)(orow % P.Hq);
     const int64_t bt = orow / P.Hq;
     const int b = (int)(bt / P.T), t = (int)(bt - (int64_t)b * P.T);
-    PagedRange r;
-    if (!paged_range(P, b, true, false, r) || r.n <= 1) return;
+    PagedRange r{};
+    paged_range(P, b, true, false, r);
     const int g = h / P.group, qrow = t * P.group + h - g * P.group;
     const int unit = g * P.tiles + qrow / (16 * NR), rr = qrow % (16 * NR);
-    auto at = [&](int s) { return ((int64_t)(r.slot0 + s) * P.units + unit) * (16 * NR) + rr; };
-    // the joint maximum
-    float M = kNegInf;
-    for (int s = threadIdx.x; s < r.n; s += kPagedThreads) M = fmaxf(M, P.part_ml[2 * at(s)]);
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
-    if (lane == 0) sh_w[wave][0] = M;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) M = fmaxf(M, sh_w[w][0]);
-    const float Ms = M == kNegInf ? 0.f : M;
-    const int grp = threadIdx.x / LPR, d = threadIdx.x % LPR;
+    const int64_t at0 = ((int64_t)r.slot0 * P.units + unit) * (16 * NR) + rr, step = (int64_t)P.units * (16 * NR);
+    const int grp = tid / LPR, d = tid % LPR;
+    const int n = r.n > 1 ? r.n : 0;
     f32x4_t acc = {};
-    float l = 0.f;
-    for (int s = grp; s < r.n; s += GR) {
-        const int64_t a = at(s);
-        const float e = fast_exp2((P.part_ml[2 * a] - Ms) * P.scale_log2);
-        l += e * P.part_ml[2 * a + 1];
-        acc += e * *reinterpret_cast<const f32x4_t*>(P.part_o + a * D + 4 * d);
+    float m = kNegInf, l = 0.f;
+    for (int s0 = grp; s0 < n; s0 += U * GR) {
+        f32x4_t x[U];
+        float xm[U], xl[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t a = at0 + min(s0 + u * GR, n - 1) * step;
+            x[u] = *reinterpret_cast<const f32x4_t*>(P.part_o + a * D + 4 * d);
+            xm[u] = s0 + u * GR < n ? P.part_ml[2 * a] : kNegInf;
+            xl[u] = P.part_ml[2 * a + 1];
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = fmaxf(top, xm[u]);
+        const float ref = top == kNegInf ? 0.f : top;
+        const float keep = fast_exp2((m - ref) * P.scale_log2);
+        acc *= keep;
+        l *= keep;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float e = fast_exp2((xm[u] - ref) * P.scale_log2);
+            acc += e * x[u];
+            l += e * xl[u];
+        }
+        m = top;
     }
-    sh_o[grp][d] = acc;
-    if (d == 0) sh_l[grp] = l;
+    sh_o[mine][grp][d] = acc;
+    if (d == 0) {
+        sh_m[mine][grp] = m;
+        sh_l[mine][grp] = l;
+    }
     __syncthreads();
-    if (grp != 0) return;
+    if (grp != 0 || n == 0 || (int64_t)blockIdx.x * ROWS + mine >= rows) return;
+    float top = kNegInf;
+#pragma unroll
+    for (int w = 0; w < GR; ++w) top = fmaxf(top, sh_m[mine][w]);
+    const float ref = top == kNegInf ? 0.f : top;
     l = 0.f;
     acc = f32x4_t{};
 #pragma unroll
     for (int w = 0; w < GR; ++w) {
-        l += sh_l[w];
-        acc += sh_o[w][d];
+        const float e = fast_exp2((sh_m[mine][w] - ref) * P.scale_log2);
+        l += e * sh_l[mine][w];
+        acc += e * sh_o[mine][w][d];
     }
     const float inv = l > 0.f ? 1.0f / l : 0.f;
     u32x2_t w2;

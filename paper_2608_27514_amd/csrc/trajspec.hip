@@ -557,7 +557,7 @@ traj_status check_paged(const traj_paged_shape* sh) {
     for (int64_t s : {sh->page_stride, sh->token_stride, sh->head_stride})
         if (s < 8 || s % 8 != 0 || s > (1ll << 40)) return TRAJ_E_SHAPE;
     if ((int64_t)sh->T * (sh->Hq / sh->Hkv) > (1 << 30) || sh->table_stride > (1ll << 40)) return TRAJ_E_SHAPE;
-    if ((sh->D != 64 && sh->D != 128) || sh->token_stride > (1 << 26)) return TRAJ_E_UNSUPPORTED;
+    if ((sh->D != 64 && sh->D != 128) || sh->token_stride > (1 << 25)) return TRAJ_E_UNSUPPORTED;
     return TRAJ_OK;
 }
 
@@ -599,17 +599,33 @@ PagedPlan plan_paged(const traj_paged_shape* sh) {
     const int64_t units = (int64_t)sh->Hkv * p.tiles;
     p.units = units > INT_MAX ? INT_MAX : (int)units;
     const int64_t cap = (int64_t)sh->max_pages * sh->page_size;
-    p.slots = std::min<int64_t>((kPagedTargetWgs + units - 1) / units + sh->B, sh->B * ((cap + kPagedChunkMin - 1) / kPagedChunkMin));
-    p.workspace = cap <= kPagedChunkMin ? 0 : (size_t)p.slots * (size_t)units * 16 * p.frags * (sh->D + 2) * sizeof(float);
+    // what paged_chunk() comes to at most: chunks of total * units / kPagedMostWgs keys or more, and of kPagedChunk or
+    // more once there are kPagedFillWgs of them
+    const auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
+    const int64_t most = std::max(up(kPagedFillWgs, units), std::min(up(kPagedMostWgs, units), sh->B * up(cap, kPagedChunk)));
+    p.slots = std::min<int64_t>(most + sh->B, sh->B * up(cap, kPagedGranule));
+    p.workspace = cap <= kPagedWhole ? 0 : (size_t)p.slots * (size_t)units * 16 * p.frags * (sh->D + 2) * sizeof(float);
     return p;
 }
 
+// Ranges of a sequence from which a row is joined by eight waves rather than one.
+#ifndef X_JOIN
+#define X_JOIN 16
+#endif
 template <int D, int NR>
-void launch_paged(const PagedAttnParams& p, int64_t wgs, bool uniform, hipStream_t st) {
-    hipLaunchKernelGGL((uniform ? paged_attn_kernel<D, NR, true> : paged_attn_kernel<D, NR, false>), dim3((unsigned)wgs),
-                       dim3(kPagedThreads), 0, st, p);
-    if (!p.single)
-        hipLaunchKernelGGL((paged_join_kernel<D, NR>), dim3((unsigned)((int64_t)p.B * p.T * p.Hq)), dim3(kPagedThreads), 0, st, p);
+void launch_paged(const PagedAttnParams& p, int64_t wgs, int64_t slots, bool uniform, hipStream_t st) {
+    // two tiles in flight where the registers hold them
+    constexpr int DEPTH = D == 64 || NR == 1 ? 2 : 1, DEPTH_LANES = D == 64 ? 2 : 1;
+    const bool once = X_NT && p.tiles == 1;
+    auto kernel = uniform ? (once ? paged_attn_kernel<D, NR, true, DEPTH, true> : paged_attn_kernel<D, NR, true, DEPTH, false>)
+                          : (once ? paged_attn_kernel<D, NR, false, DEPTH_LANES, true> : paged_attn_kernel<D, NR, false, DEPTH_LANES, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kPagedThreads), 0, st, p);
+    if (p.single) return;
+    const int64_t rows = (int64_t)p.B * p.T * p.Hq;
+    if (slots >= X_JOIN * (int64_t)p.B)
+        hipLaunchKernelGGL((paged_join_kernel<D, NR, 512>), dim3((unsigned)rows), dim3(512), 0, st, p);
+    else
+        hipLaunchKernelGGL((paged_join_kernel<D, NR, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
 }
 
 // ------------------------------------------------------------------ adjusted logits
@@ -1029,16 +1045,17 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
     p.single = plan.workspace == 0 || workspace == nullptr;
     p.causal = causal != 0;
     p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)shape->D)) * 1.4426950408889634f;
-    const int64_t wgs = (p.single ? (int64_t)p.B : plan.slots) * ((int64_t)shape->Hkv * plan.tiles);
+    const int64_t slots = p.single ? p.B : plan.slots;
+    const int64_t wgs = (slots * shape->Hkv + 7) / 8 * 8 * plan.tiles;
     if (wgs > INT_MAX || (int64_t)p.B * p.T * p.Hq > INT_MAX) return TRAJ_E_SHAPE;
     p.part_o = static_cast<float*>(workspace);
     p.part_ml = p.part_o + (p.single ? 0 : (size_t)plan.slots * p.units * 16 * plan.frags * shape->D);
-    const bool uniform = shape->page_size % 16 == 0;
+    const bool uniform = shape->page_size % 16 == 0 && shape->token_stride >= shape->D;
     hipStream_t s = as_stream(stream);
     if (shape->D == 128)
-        plan.frags == 1 ? launch_paged<128, 1>(p, wgs, uniform, s) : launch_paged<128, 2>(p, wgs, uniform, s);
+        plan.frags == 1 ? launch_paged<128, 1>(p, wgs, slots, uniform, s) : launch_paged<128, 2>(p, wgs, slots, uniform, s);
     else
-        plan.frags == 1 ? launch_paged<64, 1>(p, wgs, uniform, s) : launch_paged<64, 2>(p, wgs, uniform, s);
+        plan.frags == 1 ? launch_paged<64, 1>(p, wgs, slots, uniform, s) : launch_paged<64, 2>(p, wgs, slots, uniform, s);
     return launched();
 }
 

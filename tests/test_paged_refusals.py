@@ -44,7 +44,7 @@ def test_paged_shapes():
         assert append(shape(**bad)) == SHAPE, bad
         assert attn(shape(**bad)) == SHAPE, bad
         assert _lib.load().traj_paged_attn_workspace_size(ctypes.byref(shape(**bad))) == 0
-    for bad in (dict(D=96), dict(token_stride=(1 << 26) + 8)):
+    for bad in (dict(D=96), dict(token_stride=(1 << 25) + 8)):
         assert append(shape(**bad)) == UNSUPPORTED and attn(shape(**bad)) == UNSUPPORTED
     for none in (dict(B=0), dict(T=0)):
         assert append(shape(**none), k=None) == 0 and attn(shape(**none), q=None) == 0
