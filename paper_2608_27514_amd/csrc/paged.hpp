@@ -9,6 +9,7 @@
 
 #include <type_traits>
 
+#include "conf_topk.hpp"
 #include "layer.hpp"
 #include "verify_attn16.hpp"
 
@@ -125,35 +126,32 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(AppendPara
 }
 
 // ------------------------------------------------------------------ attention
-// Work: a workgroup takes `16 NR` query rows of one (sequence, kv head) (row = new token * group + head in
-// group) and a range of the sequence's keys; its 4 waves take 32-key tiles of the range in turn, each with its own
-// running softmax state, merged through LDS at the end.  The call reads every cached key and value once and does
-// T Hq / Hkv multiply-adds per element read, so up to some hundreds of rows the stream of K and V bounds it:
-// rows are padded to 16 for the matrix core, which idles either way.
-//   S^T = K Q^T with K fragments loaded straight from the pages into the A operand (no wave shares another's
-//   keys); V goes through the wave's own LDS tile for the transposing reads of O^T += V^T P^T (layouts of
-//   the 16-row verification kernel).  DEPTH tiles are held in registers: a tile's K registers are requested anew
-//   behind its score MFMAs and its V registers behind the LDS writes; page numbers are requested a tile earlier.
+// Every cached key and value is read once and takes T Hq / Hkv multiply-adds per element, so up to some hundreds of
+// rows (row = new token * group + head in group of one kv head) the stream of K and V bounds the call: rows are padded
+// to 16 for the matrix core, which idles either way, and what counts is how the loads are issued.
+//   * Whole 128-byte lines per load: a wave takes 4 (D = 128) or 8 rows of K or V per instruction, not the 16 rows of
+//     32 values that the K operand wants; both pass through LDS, which also does V's transposition
+//     (65536 keys, 8 heads, non-temporal: 66.8 -> 59.8 us).
+//   * Page numbers come by scalar loads and are requested a tile before they are needed.  Loaded like the keys they
+//     drained the wave's whole queue once per tile.
+//   * Two tiles in flight per wave where the registers hold them; buffers for 16 visible rows each give uniform
+//     bases and zeros behind the last key.
+//   S^T = K Q^T, weights in the lane that has the scores, O^T += V^T P^T: layouts of the 16-row verification kernel.
 //
-// Splits: the device computes from the lengths how many keys a workgroup takes (`chunk`), so that the batch makes
-// about kPagedTargetWgs workgroups whatever the lengths are; slot = index of a (sequence, range) pair in order.
+// Splits: the device computes from the lengths how many keys a workgroup takes (`chunk`).  A slot is a (sequence, range)
+// pair in order; the partial results of a sequence in several ranges are joined by a second kernel.
+//   MI355X: 32 sequences of up to 8192 keys x 32 heads of 128 (2.2 GB) 359 us = 6.2 TB/s, one of 2^20 keys x 8 heads
+//   6.7 TB/s, one of 65536 47.5 us = 5.6 TB/s (the read-only logit pass streams 6.2 TB/s).
 constexpr int kPagedWaves = 4;
 constexpr int kPagedThreads = kPagedWaves * 64;
 constexpr int kPagedTile = 32;
 constexpr int kPagedGranule = kPagedWaves * kPagedTile;
-#ifndef X_TARGET
-#define X_TARGET 2048
-#endif
-#ifndef X_FILL
-#define X_FILL 512
-#endif
-#ifndef X_CHUNK
-#define X_CHUNK 512
-#endif
-#ifndef X_NT
-#define X_NT 1
-#endif
-constexpr int kPagedFillWgs = X_FILL, kPagedMostWgs = X_TARGET, kPagedChunk = X_CHUNK;
+// Chunks make about kPagedFillWgs workgroups at least (one per CU), then stay at kPagedChunk keys, under which filling and
+// joining costs more than the shorter chain saves (65536 keys x 8 heads: 512 keys 49.0 us, 1024 47.5), and grow once there are
+// kPagedMostWgs of them: finer ones balance lengths and CUs better (32 sequences of up to 8192 keys: 4224 keys
+// 377 us, 2112 keys 359).
+constexpr int kPagedFillWgs = 256, kPagedChunk = 1024, kPagedMostWgs = 2048;
+// Caches up to this many keys are never split: a join takes longer (192 keys: 4.2 us whole, 7.7 split).
 constexpr int kPagedWhole = 256;
 
 struct PagedAttnParams {
@@ -162,8 +160,10 @@ struct PagedAttnParams {
     const int32_t* lens;
     uint16_t* out;
     float *part_o, *part_ml;  // partial results per (slot, unit, row): D values; maximum and sum
+    int2* ranges;             // [B] number of ranges, first slot
     int B, T, Hq, Hkv, group, rows;  // rows = T * group
-    int tiles, units;                // row tiles; units = Hkv * tiles
+    FastDiv by_group;
+    int tile_rows, tiles, units;     // rows per tile; tiles; units = Hkv * tiles
     int single, causal;              // single: no sequence can be split
     float scale_log2;
 };
@@ -183,41 +183,51 @@ __device__ __forceinline__ int paged_length(const PagedAttnParams& P, int b, boo
 
 // Keys per workgroup.  Every wave computes the same from the same lengths (whole numbers, quotients by powers of two).
 __device__ __forceinline__ int paged_chunk(int64_t total, int units, int capacity) {
-    const double work = (double)total * (double)units / kPagedGranule;  // of all workgroups together
+    const double work = (double)total * (double)units / kPagedGranule;
     double per = fmax(work / kPagedMostWgs, fmin(work / kPagedFillWgs, (double)(kPagedChunk / kPagedGranule)));
     per = fmin(per, (double)(capacity / kPagedGranule + 1));
     const int granules = (int)ceil(per);
     return kPagedGranule * (granules < 1 ? 1 : granules);
 }
 
-// The range that `slot` stands for (by == false), or the ranges of sequence `slot` (by == true); false where
-// the batch has fewer.  All lanes of the wave take part.
-__device__ __forceinline__ bool paged_range(const PagedAttnParams& P, int slot, bool by, bool report, PagedRange& r) {
+// Inclusive prefix sums over the wave's lanes, on the lane-exchange network: shifts by 1, 2, 4 and 8 within each row of
+// 16 lanes, then the last lane of rows 0 and 2 into the row behind, then the last of the lower half into the upper.
+__device__ __forceinline__ int wave_prefix(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+
+// The range that `slot` stands for; false where the batch has fewer.  All lanes of the wave take part.
+__device__ __forceinline__ bool paged_range(const PagedAttnParams& P, int slot, bool report, PagedRange& r) {
     const int lane = threadIdx.x & 63;
     if (P.single) {
         if (slot >= P.B) return false;
         r = PagedRange{slot, 0, 1, slot, paged_length(P, slot, report), P.cache.capacity};
         return true;
     }
-    int64_t total = 0;
-    for (int i = lane; i < P.B; i += 64) total += paged_length(P, i, report);
+    const int len0 = lane < P.B ? paged_length(P, lane, report) : 0;
+    uint64_t total = len0;
+    for (int i = lane + 64; i < P.B; i += 64) total += paged_length(P, i, report);
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
-    const int chunk = __builtin_amdgcn_readfirstlane(paged_chunk(total, P.units, P.cache.capacity));
+    for (int t = 0; t < 6; ++t) {
+        uint64_t x, y;
+        lane_pair64(t, total, x, y);
+        total = x + y;
+    }
+    const int chunk = __builtin_amdgcn_readfirstlane(paged_chunk((int64_t)total, P.units, P.cache.capacity));
     int base = 0;
     for (int i0 = 0; i0 < P.B; i0 += 64) {
         const int i = i0 + lane;
-        const int len = i < P.B ? paged_length(P, i, false) : 0;
+        const int len = i0 == 0 ? len0 : i < P.B ? paged_length(P, i, false) : 0;
         int n = (int)(((uint32_t)len + (uint32_t)chunk - 1u) / (uint32_t)chunk);
         n = i < P.B ? (n < 1 ? 1 : n) : 0;  // an empty sequence still has rows to write
-        int incl = n;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int o = __shfl_up(incl, off);
-            if (lane >= off) incl += o;
-        }
-        const int lo = base + incl - n;
-        const uint64_t hit = by ? ballot64(i == slot && i < P.B) : ballot64(slot >= lo && slot < lo + n);
+        const int incl = wave_prefix(n), lo = base + incl - n;
+        const uint64_t hit = ballot64(slot >= lo && slot < lo + n);
         if (hit != 0ull) {
             const int src = __builtin_ctzll(hit);
             r.b = i0 + src;
@@ -233,31 +243,31 @@ __device__ __forceinline__ bool paged_range(const PagedAttnParams& P, int slot, 
     return false;
 }
 
-// Where a tile's 32 keys lie.  UNIFORM (page_size % 16 == 0): each 16-key block within one page, so its page
-// comes by a scalar load and its base is uniform; otherwise lane l holds the page and the offset of key l % 32.
+// Where a tile of 16 BLK keys lies.  UNIFORM (page_size % 16 == 0): each 16-key block within one page, so its page
+// comes by a scalar load and its base is uniform; otherwise lane l holds the page and the offset of key l % (16 BLK).
 // vis: visible keys (inside the range, on a good page).
-template <bool UNIFORM>
+template <bool UNIFORM, int BLK>
 struct PagedTile {
-    int64_t at[UNIFORM ? 2 : 1];
+    int64_t at[UNIFORM ? BLK : 1];
     uint32_t vis;
 };
-template <bool UNIFORM>
+template <bool UNIFORM, int BLK>
 struct PagedPages {
-    int page[UNIFORM ? 2 : 1];
+    int page[UNIFORM ? BLK : 1];
 };
 typedef const __attribute__((address_space(4))) int32_t const_i32_t;  // read by scalar loads where uniform
 
 // Page numbers of the tile at key0: only requested here, looked at a tile later.  Keys at or behind `end`
 // take the place of `first`, which lies before it.
-template <bool UNIFORM>
-__device__ __forceinline__ PagedPages<UNIFORM> paged_pages(const PagedCache& C, const int32_t* row, int key0, int first, int end) {
-    PagedPages<UNIFORM> p;
+template <bool UNIFORM, int BLK>
+__device__ __forceinline__ PagedPages<UNIFORM, BLK> paged_pages(const PagedCache& C, const int32_t* row, int key0, int first, int end) {
+    PagedPages<UNIFORM, BLK> p;
     if constexpr (UNIFORM) {
         const_i32_t* table = (const_i32_t*)(uintptr_t)row;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) p.page[j] = table[C.by_page.div(key0 + 16 * j < end ? key0 + 16 * j : first)];
+        for (int j = 0; j < BLK; ++j) p.page[j] = table[C.by_page.div(key0 + 16 * j < end ? key0 + 16 * j : first)];
     } else {
-        const int key = key0 + (threadIdx.x & 31);
+        const int key = key0 + (threadIdx.x & (16 * BLK - 1));
         p.page[0] = row[C.by_page.div(key < end ? key : first)];
     }
     return p;
@@ -268,171 +278,123 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
     return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-template <bool UNIFORM>
-__device__ __forceinline__ PagedTile<UNIFORM> paged_tile(const PagedCache& C, const PagedPages<UNIFORM>& p, int64_t head, int key0,
-                                                         int first, int end, bool& bad) {
-    PagedTile<UNIFORM> t;
+template <bool UNIFORM, int BLK>
+__device__ __forceinline__ PagedTile<UNIFORM, BLK> paged_tile(const PagedCache& C, const PagedPages<UNIFORM, BLK>& p, int64_t head, int key0,
+                                                              int first, int end, bool& bad) {
+    PagedTile<UNIFORM, BLK> t;
     t.vis = 0;
 #pragma unroll
-    for (int j = 0; j < (UNIFORM ? 2 : 1); ++j) {
-        const int key = UNIFORM ? key0 + 16 * j : key0 + (int)(threadIdx.x & 31);
+    for (int j = 0; j < (UNIFORM ? BLK : 1); ++j) {
+        const int key = UNIFORM ? key0 + 16 * j : key0 + (int)(threadIdx.x & (16 * BLK - 1));
         const int at = key < end ? key : first;
         const bool good = p.page[j] >= 0 && p.page[j] < C.num_pages;
         bad |= !good && key < end;
+        t.at[j] = (good ? p.page[j] : 0) * C.page_stride + (at - C.by_page.div(at) * C.page_size) * C.token_stride + head;
         if constexpr (UNIFORM) {
             const int n = key < end && good ? (end - key < 16 ? end - key : 16) : 0;
             t.vis |= ((1u << n) - 1u) << (16 * j);
+            t.at[j] = uniform64(t.at[j]);
         } else {
-            t.vis = (uint32_t)ballot64(good && key < end);
+            t.vis = (uint32_t)ballot64(good && key < end) & (BLK == 2 ? 0xffffffffu : 0xffffu);
         }
-        t.at[j] = (good ? p.page[j] : 0) * C.page_stride + (at - C.by_page.div(at) * C.page_size) * C.token_stride + head;
-        if (UNIFORM) t.at[j] = uniform64(t.at[j]);
     }
     return t;
 }
 
-template <int D, int NR>
-struct PagedGeom {
-    static constexpr int kRows = 16 * NR;
-    static constexpr int kRowF = D + 4;  // floats per row of the merge buffers: rows start 4 banks apart
-    static constexpr int kKRow = D + 8;   // elements per row of a K tile: the 16 rows of a fragment read start 4 banks apart
-    static constexpr int kVRow = D + 16;  // elements per row of a V tile: the 8 rows that half a wave reads of a transposing
-                                          // load start 8 banks apart (72 and 40 words a row) and each takes 8 of the 64
-    static constexpr int kTileBytes = kPagedTile * kVRow * 2;
-    static constexpr int kMergeBytes = kRows * kRowF * 4;
-    static constexpr int kWaveBytes = kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes;
+// A tile's rows of K or V, whole 128-byte lines per wave-wide load (512 / D rows).  UNIFORM: a buffer of each block's
+// visible rows with 32-bit lane offsets, so that rows behind its end read as 0.  ONCE: nothing reads them again.
+template <int D, bool UNIFORM, int BLK, bool ONCE>
+__device__ __forceinline__ void paged_load(u32x4_t (&x)[BLK * D / 32], const uint16_t* pool, const PagedTile<UNIFORM, BLK>& t, int token_stride) {
+    constexpr int RPI = 512 / D;
+    const int lane = threadIdx.x & 63, vrow = lane / (D / 8), vchunk = lane % (D / 8);
+#pragma unroll
+    for (int i = 0; i < BLK * D / 32; ++i) {
+        if constexpr (UNIFORM) {
+            const int j = i * RPI / 16, rows = __popc(t.vis >> (16 * j) & 0xffffu);
+            const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)(pool + t.at[j]), (short)0, rows * 2 * token_stride, kBufferFlags);
+            x[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, 2 * (((i * RPI) % 16 + vrow) * token_stride + 8 * vchunk), 0, ONCE ? 2 : 0);
+        } else {
+            const u32x4_t* p = reinterpret_cast<const u32x4_t*>(pool + __shfl(t.at[0], i * RPI + vrow) + 8 * vchunk);
+            x[i] = ONCE ? __builtin_nontemporal_load(p) : *p;
+        }
+    }
+}
+
+// LDS rows: elements per row of a K tile (the 16 rows of a fragment read start 4 banks apart), of a V tile (the 8 rows
+// that half a wave reads of a transposing load start 8 banks apart, 72 and 40 words a row, and each takes 8 of the
+// 64), and floats per row of the merge buffers.
+template <int D>
+struct PagedLds {
+    static constexpr int kKRow = D + 8, kVRow = D + 16, kMergeRow = D + 4;
 };
 
-template <int D, int NR, bool UNIFORM, int DEPTH, bool ONCE>
-__global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnParams P) {
-    using G = PagedGeom<D, NR>;
-    constexpr int KS = D / 32;       // k steps of the scores
-    constexpr int NDB = D / 16;      // head-dim blocks of the output
-    constexpr int RPI = 512 / D;     // V rows per wave-wide 16-byte load
-    constexpr int NVL = kPagedTile / RPI;
-    __shared__ __align__(16) char lds[kPagedWaves * G::kWaveBytes];
-    __shared__ float sh_m[kPagedWaves][G::kRows], sh_l[kPagedWaves][G::kRows];
-
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int q4 = lane >> 4, l16 = lane & 15;
-    // Workgroup i runs on XCD i % 8.  The row tiles of one (slot, kv head) follow each other on one XCD, whose L2
-    // they share; the (slot, kv head) pairs go round the XCDs in order, so that slots without work, the last ones,
-    // leave none of them idle.
-    const int turn = blockIdx.x / 8 / P.tiles, row_tile = blockIdx.x / 8 - turn * P.tiles;
-    const int pair = turn * 8 + blockIdx.x % 8, slot = pair / P.Hkv, g = pair - slot * P.Hkv;
-    const int unit = g * P.tiles + row_tile, tile_row = row_tile * G::kRows;
-    PagedRange r;
-    if (!paged_range(P, slot, false, blockIdx.x == 0, r)) return;
-    const int b = r.b, len = r.len;
-    const int begin = r.split * r.chunk, end = len - begin > r.chunk ? begin + r.chunk : len;
-
-    // query fragments: row tile_row + 16 f + l16, head dims 32 ks + 8 q4 ..
-    bf16x8_t qf[NR][KS];
-    int limit[NR];  // keys that the row sees
-#pragma unroll
-    for (int f = 0; f < NR; ++f) {
-        const int row = min(tile_row + 16 * f + l16, P.rows - 1);  // rows past the last repeat it and are not stored
-        const int t = row / P.group, h = g * P.group + row - t * P.group;
-        limit[f] = P.causal ? len - P.T + t + 1 : len;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-            qf[f][ks] = __builtin_bit_cast(bf16x8_t, ldg16(P.q + (((int64_t)b * P.T + t) * P.Hq + h) * D + 32 * ks + 8 * q4));
-    }
-    const int min_limit = P.causal ? len - P.T + 1 : len;
-
-    f32x4_t o[NR][NDB];
+// A wave's query rows: 16 NR of them, row 16 f + lane % 16 in fragment f.
+template <int D, int NR>
+struct PagedRows {
+    bf16x8_t qf[NR][D / 32];     // head dims 32 ks + 8 (lane / 16) ..
+    int limit[NR];               // keys that the row sees
+    f32x4_t o[NR][D / 16];       // O^T: head dims 16 db + 4 (lane / 16) ..
     float m[NR], thr[NR], neg_mc[NR], lsum[NR];
+
+    __device__ __forceinline__ void init(const PagedAttnParams& P, int b, int g, int len, int row0) {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int f = 0; f < NR; ++f) {
-        m[f] = kNegInf;
-        thr[f] = kNegInf;
-        neg_mc[f] = 0.f;
-        lsum[f] = 0.f;
+        for (int f = 0; f < NR; ++f) {
+            const int row = min(row0 + 16 * f + (lane & 15), P.rows - 1);  // rows past the last repeat it and are not stored
+            const int t = P.by_group.div(row), h = g * P.group + row - t * P.group;
+            limit[f] = P.causal ? len - P.T + t + 1 : len;
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) o[f][db] = f32x4_t{};
+            for (int ks = 0; ks < D / 32; ++ks)
+                qf[f][ks] = __builtin_bit_cast(bf16x8_t, ldg16(P.q + (((int64_t)b * P.T + t) * P.Hq + h) * D + 32 * ks + 8 * (lane >> 4)));
+            m[f] = kNegInf;
+            thr[f] = kNegInf;
+            neg_mc[f] = 0.f;
+            lsum[f] = 0.f;
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db) o[f][db] = f32x4_t{};
+        }
     }
 
-    uint16_t* vt = reinterpret_cast<uint16_t*>(lds + wave * G::kWaveBytes);
-    const uint16_t* kread = vt + l16 * G::kKRow + 8 * q4;
-    const uint16_t* vread = vt + (4 * q4 + (l16 >> 2)) * G::kVRow + 4 * (l16 & 3);
-    const int vrow = lane / (D / 8), vchunk = lane % (D / 8);  // of a V load
-    uint16_t* kwrite = vt + vrow * G::kKRow + 8 * vchunk;
-    uint16_t* vwrite = vt + vrow * G::kVRow + 8 * vchunk;
-
-    const PagedCache& C = P.cache;
-    const int32_t* row = C.table + b * C.table_stride;
-    const int64_t head = g * C.head_stride;
-    const float c = P.scale_log2, lazy = kLazyLog2 / c;
-    const int first = begin + wave * kPagedTile;
-    u32x4_t kr[DEPTH][NVL], vr[DEPTH][NVL];
-    uint32_t vis[DEPTH];
-    bool bad = false;
-
-    int voff[16 / RPI];
-#pragma unroll
-    for (int i = 0; i < 16 / RPI; ++i) voff[i] = 2 * ((i * RPI + vrow) * (int)C.token_stride + 8 * vchunk);
-    // A tile's rows of K or V, whole 128-byte lines per load.  UNIFORM: a buffer of each block's visible rows with
-    // 32-bit lane offsets, so that rows behind its end read as 0.
-    auto load = [&](u32x4_t (&x)[NVL], const uint16_t* pool, const PagedTile<UNIFORM>& t) {
-#pragma unroll
-        for (int i = 0; i < NVL; ++i) {
-            if constexpr (UNIFORM) {
-                const int j = i * RPI / 16, rows = __popc(t.vis >> (16 * j) & 0xffffu);
-                const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)(pool + t.at[j]), (short)0, rows * 2 * (int)C.token_stride, kBufferFlags);
-                x[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, voff[i % (16 / RPI)], 0, ONCE ? 2 : 0);
-            } else {
-                const u32x4_t* p = reinterpret_cast<const u32x4_t*>(pool + __shfl(t.at[0], i * RPI + vrow) + 8 * vchunk);
-                x[i] = ONCE ? __builtin_nontemporal_load(p) : *p;
-            }
-        }
-    };
-    PagedPages<UNIFORM> pages;  // of the tile after those in flight
-    // The tile at key0, held in ring slot u; with `more` also the loads of the tile DEPTH rounds behind it.
-    auto step = [&](auto slot, int key0, bool more) {
-        constexpr int u = decltype(slot)::value;
-#pragma unroll
-        for (int i = 0; i < NVL; ++i) *reinterpret_cast<u32x4_t*>(kwrite + i * RPI * G::kKRow) = kr[u][i];
-        f32x4_t s[NR][2];
+    // S^T = K Q^T of the 32 NK keys whose LDS rows start at k
+    template <int NK>
+    __device__ __forceinline__ void scores(const uint16_t* k, f32x4_t (&s)[NR][2 * NK]) const {
+        const int lane = threadIdx.x & 63;
+        const uint16_t* kread = k + (lane & 15) * PagedLds<D>::kKRow + 8 * (lane >> 4);
 #pragma unroll
         for (int f = 0; f < NR; ++f)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) s[f][j] = f32x4_t{};
+            for (int j = 0; j < 2 * NK; ++j) s[f][j] = f32x4_t{};
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < D / 32; ++ks)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const bf16x8_t kf = lds16(kread + 16 * j * G::kKRow + 32 * ks);
+            for (int j = 0; j < 2 * NK; ++j) {
+                const bf16x8_t kf = lds16(kread + 16 * j * PagedLds<D>::kKRow + 32 * ks);
 #pragma unroll
                 for (int f = 0; f < NR; ++f) s[f][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[f][ks], s[f][j], 0, 0, 0);
             }
-        PagedTile<UNIFORM> next;
-        if (more) {
-            next = paged_tile<UNIFORM>(C, pages, head, key0 + DEPTH * kPagedGranule, first, end, bad);
-            pages = paged_pages<UNIFORM>(C, row, key0 + (DEPTH + 1) * kPagedGranule, first, end);
-            load(kr[u], C.k, next);
-        }
-        if (vis[u] != 0xffffffffu || key0 + kPagedTile > min_limit) {  // rare: a sequence's last tile
+    }
+
+    // scores of keys key0 .. that are not in vis or behind the row's last key
+    template <int NK>
+    __device__ __forceinline__ void mask(f32x4_t (&s)[NR][2 * NK], uint64_t vis, int key0) const {
 #pragma unroll
-            for (int f = 0; f < NR; ++f)
+        for (int f = 0; f < NR; ++f)
 #pragma unroll
-                for (int v = 0; v < 8; ++v) {
-                    const int k = 16 * (v >> 2) + 4 * q4 + (v & 3);
-                    const bool seen = ((vis[u] >> k) & 1u) != 0u && key0 + k < limit[f];
-                    s[f][v >> 2][v & 3] = seen ? s[f][v >> 2][v & 3] : kNegInf;
-                }
-            // V rows that are not visible may hold anything and count as 0 (a block's buffer ends before them)
-            if constexpr (!UNIFORM) {
-#pragma unroll
-                for (int i = 0; i < NVL; ++i)
-                    if (((vis[u] >> (i * RPI + vrow)) & 1u) == 0u) vr[u][i] = u32x4_t{};
+            for (int v = 0; v < 8 * NK; ++v) {
+                const int k = 16 * (v >> 2) + 4 * ((threadIdx.x & 63) >> 4) + (v & 3);
+                const bool seen = ((vis >> k) & 1ull) != 0ull && key0 + k < limit[f];
+                s[f][v >> 2][v & 3] = seen ? s[f][v >> 2][v & 3] : kNegInf;
             }
-        }
-        bf16x8_t pf[NR];
+    }
+
+    // weights of the keys against the running reference, in the operand order of values()
+    template <int NK>
+    __device__ __forceinline__ void weights(const f32x4_t (&s)[NR][2 * NK], float c, float lazy, bf16x8_t (&pf)[NR][NK]) {
 #pragma unroll
         for (int f = 0; f < NR; ++f) {
             float mx = s[f][0][0];
 #pragma unroll
-            for (int v = 1; v < 8; ++v) mx = __builtin_elementwise_maximum(mx, s[f][v >> 2][v & 3]);
+            for (int v = 1; v < 8 * NK; ++v) mx = __builtin_elementwise_maximum(mx, s[f][v >> 2][v & 3]);
             mx = quad_max(mx);
             const bool up = mx > thr[f];
             if (ballot64(up) != 0ull) {  // the reference follows the maximum in steps of at least 2^8
@@ -440,50 +402,201 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnP
                 const float alpha = up ? fast_exp2((m[f] - m_new) * c) : 1.0f;  // 0 at the first reference
                 lsum[f] *= alpha;
 #pragma unroll
-                for (int db = 0; db < NDB; ++db) o[f][db] *= alpha;
+                for (int db = 0; db < D / 16; ++db) o[f][db] *= alpha;
                 m[f] = m_new;
                 thr[f] = m_new + lazy;
                 neg_mc[f] = m_new == kNegInf ? 0.f : -m_new * c;
             }
 #pragma unroll
-            for (int v = 0; v < 8; ++v) {
+            for (int v = 0; v < 8 * NK; ++v) {
                 const float p = fast_exp2(__builtin_fmaf(s[f][v >> 2][v & 3], c, neg_mc[f]));
                 lsum[f] += p;
-                pf[f][v] = (__bf16)p;
+                pf[f][v / 8][v % 8] = (__bf16)p;
             }
         }
+    }
+
+    // O^T += V^T P^T over the 32 NK keys whose LDS rows start at v
+    template <int NK>
+    __device__ __forceinline__ void values(const uint16_t* v, const bf16x8_t (&pf)[NR][NK]) {
+        const int lane = threadIdx.x & 63;
+        const uint16_t* vread = v + (4 * (lane >> 4) + ((lane & 15) >> 2)) * PagedLds<D>::kVRow + 4 * (lane & 3);
 #pragma unroll
-        for (int i = 0; i < NVL; ++i) {
-            *reinterpret_cast<u32x4_t*>(vwrite + i * RPI * G::kVRow) = vr[u][i];
+        for (int i = 0; i < NK; ++i)
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db) {
+                const bf16x4_t a0 = lds_read_tr(vread + 16 * db + 32 * i * PagedLds<D>::kVRow);
+                const bf16x4_t a1 = lds_read_tr(vread + 16 * db + (32 * i + 16) * PagedLds<D>::kVRow);
+                const bf16x8_t va = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                for (int f = 0; f < NR; ++f) o[f][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[f][i], o[f][db], 0, 0, 0);
+            }
+    }
+
+    // this wave's state into its rows of a merge buffer
+    __device__ __forceinline__ void leave(float* buf, float* sm, float* sl) const {
+        const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
+#pragma unroll
+        for (int f = 0; f < NR; ++f) {
+            const float l = quad_sum(lsum[f]);
+            if (q4 == 0) {
+                sm[16 * f + l16] = m[f];
+                sl[16 * f + l16] = l;
+            }
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db)
+                *reinterpret_cast<f32x4_t*>(buf + (16 * f + l16) * PagedLds<D>::kMergeRow + 16 * db + 4 * q4) = o[f][db];
         }
+    }
+};
+
+// Workgroup i runs on XCD i % 8.  The row tiles of one (slot, kv head) follow each other on one XCD, whose L2
+// they share; the (slot, kv head) pairs go round the XCDs in order, so that slots without work, the last ones,
+// leave none of them idle.
+struct PagedPlace {
+    int slot, g, unit, row_tile;
+};
+__device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams& P) {
+    PagedPlace w;
+    const int turn = blockIdx.x / 8 / P.tiles, pair = turn * 8 + blockIdx.x % 8;
+    w.row_tile = blockIdx.x / 8 - turn * P.tiles;
+    w.slot = pair / P.Hkv;
+    w.g = pair - w.slot * P.Hkv;
+    w.unit = w.g * P.tiles + w.row_tile;
+    return w;
+}
+
+// Joins the SETS states of each of a workgroup's ROWS rows and writes the result, or its part of a sequence in several
+// ranges.
+template <int D, int ROWS, int SETS>
+__device__ __forceinline__ void paged_store(const PagedAttnParams& P, const PagedRange& r, const PagedPlace& w, const float* buf,
+                                            const float* sm, const float* sl) {
+    constexpr int kRow = PagedLds<D>::kMergeRow, LPR = D / 4, STEP = kPagedThreads / LPR;
+    const int d = 4 * (threadIdx.x % LPR), first = threadIdx.x / LPR;
+    if (!P.single && w.unit == 0 && r.split == 0 && threadIdx.x == 0) P.ranges[r.b] = make_int2(r.n, r.slot0);
+#pragma unroll
+    for (int i = 0; i < ROWS / STEP; ++i) {
+        const int rr = first + i * STEP, qrow = w.row_tile * ROWS + rr;
+        float M = kNegInf;
+#pragma unroll
+        for (int e = 0; e < SETS; ++e) M = fmaxf(M, sm[e * ROWS + rr]);
+        const float Ms = M == kNegInf ? 0.f : M;
+        f32x4_t acc = {};
+        float l = 0.f;
+#pragma unroll
+        for (int e = 0; e < SETS; ++e) {
+            const float scale = SETS == 1 ? 1.0f : fast_exp2((sm[e * ROWS + rr] - Ms) * P.scale_log2);  // 0 for a state without keys
+            l += scale * sl[e * ROWS + rr];
+            acc += scale * *reinterpret_cast<const f32x4_t*>(buf + (e * ROWS + rr) * kRow + d);
+        }
+        if (r.n == 1) {
+            const float inv = l > 0.f ? 1.0f / l : 0.f;  // a row that sees nothing: 0
+            const int t = P.by_group.div(qrow), h = w.g * P.group + qrow - t * P.group;
+            u32x2_t x;
+            x[0] = (uint32_t)f2bf(acc[0] * inv) | ((uint32_t)f2bf(acc[1] * inv) << 16);
+            x[1] = (uint32_t)f2bf(acc[2] * inv) | ((uint32_t)f2bf(acc[3] * inv) << 16);
+            if (qrow < P.rows) *reinterpret_cast<u32x2_t*>(P.out + (((int64_t)r.b * P.T + t) * P.Hq + h) * D + d) = x;
+        } else if (qrow < P.rows) {
+            const int64_t at = ((int64_t)w.slot * P.units + w.unit) * ROWS + rr;
+            *reinterpret_cast<f32x4_t*>(P.part_o + at * D + d) = acc;
+            if (d == 0) *reinterpret_cast<float2*>(P.part_ml + 2 * at) = make_float2(M, l);
+        }
+    }
+}
+
+// Up to 32 rows: the waves take the range's 32-key tiles in turn.
+template <int D, int NR, bool UNIFORM, int DEPTH>
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnParams P) {
+    using L = PagedLds<D>;
+    constexpr int ROWS = 16 * NR, NVL = D / 16, RPI = 512 / D;
+    constexpr int kTileBytes = kPagedTile * L::kVRow * 2, kMergeBytes = ROWS * L::kMergeRow * 4;
+    constexpr int kTiles = kPagedWaves * kTileBytes, kMerge = kPagedWaves * kMergeBytes;
+    __shared__ __align__(16) char lds[kTiles > kMerge ? kTiles : kMerge];
+    __shared__ float sh_m[kPagedWaves * ROWS], sh_l[kPagedWaves * ROWS];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const PagedPlace w = paged_place(P);
+    PagedRange r;
+    if (!paged_range(P, w.slot, blockIdx.x == 0, r)) return;
+    const int len = r.len;
+    const int begin = r.split * r.chunk, end = len - begin > r.chunk ? begin + r.chunk : len;
+    const int min_limit = P.causal ? len - P.T + 1 : len;
+
+    // one LDS tile per wave, K's and then V's
+    uint16_t* tile = reinterpret_cast<uint16_t*>(lds + wave * kTileBytes);
+    const int vrow = lane / (D / 8), vchunk = lane % (D / 8);  // of a load
+    uint16_t* kwrite = tile + vrow * L::kKRow + 8 * vchunk;
+    uint16_t* vwrite = tile + vrow * L::kVRow + 8 * vchunk;
+
+    const PagedCache& C = P.cache;
+    const int ts = (int)C.token_stride;
+    const int32_t* row = C.table + r.b * C.table_stride;
+    const int64_t head = w.g * C.head_stride;
+    const float c = P.scale_log2, lazy = kLazyLog2 / c;
+    const int first = begin + wave * kPagedTile;
+    u32x4_t kr[DEPTH][NVL], vr[DEPTH][NVL];
+    uint32_t vis[DEPTH];
+    bool bad = false;
+    using Tile = PagedTile<UNIFORM, 2>;
+    using Pages = PagedPages<UNIFORM, 2>;
+    PagedRows<D, NR> st;
+    Pages pages;  // of the tile after those in flight
+    // The tile at key0, held in ring slot u; with `more` also the loads of the tile DEPTH rounds behind it.
+    auto step = [&](auto slot, int key0, bool more) {
+        constexpr int u = decltype(slot)::value;
+#pragma unroll
+        for (int i = 0; i < NVL; ++i) *reinterpret_cast<u32x4_t*>(kwrite + i * RPI * L::kKRow) = kr[u][i];
+        f32x4_t s[NR][2];
+        st.template scores<1>(tile, s);
+        if (!UNIFORM) __builtin_amdgcn_sched_barrier(0);  // lane addresses only while they are needed
+        Tile next;
         if (more) {
-            load(vr[u], C.v, next);
+            next = paged_tile<UNIFORM, 2>(C, pages, head, key0 + DEPTH * kPagedGranule, first, end, bad);
+            pages = paged_pages<UNIFORM, 2>(C, row, key0 + (DEPTH + 1) * kPagedGranule, first, end);
+            paged_load<D, UNIFORM, 2, true>(kr[u], C.k, next, ts);
+        }
+        if (!UNIFORM) __builtin_amdgcn_sched_barrier(0);
+        if (vis[u] != 0xffffffffu || key0 + kPagedTile > min_limit) {  // rare: a sequence's last tile
+            st.template mask<1>(s, vis[u], key0);
+            // V rows that are not visible may hold anything and count as 0 (a block's buffer ends before them)
+            if constexpr (!UNIFORM) {
+#pragma unroll
+                for (int i = 0; i < NVL; ++i)
+                    if (((vis[u] >> (i * RPI + vrow)) & 1u) == 0u) vr[u][i] = u32x4_t{};
+            }
+        }
+        bf16x8_t pf[NR][1];
+        st.template weights<1>(s, c, lazy, pf);
+#pragma unroll
+        for (int i = 0; i < NVL; ++i) *reinterpret_cast<u32x4_t*>(vwrite + i * RPI * L::kVRow) = vr[u][i];
+        if (!UNIFORM) __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            paged_load<D, UNIFORM, 2, true>(vr[u], C.v, next, ts);
             vis[u] = next.vis;
         }
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) {
-            const bf16x4_t a0 = lds_read_tr(vread + 16 * db);
-            const bf16x4_t a1 = lds_read_tr(vread + 16 * db + 16 * G::kVRow);
-            const bf16x8_t va = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-            for (int f = 0; f < NR; ++f) o[f][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[f], o[f][db], 0, 0, 0);
-        }
+        if (!UNIFORM) __builtin_amdgcn_sched_barrier(0);
+        st.template values<1>(tile, pf);
     };
 
+    auto fetch = [&](int u) { return paged_pages<UNIFORM, 2>(C, row, first + u * kPagedGranule, first, end); };
+    Pages p0{}, p1{};
+    if (first < end) {
+        p0 = fetch(0);
+        p1 = fetch(DEPTH - 1);
+        pages = fetch(DEPTH);
+    }
+    st.init(P, r.b, w.g, len, w.row_tile * ROWS);
     int left = first < end ? (end - first + kPagedGranule - 1) / kPagedGranule : 0;  // tiles of this wave
     if (left > 0) {
         using Slot0 = std::integral_constant<int, 0>;
         using Slot1 = std::integral_constant<int, DEPTH - 1>;
-        auto fetch = [&](int u) { return paged_pages<UNIFORM>(C, row, first + u * kPagedGranule, first, end); };
-        auto request = [&](auto slot, const PagedPages<UNIFORM>& p) {
+        auto request = [&](auto slot, const Pages& p) {
             constexpr int u = decltype(slot)::value;
-            const PagedTile<UNIFORM> t = paged_tile<UNIFORM>(C, p, head, first + u * kPagedGranule, first, end, bad);
+            const Tile t = paged_tile<UNIFORM, 2>(C, p, head, first + u * kPagedGranule, first, end, bad);
             vis[u] = t.vis;
-            load(kr[u], C.k, t);
-            load(vr[u], C.v, t);
+            paged_load<D, UNIFORM, 2, true>(kr[u], C.k, t, ts);
+            paged_load<D, UNIFORM, 2, true>(vr[u], C.v, t, ts);
         };
-        const PagedPages<UNIFORM> p0 = fetch(0), p1 = fetch(DEPTH - 1);
-        pages = fetch(DEPTH);
         int key0 = first;
         // No load under a condition ahead of the loop: the compiler's waits count the loads that every path issued.
         if constexpr (DEPTH == 1) {
@@ -512,58 +625,114 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnP
         if (ballot64(bad) != 0ull && lane == 0) flag_device_status(kDevBadPage);
     }
 
-    // waves -> workgroup
     __syncthreads();
-    float* mine = reinterpret_cast<float*>(lds + wave * G::kWaveBytes);
-#pragma unroll
-    for (int f = 0; f < NR; ++f) {
-        const float l = quad_sum(lsum[f]);
-        if (q4 == 0) {
-            sh_m[wave][16 * f + l16] = m[f];
-            sh_l[wave][16 * f + l16] = l;
-        }
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4_t*>(mine + (16 * f + l16) * G::kRowF + 16 * db + 4 * q4) = o[f][db];
-    }
+    float* buf = reinterpret_cast<float*>(lds);
+    st.leave(buf + wave * ROWS * L::kMergeRow, sh_m + wave * ROWS, sh_l + wave * ROWS);
     __syncthreads();
-    for (int i = threadIdx.x; i < G::kRows * (D / 4); i += kPagedThreads) {
-        const int rr = i / (D / 4), d = 4 * (i % (D / 4));
-        const int qrow = tile_row + rr;
-        if (qrow >= P.rows) continue;
-        float M = kNegInf;
+    paged_store<D, ROWS, kPagedWaves>(P, r, w, buf, sh_m, sh_l);
+}
+
+// More rows: RW waves of 32 rows each share the stages of 16 RW keys that they load into LDS together (a stage's K and
+// V would otherwise pass from the L2 once per 32 rows); 4 / RW such groups of waves take the range's stages in turn.
+// While a stage is multiplied the next one lies in registers on its way to the other buffer.
+template <int D, int RW, bool UNIFORM, bool ONCE>
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedAttnParams P) {
+    using L = PagedLds<D>;
+    constexpr int NR = 2, KW = kPagedWaves / RW, ROWS = 32 * RW, STAGE = 16 * RW, NK = STAGE / 32, NVL = D / 32, RPI = 512 / D;
+    constexpr int kStage = STAGE * (L::kKRow + L::kVRow);  // elements
+    constexpr int kStages = KW * 2 * kStage * 2, kMerge = KW * ROWS * L::kMergeRow * 4;
+    __shared__ __align__(16) char lds[kStages > kMerge ? kStages : kMerge];
+    __shared__ float sh_m[KW * ROWS], sh_l[KW * ROWS];
+    __shared__ uint32_t sh_vis[KW][2][RW];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kg = wave / RW, rw = wave % RW;
+    const PagedPlace w = paged_place(P);
+    PagedRange r;
+    if (!paged_range(P, w.slot, blockIdx.x == 0, r)) return;
+    const int len = r.len;
+    const int begin = r.split * r.chunk, end = len - begin > r.chunk ? begin + r.chunk : len;
+    const int min_limit = P.causal ? len - P.T + 1 : len;
+
+    uint16_t* stage = reinterpret_cast<uint16_t*>(lds) + kg * 2 * kStage;  // two of them, K rows then V rows
+    const int vrow = lane / (D / 8), vchunk = lane % (D / 8);
+    const PagedCache& C = P.cache;
+    const int ts = (int)C.token_stride;
+    const int32_t* row = C.table + r.b * C.table_stride;
+    const int64_t head = w.g * C.head_stride;
+    const float c = P.scale_log2, lazy = kLazyLog2 / c;
+    u32x4_t kr[NVL], vr[NVL];  // this wave's 16 keys of the next stage
+    uint32_t vis = 0;
+    bool bad = false;
+    const int rounds = (end - begin + KW * STAGE - 1) / (KW * STAGE);
+    auto stage_key = [&](int n) { return begin + (n * KW + kg) * STAGE; };
+    PagedPages<UNIFORM, 1> pages;
+    auto fetch = [&](int n) { pages = paged_pages<UNIFORM, 1>(C, row, stage_key(n) + 16 * rw, begin, end); };
+    auto request = [&](int n) {
+        const PagedTile<UNIFORM, 1> t = paged_tile<UNIFORM, 1>(C, pages, head, stage_key(n) + 16 * rw, begin, end, bad);
+        fetch(n + 1);
+        paged_load<D, UNIFORM, 1, ONCE>(kr, C.k, t, ts);
+        paged_load<D, UNIFORM, 1, ONCE>(vr, C.v, t, ts);
+        vis = t.vis;
+    };
+    auto put = [&](int n) {
+        uint16_t* k = stage + (n & 1) * kStage;
+        uint16_t* kwrite = k + (16 * rw + vrow) * L::kKRow + 8 * vchunk;
+        uint16_t* vwrite = k + STAGE * L::kKRow + (16 * rw + vrow) * L::kVRow + 8 * vchunk;
 #pragma unroll
-        for (int w = 0; w < kPagedWaves; ++w) M = fmaxf(M, sh_m[w][rr]);
-        const float Ms = M == kNegInf ? 0.f : M;
-        f32x4_t acc = {};
-        float l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kPagedWaves; ++w) {
-            const float e = fast_exp2((sh_m[w][rr] - Ms) * c);  // 0 for a wave without keys
-            l += e * sh_l[w][rr];
-            acc += e * *reinterpret_cast<const f32x4_t*>(lds + w * G::kWaveBytes + (rr * G::kRowF + d) * 4);
+        for (int i = 0; i < NVL; ++i) {
+            *reinterpret_cast<u32x4_t*>(kwrite + i * RPI * L::kKRow) = kr[i];
+            u32x4_t x = vr[i];
+            // rows that are not visible may hold anything and count as 0 (a block's buffer ends before them)
+            if (!UNIFORM) x = ((vis >> (i * RPI + vrow)) & 1u) != 0u ? x : u32x4_t{};
+            *reinterpret_cast<u32x4_t*>(vwrite + i * RPI * L::kVRow) = x;
         }
-        if (r.n == 1) {
-            const float inv = l > 0.f ? 1.0f / l : 0.f;  // a row that sees nothing: 0
-            const int t = qrow / P.group, h = g * P.group + qrow - t * P.group;
-            u32x2_t w2;
-            w2[0] = (uint32_t)f2bf(acc[0] * inv) | ((uint32_t)f2bf(acc[1] * inv) << 16);
-            w2[1] = (uint32_t)f2bf(acc[2] * inv) | ((uint32_t)f2bf(acc[3] * inv) << 16);
-            *reinterpret_cast<u32x2_t*>(P.out + (((int64_t)b * P.T + t) * P.Hq + h) * D + d) = w2;
-        } else {
-            const int64_t at = ((int64_t)slot * P.units + unit) * G::kRows + rr;
-            *reinterpret_cast<f32x4_t*>(P.part_o + at * D + d) = acc;
-            if (d == 0) {
-                P.part_ml[2 * at] = M;
-                P.part_ml[2 * at + 1] = l;
+        if (lane == 0) sh_vis[kg][n & 1][rw] = vis;
+    };
+    PagedRows<D, NR> st;
+    if (rounds > 0) fetch(0);
+    st.init(P, r.b, w.g, len, w.row_tile * ROWS + 32 * rw);
+    if (rounds > 0) {
+        request(0);
+        put(0);
+        request(1);  // past the end: the range's first row, not visible
+        __syncthreads();
+        for (int n = 0; n < rounds; ++n) {
+            if (n + 1 < rounds) {
+                put(n + 1);
+                request(n + 2);
             }
+            const uint16_t* k = stage + (n & 1) * kStage;
+            uint32_t seen[NK];
+#pragma unroll
+            for (int i = 0; i < NK; ++i)
+                seen[i] = __builtin_amdgcn_readfirstlane(sh_vis[kg][n & 1][2 * i] | sh_vis[kg][n & 1][2 * i + 1] << 16);
+            const uint64_t all = NK == 1 ? seen[0] : seen[0] | (uint64_t)seen[NK - 1] << 32;
+            if (all != 0ull) {
+                f32x4_t s[NR][2 * NK];
+                st.template scores<NK>(k, s);
+                const int key0 = stage_key(n);
+                if (all != (NK == 1 ? 0xffffffffull : ~0ull) || key0 + STAGE > min_limit) st.template mask<NK>(s, all, key0);
+                bf16x8_t pf[NR][NK];
+                st.template weights<NK>(s, c, lazy, pf);
+                st.template values<NK>(k + STAGE * L::kKRow, pf);
+            }
+            __syncthreads();
         }
+        if (ballot64(bad) != 0ull && lane == 0) flag_device_status(kDevBadPage);
     }
+
+    float* buf = reinterpret_cast<float*>(lds);
+    const int set = kg * ROWS + 32 * rw;
+    st.leave(buf + set * L::kMergeRow, sh_m + set, sh_l + set);
+    __syncthreads();
+    paged_store<D, ROWS, KW>(P, r, w, buf, sh_m, sh_l);
 }
 
 // THREADS threads per (sequence, new token, query head): each range by D / 4 lanes, THREADS * 4 / D ranges at a time,
 // every group with its own running maximum, joined through LDS in the groups' order.  Sequences in one range were
 // written by the attention itself.
-template <int D, int NR, int THREADS>
+template <int D, int THREADS>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void paged_join_kernel(PagedAttnParams P) {
     constexpr int LPR = D / 4, GR = THREADS / LPR, ROWS = THREADS < 256 ? 256 / THREADS : 1, U = 4;
     static_assert(THREADS >= 64, "a row's lanes of a wave have one sequence");
@@ -575,13 +744,12 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void paged_join_kern
     const int h = (int)(orow % P.Hq);
     const int64_t bt = orow / P.Hq;
     const int b = (int)(bt / P.T), t = (int)(bt - (int64_t)b * P.T);
-    PagedRange r{};
-    paged_range(P, b, true, false, r);
+    const int2 r = P.ranges[b];
     const int g = h / P.group, qrow = t * P.group + h - g * P.group;
-    const int unit = g * P.tiles + qrow / (16 * NR), rr = qrow % (16 * NR);
-    const int64_t at0 = ((int64_t)r.slot0 * P.units + unit) * (16 * NR) + rr, step = (int64_t)P.units * (16 * NR);
+    const int unit = g * P.tiles + qrow / P.tile_rows, rr = qrow % P.tile_rows;
+    const int64_t at0 = ((int64_t)r.y * P.units + unit) * P.tile_rows + rr, step = (int64_t)P.units * P.tile_rows;
     const int grp = tid / LPR, d = tid % LPR;
-    const int n = r.n > 1 ? r.n : 0;
+    const int n = r.x > 1 ? r.x : 0;
     f32x4_t acc = {};
     float m = kNegInf, l = 0.f;
     for (int s0 = grp; s0 < n; s0 += U * GR) {

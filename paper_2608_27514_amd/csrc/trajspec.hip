@@ -583,10 +583,10 @@ PagedCache paged_cache(const traj_paged_shape* sh, const void* k, const void* v,
     return c;
 }
 
-// Row tiles of one or two 16-row fragments, and the slots that the device's split can come to: chunks of the batch's
-// keys over the target, and a last, short one per sequence.
+// Rows per tile (16, 32, 64 or 128, the last two shared by several waves), and the slots that the device's split can
+// come to.
 struct PagedPlan {
-    int frags, tiles, units;
+    int tile_rows, tiles, units;
     int64_t slots;
     size_t workspace;  // 0: no sequence can be split
 };
@@ -594,8 +594,8 @@ struct PagedPlan {
 PagedPlan plan_paged(const traj_paged_shape* sh) {
     PagedPlan p{};
     const int rows = sh->T * (sh->Hq / sh->Hkv);
-    p.frags = rows <= 16 ? 1 : 2;
-    p.tiles = (rows + 16 * p.frags - 1) / (16 * p.frags);
+    p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
     const int64_t units = (int64_t)sh->Hkv * p.tiles;
     p.units = units > INT_MAX ? INT_MAX : (int)units;
     const int64_t cap = (int64_t)sh->max_pages * sh->page_size;
@@ -604,28 +604,35 @@ PagedPlan plan_paged(const traj_paged_shape* sh) {
     const auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
     const int64_t most = std::max(up(kPagedFillWgs, units), std::min(up(kPagedMostWgs, units), sh->B * up(cap, kPagedChunk)));
     p.slots = std::min<int64_t>(most + sh->B, sh->B * up(cap, kPagedGranule));
-    p.workspace = cap <= kPagedWhole ? 0 : (size_t)p.slots * (size_t)units * 16 * p.frags * (sh->D + 2) * sizeof(float);
+    p.workspace = cap <= kPagedWhole ? 0 : (size_t)p.slots * (size_t)units * p.tile_rows * (sh->D + 2) * sizeof(float) + (size_t)sh->B * sizeof(int2);
     return p;
 }
 
-// Ranges of a sequence from which a row is joined by eight waves rather than one.
-#ifndef X_JOIN
-#define X_JOIN 16
-#endif
-template <int D, int NR>
-void launch_paged(const PagedAttnParams& p, int64_t wgs, int64_t slots, bool uniform, hipStream_t st) {
+// Few rows of many ranges are joined by eight waves each rather than one (32 rows of 128 ranges: 8.6 -> 4.7 us); with
+// many rows that only makes more workgroups (3584 rows: 37.5 us the call with one wave each, 42.6 with eight).
+constexpr int64_t kPagedWideJoin = 16, kPagedWideJoinRows = 512;
+
+template <int D, bool UNIFORM>
+void launch_paged_attn(const PagedAttnParams& p, int64_t wgs, hipStream_t st) {
     // two tiles in flight where the registers hold them
-    constexpr int DEPTH = D == 64 || NR == 1 ? 2 : 1, DEPTH_LANES = D == 64 ? 2 : 1;
-    const bool once = X_NT && p.tiles == 1;
-    auto kernel = uniform ? (once ? paged_attn_kernel<D, NR, true, DEPTH, true> : paged_attn_kernel<D, NR, true, DEPTH, false>)
-                          : (once ? paged_attn_kernel<D, NR, false, DEPTH_LANES, true> : paged_attn_kernel<D, NR, false, DEPTH_LANES, false>);
+    constexpr int DEPTH1 = D == 64 || UNIFORM ? 2 : 1, DEPTH2 = D == 64 ? 2 : 1;
+    auto kernel = p.tile_rows == 16   ? paged_attn_kernel<D, 1, UNIFORM, DEPTH1>
+                  : p.tile_rows == 32 ? paged_attn_kernel<D, 2, UNIFORM, DEPTH2>
+                  : p.tile_rows == 64 ? paged_rows_kernel<D, 2, UNIFORM, true>
+                  : p.tiles == 1      ? paged_rows_kernel<D, 4, UNIFORM, true>
+                                      : paged_rows_kernel<D, 4, UNIFORM, false>;  // tiles share the keys
     hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kPagedThreads), 0, st, p);
+}
+
+template <int D>
+void launch_paged(const PagedAttnParams& p, int64_t wgs, int64_t slots, bool uniform, hipStream_t st) {
+    uniform ? launch_paged_attn<D, true>(p, wgs, st) : launch_paged_attn<D, false>(p, wgs, st);
     if (p.single) return;
     const int64_t rows = (int64_t)p.B * p.T * p.Hq;
-    if (slots >= X_JOIN * (int64_t)p.B)
-        hipLaunchKernelGGL((paged_join_kernel<D, NR, 512>), dim3((unsigned)rows), dim3(512), 0, st, p);
+    if (slots >= kPagedWideJoin * p.B && rows <= kPagedWideJoinRows)
+        hipLaunchKernelGGL((paged_join_kernel<D, 512>), dim3((unsigned)rows), dim3(512), 0, st, p);
     else
-        hipLaunchKernelGGL((paged_join_kernel<D, NR, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
+        hipLaunchKernelGGL((paged_join_kernel<D, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
 }
 
 // ------------------------------------------------------------------ adjusted logits
@@ -1040,6 +1047,8 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
     p.Hkv = shape->Hkv;
     p.group = shape->Hq / shape->Hkv;
     p.rows = p.T * p.group;
+    p.by_group = fast_div(p.group);
+    p.tile_rows = plan.tile_rows;
     p.tiles = plan.tiles;
     p.units = plan.units;
     p.single = plan.workspace == 0 || workspace == nullptr;
@@ -1049,13 +1058,11 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
     const int64_t wgs = (slots * shape->Hkv + 7) / 8 * 8 * plan.tiles;
     if (wgs > INT_MAX || (int64_t)p.B * p.T * p.Hq > INT_MAX) return TRAJ_E_SHAPE;
     p.part_o = static_cast<float*>(workspace);
-    p.part_ml = p.part_o + (p.single ? 0 : (size_t)plan.slots * p.units * 16 * plan.frags * shape->D);
+    p.part_ml = p.part_o + (p.single ? 0 : (size_t)plan.slots * p.units * p.tile_rows * shape->D);
+    p.ranges = reinterpret_cast<int2*>(p.part_ml + (p.single ? 0 : (size_t)plan.slots * p.units * p.tile_rows * 2));
     const bool uniform = shape->page_size % 16 == 0 && shape->token_stride >= shape->D;
     hipStream_t s = as_stream(stream);
-    if (shape->D == 128)
-        plan.frags == 1 ? launch_paged<128, 1>(p, wgs, slots, uniform, s) : launch_paged<128, 2>(p, wgs, slots, uniform, s);
-    else
-        plan.frags == 1 ? launch_paged<64, 1>(p, wgs, slots, uniform, s) : launch_paged<64, 2>(p, wgs, slots, uniform, s);
+    shape->D == 128 ? launch_paged<128>(p, wgs, slots, uniform, s) : launch_paged<64>(p, wgs, slots, uniform, s);
     return launched();
 }
 

@@ -1,6 +1,7 @@
 """What the paged-cache and adjusted-logits calls refuse, before anything reaches the device (CPU only)."""
 
 import ctypes
+import math
 import os
 
 import pytest
@@ -81,16 +82,19 @@ def test_a_workspace_covers_every_split_of_the_lengths():
     for B, T, Hq, Hkv, columns in ((1, 1, 8, 8, 4000), (7, 1, 4, 1, 300), (300, 2, 2, 2, 50), (3, 64, 4, 1, 1000), (1, 1, 1, 1, 9)):
         sh = shape(B=B, T=T, Hq=Hq, Hkv=Hkv, max_pages=columns, table_stride=columns)
         rows = T * Hq // Hkv
-        frags = 1 if rows <= 16 else 2
-        per_slot = Hkv * -(-rows // (16 * frags)) * 16 * frags * (128 + 2) * 4
-        slots, rest = divmod(sizes(ctypes.byref(sh)), per_slot)
-        assert rest == 0
+        tile = next(n for n in (16, 32, 64, 128) if rows <= n or n == 128)
+        units = Hkv * -(-rows // tile)
         cap = columns * 16
-        target, least = 1024, 128
-        units = Hkv * -(-rows // (16 * frags))
-        for lens in ([cap] * B, [cap] + [0] * (B - 1), [1] * B, [least + 1] * B, [(i * 7919) % cap for i in range(B)]):
-            chunk = least * max(1, -(-sum(lens) * units // (target * least)))
-            assert sum(max(1, -(-n // chunk)) for n in lens) <= max(slots, B)
+        size = sizes(ctypes.byref(sh))
+        if cap <= 256:  # never split
+            assert size == 0
+            continue
+        slots, rest = divmod(size - 8 * B, units * tile * (128 + 2) * 4)
+        assert rest == 0
+        for lens in ([cap] * B, [cap] + [0] * (B - 1), [1] * B, [129] * B, [(i * 7919) % cap for i in range(B)], [cap // 2] * (B // 2 + 1)):
+            work = sum(lens) * units / 128
+            chunk = 128 * max(1, math.ceil(max(work / 2048, min(work / 256, 8))))
+            assert sum(max(1, -(-n // chunk)) for n in lens) <= max(slots, B), (B, T, lens[:3])
 
 
 def adjust(sh=None, k=3, logits=FAKE, conf=FAKE, idx=FAKE, ws=None, ws_bytes=0, **kw):
