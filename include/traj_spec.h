@@ -493,7 +493,7 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
  * -inf), mask [n_masks, mask_stride] uint32, mask_index [rows] int32 (NULL: m = r; -1: every token is allowed;
  * any other value outside [0, n_masks): none is, TRAJ_DEV_BAD_MASK); n_seq = ceil(rows / rows_per_seq).
  * history_size == 0 / bias_size == 0 / mask == NULL leave that part out.
- * Limits: those of traj_confidence_topk; vocab <= 2^20 (else TRAJ_E_UNSUPPORTED); rows_per_seq >= 1;
+ * Limits: those of traj_confidence_topk; vocab <= 2^19 (else TRAJ_E_UNSUPPORTED); rows_per_seq >= 1;
  *   history_size, bias_size >= 0, their sum < 2^30; mask_stride >= ceil(vocab / 32); without mask_index
  *   n_masks >= rows.
  * workspace: traj_confidence_topk_adjusted_workspace_size() bytes, 16-byte aligned; one sized for more rows

@@ -18,10 +18,10 @@ namespace trajspec {
 constexpr int kDevBadMask = 0x40;    // TRAJ_DEV_BAD_MASK
 constexpr int kDevBadHistory = 0x80; // TRAJ_DEV_BAD_HISTORY
 
-constexpr int kAdjustMaxVocab = 1 << 20;  // one bit per token in LDS: 128 KB
+constexpr int kAdjustMaxVocab = 1 << 19;  // a bit per token and two bytes per 32 of them in LDS: 96 KB
 constexpr int kAdjustPrepThreads = 1024;
 constexpr int kAdjustGroup = 512;         // tokens per popcount prefix
-constexpr int kAdjustWindow = 2048;       // records counted at a time
+constexpr int kAdjustLds = 144 << 10;      // of adjust_prepare_kernel
 constexpr uint32_t kAdjustSeen = 0x80000000u;
 constexpr uint32_t kFloorFinite = 0x00800000u;  // order_bits of the lowest finite value: -inf is no candidate
 
@@ -44,9 +44,9 @@ struct AdjustParams {
     int n_masks;
     // what adjust_prepare_kernel leaves (null: no special tokens)
     uint32_t* special;           // [n_seq, words]
-    AdjustRecord* records;       // [n_seq, max_records]
-    int32_t* n_records;          // [n_seq]
-    int V, words;
+    AdjustRecord* records;       // [n_seq, max_records], in the order of their ids
+    int32_t* before;             // [n_seq, groups + 1]: records before each group of kAdjustGroup tokens
+    int V, words, groups, window;  // window: records counted at a time
 };
 
 // bias - (f c + p), each operation rounded by itself.
@@ -58,16 +58,20 @@ __device__ __forceinline__ float adjust_add(float bias, float f, float p, int c)
 
 // One workgroup per sequence.  LDS: the bitmap (words), a prefix of popcounts per group of 512 tokens, and a window
 // of counts and biases.  A record's place is its token's rank among the set bits, so no order of atomics shows.
+// A chain of LDS latencies between barriers (a sequence of 500 ids 5.2 us, 64 of 2048 ids 7.8).
 __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(AdjustParams P) {
     extern __shared__ uint32_t prep_lds[];
     __shared__ int sh_wave[kAdjustPrepThreads / 64];
-    __shared__ int sh_dup;
     constexpr int WPG = kAdjustGroup / 32;
-    const int words = P.words, groups = (words + WPG - 1) / WPG;
+    const int words = P.words, groups = P.groups;
     uint32_t* bits = prep_lds;
-    int* prefix = reinterpret_cast<int*>(prep_lds + groups * WPG);
-    int* count = prefix + groups;
-    float* bias_sum = reinterpret_cast<float*>(count + kAdjustWindow);
+    uint16_t* inside = reinterpret_cast<uint16_t*>(prep_lds + groups * WPG);             // set bits of the group before the word
+    int* prefix = reinterpret_cast<int*>(prep_lds + groups * WPG + groups * (WPG / 2));  // and before the group
+    int* count = prefix + groups;                       // times seen
+    int* summed = count + P.window;                     // the last entry of the bias list that is in the sum, -1: none
+    int* turn = summed + P.window;                      // the entry that is next
+    float* bias_sum = reinterpret_cast<float*>(turn + P.window);
+    __shared__ int sh_more;
     const int seq = blockIdx.x, tid = threadIdx.x;
     const int32_t* history = P.history + (int64_t)seq * P.H;
     const int32_t* ids = P.bias_ids + (int64_t)seq * P.NB;
@@ -80,101 +84,138 @@ __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(Adju
             hl = hl < 0 ? 0 : P.H;
         }
     }
+    // the first entries are requested before anything waits
+    const int h0 = tid < P.H ? history[tid] : -1, b0 = tid < P.NB ? ids[tid] : -1;
+    const float y0 = tid < P.NB ? bias[tid] : 0.f;
+    const float f = P.frequency != nullptr ? P.frequency[seq] : 0.f;
+    const float p = P.presence != nullptr ? P.presence[seq] : 0.f;
+    auto seen_at = [&](int i) { return i < kAdjustPrepThreads ? h0 : history[i]; };
+    auto named_at = [&](int j) { return j < kAdjustPrepThreads ? b0 : ids[j]; };
     auto in_vocab = [&](int id) { return id >= 0 && id < P.V; };
 
-    for (int w = tid; w < groups * WPG; w += kAdjustPrepThreads) bits[w] = 0u;
-    if (tid == 0) sh_dup = 0;
-    __syncthreads();
-    for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
-        const int id = ids[j];
-        if (in_vocab(id) && ((atomicOr(&bits[id >> 5], 1u << (id & 31)) >> (id & 31)) & 1u)) sh_dup = 1;
-    }
+    for (int w = tid; w < groups * (WPG / 4); w += kAdjustPrepThreads) reinterpret_cast<u32x4_t*>(bits)[w] = u32x4_t{};
+    auto clear_window = [&] {
+        for (int i = tid; i < P.window; i += kAdjustPrepThreads) {
+            count[i] = 0;
+            summed[i] = -1;
+            turn[i] = INT32_MAX;
+            bias_sum[i] = 0.f;
+        }
+    };
+    clear_window();
     __syncthreads();
     for (int i = tid; i < hl; i += kAdjustPrepThreads) {
-        const int id = history[i];
+        const int id = seen_at(i);
+        if (in_vocab(id)) atomicOr(&bits[id >> 5], 1u << (id & 31));
+    }
+    for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
+        const int id = named_at(j);
         if (in_vocab(id)) atomicOr(&bits[id >> 5], 1u << (id & 31));
     }
     __syncthreads();
-    // exclusive prefix of the groups' popcounts: two consecutive groups per thread (2048 groups at most)
-    static_assert(kAdjustMaxVocab / kAdjustGroup <= 2 * kAdjustPrepThreads, "two groups per thread");
-    int own[2] = {0, 0};
+    // prefixes of the words' popcounts: a group per thread
+    static_assert(kAdjustMaxVocab / kAdjustGroup <= kAdjustPrepThreads, "a group per thread");
+    int own = 0;
+    if (tid < groups) {
+        const u32x4_t* x = reinterpret_cast<const u32x4_t*>(bits + tid * WPG);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int gidx = 2 * tid + e;
-        if (gidx < groups)
-            for (int w = 0; w < WPG; ++w) own[e] += __popc(bits[gidx * WPG + w]);
+        for (int i = 0; i < WPG / 4; ++i) {
+            const u32x4_t v = x[i];
+            u32x2_t two;
+            two[0] = (uint32_t)own;
+            own += __popc(v[0]);
+            two[0] |= (uint32_t)own << 16;
+            own += __popc(v[1]);
+            two[1] = (uint32_t)own;
+            own += __popc(v[2]);
+            two[1] |= (uint32_t)own << 16;
+            own += __popc(v[3]);
+            reinterpret_cast<u32x2_t*>(inside + tid * WPG)[i] = two;
+        }
     }
-    int incl = own[0] + own[1];
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int o = __shfl_up(incl, off);
-        if ((tid & 63) >= off) incl += o;
-    }
+    const int incl = wave_prefix(own);
     if ((tid & 63) == 63) sh_wave[tid >> 6] = incl;
     __syncthreads();
-    int before = 0, total = 0;
+    int excl = incl - own, total = 0;
+#pragma unroll
     for (int w = 0; w < kAdjustPrepThreads / 64; ++w) {
-        if (w < (tid >> 6)) before += sh_wave[w];
+        excl += w < (tid >> 6) ? sh_wave[w] : 0;
         total += sh_wave[w];
     }
-    const int excl = before + incl - own[0] - own[1];
-    if (2 * tid < groups) prefix[2 * tid] = excl;
-    if (2 * tid + 1 < groups) prefix[2 * tid + 1] = excl + own[0];
+    int32_t* before = P.before + (int64_t)seq * (groups + 1);
+    if (tid < groups) {
+        prefix[tid] = excl;
+        before[tid] = excl;
+    }
+    if (tid == 0) before[groups] = total;
     uint32_t* special = P.special + (int64_t)seq * words;
     for (int w = tid; w < words; w += kAdjustPrepThreads) special[w] = bits[w];
-    if (tid == 0) P.n_records[seq] = total;
     __syncthreads();
 
-    auto rank = [&](int id) {
-        int r = prefix[id / kAdjustGroup];
-        const int w1 = id >> 5;
-        for (int w = id / kAdjustGroup * WPG; w < w1; ++w) r += __popc(bits[w]);
-        return r + __popc(bits[w1] & ((1u << (id & 31)) - 1u));
+    auto rank = [&](int id) -> int {
+        return prefix[id / kAdjustGroup] + (int)inside[id >> 5] + __popc(bits[id >> 5] & ((1u << (id & 31)) - 1u));
     };
-    const float f = P.frequency != nullptr ? P.frequency[seq] : 0.f;
-    const float p = P.presence != nullptr ? P.presence[seq] : 0.f;
     AdjustRecord* records = P.records + (int64_t)seq * P.max_records;
-    for (int w0 = 0; w0 < total; w0 += kAdjustWindow) {
-        for (int i = tid; i < kAdjustWindow; i += kAdjustPrepThreads) {
-            count[i] = 0;
-            bias_sum[i] = 0.f;
+    for (int w0 = 0; w0 < total; w0 += P.window) {
+        if (w0 > 0) {
+            __syncthreads();
+            clear_window();
+            __syncthreads();
         }
-        __syncthreads();
         for (int i = tid; i < hl; i += kAdjustPrepThreads) {
-            const int id = history[i];
+            const int id = seen_at(i);
             if (!in_vocab(id)) continue;
             const int r = rank(id) - w0;
-            if (r >= 0 && r < kAdjustWindow) atomicAdd(&count[r], 1);
+            if (r >= 0 && r < P.window) atomicAdd(&count[r], 1);
         }
-        for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
+        // Biases of one token add up in the order of the list: a round adds each token's first entry that is not in
+        // its sum (one round, unless a token is named twice).
+        const int id0 = named_at(tid);
+        const int r0 = tid < P.NB && in_vocab(id0) ? rank(id0) - w0 : -1;
+        auto rank_at = [&](int j) -> int {
+            if (j < kAdjustPrepThreads) return r0;
             const int id = ids[j];
-            if (!in_vocab(id)) continue;
-            const int r = rank(id) - w0;
-            if (r < 0 || r >= kAdjustWindow) continue;
-            float sum = bias[j];
-            bool owner = true;
-            if (sh_dup) {  // biases of one token add up in the order of the list
-                for (int i = 0; i < P.NB && owner; ++i) {
-                    if (ids[i] != id) continue;
-                    if (i < j) owner = false;
-                    if (i > j) sum += bias[i];
+            return in_vocab(id) ? rank(id) - w0 : -1;
+        };
+        for (bool more = P.NB > 0; more;) {
+            if (tid == 0) sh_more = 0;
+            for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
+                const int r = rank_at(j);
+                if (r >= 0 && r < P.window && j > summed[r]) atomicMin(&turn[r], j);
+            }
+            __syncthreads();
+            for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
+                const int r = rank_at(j);
+                if (r < 0 || r >= P.window) continue;
+                const int t = turn[r];
+                if (j > t) sh_more = 1;
+                if (j == t) {
+                    bias_sum[r] = summed[r] < 0 ? (j < kAdjustPrepThreads ? y0 : bias[j]) : bias_sum[r] + (j < kAdjustPrepThreads ? y0 : bias[j]);
                 }
             }
-            if (owner) bias_sum[r] = sum;
+            __syncthreads();
+            more = sh_more != 0;
+            for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
+                const int r = rank_at(j);
+                if (r >= 0 && r < P.window && turn[r] == j) {
+                    summed[r] = j;
+                    turn[r] = INT32_MAX;
+                }
+            }
+            __syncthreads();
         }
-        __syncthreads();
+        if (P.NB == 0) __syncthreads();
         for (int w = tid; w < words; w += kAdjustPrepThreads) {
             uint32_t x = bits[w];
             if (x == 0u) continue;
             int r = rank(w * 32) - w0;
             for (; x != 0u; x &= x - 1u, ++r) {
-                if (r < 0 || r >= kAdjustWindow) continue;
+                if (r < 0 || r >= P.window) continue;
                 const int c = count[r];
-                const float add = c > 0 ? adjust_add(bias_sum[r], f, p, c) : bias_sum[r];
-                records[w0 + r] = AdjustRecord{(uint32_t)(w * 32 + __builtin_ctz(x)) | (c > 0 ? kAdjustSeen : 0u), add};
+                const float y = bias_sum[r];
+                records[w0 + r] = AdjustRecord{(uint32_t)(w * 32 + __builtin_ctz(x)) | (c > 0 ? kAdjustSeen : 0u), c > 0 ? adjust_add(y, f, p, c) : y};
             }
         }
-        __syncthreads();
     }
 }
 
@@ -237,21 +278,34 @@ __device__ __forceinline__ void adjust_finish(const uint64_t (&key)[K], float m,
     }
 }
 
-// grid.x = rows * splits, slices and register ring as conf_topk_kernel.  LDS: the slice's allowed bits.
+// grid.x = rows * splits, slices and register ring as conf_topk_kernel.  LDS: the slice's allowed bits, and the list of
+// a slice with few allowed tokens.
+//   * Vectors without an allowed token are not read (their lanes load the slice's first vector), and a slice with at
+//     most kAdjustList allowed ones gathers just those (256 rows of 126464 under masks of 250 tokens: 22.5 -> 8.3 us).
+//   * The special tokens are gathered behind the stream, several per lane at a time.  Each costs a 64-byte sector of
+//     its row: 2048 rows of 126464 bf16 take 87 us with nothing to adjust (6.0 TB/s), 100 with a mask of 97%, 129 with
+//     1800 special tokens each besides (222 MB of sectors).  Gathered along the way, with the lines just streamed, they
+//     took as long: the registers cost a wave per SIMD, and the XCD's 4 MB L2 does not hold its 256 rows' windows.
+constexpr int kAdjustList = 512;
+
 template <typename T, int K, int THREADS, int U, int DEPTH>
 __global__ __launch_bounds__(THREADS) void adjust_topk_kernel(AdjustParams A, const T* __restrict__ logits, int64_t row_stride, int k,
                                                               int splits, int chunk, float* __restrict__ conf,
                                                               int32_t* __restrict__ idx, float* __restrict__ partial) {
     constexpr int NV = VecOf<T>::n;
     constexpr int SW = THREADS * U;
+    constexpr int NW = THREADS / 64;
+    static_assert(NW > 1 && NW <= 16, "the row reduction covers at most 16 waves");
     constexpr uint32_t kAll = (1u << NV) - 1u;
     extern __shared__ uint32_t allowed[];
+    __shared__ uint32_t sh_floor[NW];
+    __shared__ int sh_count[NW];
     const int row = blockIdx.x / splits;
     const int split = blockIdx.x - row * splits;
-    const int begin = split * chunk;  // a multiple of 32
+    const int begin = split * chunk;  // a multiple of kAdjustGroup
     const int end = min(A.V, begin + chunk);
     const T* base = logits + (int64_t)row * row_stride;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int seq = row / A.rows_per_seq;
 
     const uint32_t* mrow = nullptr;
@@ -265,72 +319,136 @@ __global__ __launch_bounds__(THREADS) void adjust_topk_kernel(AdjustParams A, co
             forbidden = true;
         }
     }
+    const bool masked = mrow != nullptr || forbidden;
+
+    const int lead = (int)((0u - (unsigned)(reinterpret_cast<uintptr_t>(base + begin) / sizeof(T))) % NV);
+    const int head = min(lead, end - begin);
+    const int vbegin = begin + head;
+    const int nvec = (end - vbegin) / NV;
+    const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(base + vbegin);
+    u32x4_t buf[DEPTH][U];
+    if (!masked && nvec > 0) {  // the first sweeps are on their way while the special tokens' bits arrive
+#pragma unroll
+        for (int d = 0; d + 1 < DEPTH; ++d)
+#pragma unroll
+            for (int u = 0; u < U; ++u) buf[d][u] = __builtin_nontemporal_load(vp + min(d * SW + u * THREADS + tid, nvec - 1));
+    }
+
+    // the slice's special tokens
+    const int32_t* before = A.before + (int64_t)seq * (A.groups + 1);
+    const AdjustRecord* rec = A.records + (int64_t)seq * A.max_records;
+    const bool specials = A.special != nullptr && !forbidden;
+    const int first_special = specials ? before[begin / kAdjustGroup] : 0;
+    const int last_special = specials ? before[(end + kAdjustGroup - 1) / kAdjustGroup] : 0;
+    const float r = A.repetition != nullptr ? A.repetition[seq] : 1.0f;
+    auto special_value = [&](const AdjustRecord& a, float l, uint32_t m) {
+        if (a.id & kAdjustSeen) l = l > 0.f ? l / r : l * r;
+        return ((m >> (a.id & 31)) & 1u) != 0u ? l + a.add : kNegInf;
+    };
+
     const int nw = (end - begin + 31) / 32;
+    int n_allowed = 0;
     for (int w = tid; w < nw; w += THREADS) {
         uint32_t x = forbidden ? 0u : 0xffffffffu;
         if (mrow != nullptr) x = mrow[begin / 32 + w];
         if (A.special != nullptr) x &= ~A.special[(int64_t)seq * A.words + begin / 32 + w];
+        if (w == nw - 1 && (end & 31) != 0) x &= (1u << (end & 31)) - 1u;  // only the row's last word is not whole
         allowed[w] = x;
+        n_allowed += __popc(x);
     }
+    const int before_lane = wave_prefix(n_allowed) - n_allowed;
+    if (lane == 63) sh_count[wave] = before_lane + n_allowed;
+    if (lane == 0) sh_floor[wave] = 0u;
     __syncthreads();
+    int list_at = before_lane, listed = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        list_at += w < wave ? sh_count[w] : 0;
+        listed += sh_count[w];
+    }
 
     TopkLane<K> st;
     st.init();
     uint32_t floor_bits = kFloorFinite;
     st.refresh(floor_bits);
 
-    const int lead = (int)((0u - (unsigned)(reinterpret_cast<uintptr_t>(base + begin) / sizeof(T))) % NV);
-    const int head = min(lead, end - begin);
-    const int vbegin = begin + head;
-    const int nvec = (end - vbegin) / NV;
-    // allowed bits of vector v
-    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(allowed);
-    auto vec_bits = [&](int v) -> uint32_t {
-        const int at = head + v * NV;
-        uint32_t x = bytes[at >> 3];
-        if (head != 0) x |= (uint32_t)bytes[(at >> 3) + 1] << 8;  // uniform; the LDS holds a word more
-        return (x >> (at & 7)) & kAll;
-    };
-    {
-        const int nsw = (nvec + SW - 1) / SW;
-        const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(base + vbegin);
-        // Vectors without an allowed value (and those past the slice) load its first vector instead: one cache line.
+    const bool few = listed <= kAdjustList;
+    int32_t* list = reinterpret_cast<int32_t*>(allowed + (chunk + 31) / 32 + 1);
+    if (few) {
+        for (int w = tid; w < nw; w += THREADS)
+            for (uint32_t x = allowed[w]; x != 0u; x &= x - 1u) list[list_at++] = begin + 32 * w + __builtin_ctz(x);
+        __syncthreads();
+        for (int i = tid; i < listed; i += THREADS) {
+            const int id = list[i];
+            const float x[1] = {load_scalar(base + id)};
+            adjust_absorb<K, 1>(x, x[0], id, st, floor_bits);
+        }
+    } else {
+        // The waves of a workgroup share their floors through LDS, as in conf_topk_kernel.
+        auto share_floor = [&](uint32_t fb) {
+            if (lane == 0) __hip_atomic_store(&sh_floor[wave], fb, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const uint32_t o = __hip_atomic_load(&sh_floor[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                fb = o > fb ? o : fb;
+            }
+            return fb;
+        };
+        // Allowed bits of this lane's vector in a sweep, 0 past the slice.  A vector's first bit has the same place in its
+        // byte in every sweep (THREADS * NV is a multiple of 8); bits behind a byte come from the next (the LDS holds a
+        // word more).
+        const uint8_t* bytes = reinterpret_cast<const uint8_t*>(allowed) + ((head + tid * NV) >> 3);
+        const int shift = (head + tid * NV) & 7;
+        const bool any_bits = masked || A.special != nullptr;
+        auto vec_bits = [&](int v) -> uint32_t {  // v: of lane 0
+            const int at = v + tid < nvec ? v * NV / 8 : 0;
+            uint32_t x = bytes[at];
+            if (head != 0) x |= (uint32_t)bytes[at + 1] << 8;  // uniform
+            return v + tid < nvec ? x >> shift & kAll : 0u;
+        };
         auto load = [&](int sweep, u32x4_t (&b)[U]) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int v = sweep * SW + u * THREADS + tid;
-                const bool some = v < nvec && vec_bits(v < nvec ? v : 0) != 0u;
-                b[u] = __builtin_nontemporal_load(vp + (some ? v : 0));
+                const int v0 = sweep * SW + u * THREADS, v = min(v0 + tid, nvec - 1);
+                b[u] = __builtin_nontemporal_load(vp + (!masked || vec_bits(v0) != 0u ? v : 0));
             }
         };
         auto absorb_sweep = [&](int sweep, const u32x4_t (&b)[U]) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int v = sweep * SW + u * THREADS + tid;
-                const uint32_t bits = v < nvec ? vec_bits(v) : 0u;
-                if (ballot64(bits != 0u) == 0ull) continue;
+                const int v0 = sweep * SW + u * THREADS;
+                const uint32_t ok = any_bits ? vec_bits(v0) : v0 + tid < nvec ? kAll : 0u;
+                if (ballot64(ok != 0u) == 0ull) continue;
                 float x[NV];
                 unpack(b[u], x);
-                if (ballot64(bits != kAll) != 0ull) {
+                if (ballot64(ok != kAll) != 0ull) {
 #pragma unroll
                     for (int j = 0; j < NV; ++j) {
-                        const int m = (int)(bits << (31 - j)) >> 31;
+                        const int m = (int)(ok << (31 - j)) >> 31;
                         const int xi = __builtin_bit_cast(int, x[j]);
                         x[j] = __builtin_bit_cast(float, (xi & m) | ((int)0xff800000 & ~m));
                     }
                 }
-                adjust_absorb<K, NV>(x, vec_max<NV>(x), vbegin + v * NV, st, floor_bits);
+                adjust_absorb<K, NV>(x, vec_max<NV>(x), vbegin + (v0 + tid) * NV, st, floor_bits);
             }
             if ((sweep & (sweep + 1)) == 0) {
                 const uint32_t own = wave_kth_floor<K>(st.lmax, k);
-                floor_bits = own > floor_bits ? own : floor_bits;
+                floor_bits = share_floor(own > floor_bits ? own : floor_bits);
                 st.refresh(floor_bits);
+            } else {
+                const uint32_t f = share_floor(floor_bits);
+                if (f != floor_bits) {  // wave-uniform
+                    floor_bits = f;
+                    st.refresh(floor_bits);
+                }
             }
         };
+        const int nsw = (nvec + SW - 1) / SW;
         if (nsw > 0) {
-            u32x4_t buf[DEPTH][U];
+            if (masked) {
 #pragma unroll
-            for (int d = 0; d + 1 < DEPTH; ++d) load(d, buf[d]);
+                for (int d = 0; d + 1 < DEPTH; ++d) load(d, buf[d]);
+            }
             for (int it = 0; it < nsw; it += DEPTH) {
 #pragma unroll
                 for (int j = 0; j < DEPTH; ++j) {
@@ -341,35 +459,34 @@ __global__ __launch_bounds__(THREADS) void adjust_topk_kernel(AdjustParams A, co
                 }
             }
         }
+        const int tail = vbegin + nvec * NV;  // values before and behind the vectors
+        for (int i = tid; i < head + (end - tail); i += THREADS) {
+            const int e = i < head ? begin + i : tail + (i - head);
+            const bool ok = ((allowed[(e - begin) >> 5] >> (e & 31)) & 1u) != 0u;
+            const float l = load_scalar(base + e);
+            const float x[1] = {ok ? l : kNegInf};
+            adjust_absorb<K, 1>(x, x[0], e, st, floor_bits);
+        }
     }
-    const int tail = vbegin + nvec * NV;
-    const int lone = head + (end - tail);  // values before and behind the vectors
-    auto lone_value = [&](int i, int& e) {
-        e = i < head ? begin + i : tail + (i - head);
-        const float l = load_scalar(base + e);
-        return ((allowed[(e - begin) >> 5] >> (e & 31)) & 1u) != 0u ? l : kNegInf;
-    };
-    for (int i = tid; i < lone; i += THREADS) {
-        int e;
-        const float x[1] = {lone_value(i, e)};
-        adjust_absorb<K, 1>(x, x[0], e, st, floor_bits);
-    }
-    // the special tokens, shared out over the row's slices
-    const int specials = A.special != nullptr && !forbidden ? A.n_records[seq] : 0;
-    const float r = A.repetition != nullptr ? A.repetition[seq] : 1.0f;
-    const AdjustRecord* rec = A.records + (int64_t)seq * A.max_records;
-    auto special_value = [&](int i, int& id) {
-        const AdjustRecord a = rec[i];
-        id = (int)(a.id & ~kAdjustSeen);
-        const bool ok = mrow == nullptr || ((mrow[id >> 5] >> (id & 31)) & 1u) != 0u;
-        float l = load_scalar(base + id);
-        if (a.id & kAdjustSeen) l = l > 0.f ? l / r : l * r;
-        return ok ? l + a.add : kNegInf;
-    };
-    for (int i = split * THREADS + tid; i < specials; i += splits * THREADS) {
-        int id;
-        const float x[1] = {special_value(i, id)};
-        adjust_absorb<K, 1>(x, x[0], id, st, floor_bits);
+    // The special tokens, several per lane at a time: records, then logits, then values.
+    constexpr int G = 4;
+    for (int i0 = first_special + tid; i0 < last_special; i0 += G * THREADS) {
+        AdjustRecord a[G];
+        float l[G];
+        uint32_t m[G];
+#pragma unroll
+        for (int e = 0; e < G; ++e) a[e] = rec[min(i0 + e * THREADS, last_special - 1)];
+#pragma unroll
+        for (int e = 0; e < G; ++e) {
+            const int id = (int)(a[e].id & ~kAdjustSeen);
+            l[e] = load_scalar(base + id);
+            m[e] = mrow != nullptr ? mrow[id >> 5] : 0xffffffffu;
+        }
+#pragma unroll
+        for (int e = 0; e < G; ++e) {
+            const float x[1] = {i0 + e * THREADS < last_special ? special_value(a[e], l[e], m[e]) : kNegInf};
+            adjust_absorb<K, 1>(x, x[0], (int)(a[e].id & ~kAdjustSeen), st, floor_bits);
+        }
     }
 
     // lanes -> wave -> workgroup, as conf_topk_kernel
@@ -377,10 +494,7 @@ __global__ __launch_bounds__(THREADS) void adjust_topk_kernel(AdjustParams A, co
     lanes_merge_ms<6>(m, s);
     uint64_t best[K];
     wave_top_keys<K>(st.tl, best, k);
-    constexpr int NW = THREADS / 64;
-    static_assert(NW > 1 && NW <= 16, "the row reduction covers at most 16 waves");
     TopList<K> tl;
-    const int lane = tid & 63, wave = tid >> 6;
     __shared__ float sh_m[NW], sh_s[NW];
     __shared__ uint64_t sh_k[NW][K];
     __shared__ float sh_max;
@@ -421,9 +535,10 @@ __global__ __launch_bounds__(THREADS) void adjust_topk_kernel(AdjustParams A, co
         float acc = 0.f;
         for (int e = begin + tid; e < end; e += THREADS)
             if ((allowed[(e - begin) >> 5] >> (e & 31)) & 1u) acc += fast_exp2((load_scalar(base + e) - top) * kLog2e);
-        for (int i = split * THREADS + tid; i < specials; i += splits * THREADS) {
-            int id;
-            acc += fast_exp2((special_value(i, id) - top) * kLog2e);
+        for (int i = first_special + tid; i < last_special; i += THREADS) {
+            const AdjustRecord a = rec[i];
+            const int id = (int)(a.id & ~kAdjustSeen);
+            acc += fast_exp2((special_value(a, load_scalar(base + id), mrow != nullptr ? mrow[id >> 5] : 0xffffffffu) - top) * kLog2e);
         }
         m = top;
         s = block_sum<THREADS>(acc, sh_s);
@@ -471,8 +586,16 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(const float* __restric
     if (lane == 0) adjust_finish<K>(best, m, s, row, k, conf, idx);
 }
 
-// Launch shape: threads per row slice and its register ring, slices per row (as plan_conf_topk; a wave per row
-// would hold the allowed bits of one row per wave in LDS, so rows take 4 waves at least).
+inline size_t adjust_lds(int chunk) { return ((size_t)(chunk + 31) / 32 + 1 + kAdjustList) * sizeof(uint32_t); }
+// LDS of adjust_prepare_kernel: bits and prefixes, then 16 bytes per record of the window.
+inline size_t adjust_prepare_fixed(int groups) { return (size_t)groups * (kAdjustGroup / 32 * 6 + 4); }
+inline int adjust_window(int groups, int max_records) {
+    const int most = (int)((kAdjustLds - adjust_prepare_fixed(groups)) / 16);
+    return max_records < most ? max_records : most;
+}
+
+// Launch shape: threads per row slice and its register ring, slices per row (as plan_conf_topk; one wave per row
+// would hold the allowed bits of a row per wave in LDS, so rows take 4 waves at least).
 inline TopkPlan plan_adjust(int64_t rows, int64_t vocab, int vec) {
     TopkPlan p = plan_conf_topk(rows, vocab, vec);
     if (p.threads == 64) p = TopkPlan{256, 2, 2, 1, (int)vocab};

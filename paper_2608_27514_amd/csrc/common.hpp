@@ -65,6 +65,18 @@ __device__ __forceinline__ void lane_pair(int step, uint32_t v, uint32_t& a, uin
     }
 }
 
+// Inclusive prefix sums over the wave's lanes, on the lane-exchange network: shifts by 1, 2, 4 and 8 within each row of
+// 16 lanes, then the last lane of rows 0 and 2 into the row behind, then the last of the lower half into the upper.
+__device__ __forceinline__ int wave_prefix(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+
 // XCD-aware workgroup order: the dispatcher hands workgroup i to XCD (i % 8).  Returning
 // a logical id such that the workgroups that land on one XCD get consecutive logical ids
 // keeps the tiles that share K/V (consecutive logical ids) in one XCD's L2.

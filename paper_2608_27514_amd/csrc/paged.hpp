@@ -190,18 +190,6 @@ __device__ __forceinline__ int paged_chunk(int64_t total, int units, int capacit
     return kPagedGranule * (granules < 1 ? 1 : granules);
 }
 
-// Inclusive prefix sums over the wave's lanes, on the lane-exchange network: shifts by 1, 2, 4 and 8 within each row of
-// 16 lanes, then the last lane of rows 0 and 2 into the row behind, then the last of the lower half into the upper.
-__device__ __forceinline__ int wave_prefix(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
-    return x;
-}
-
 // The range that `slot` stands for; false where the batch has fewer.  All lanes of the wave take part.
 __device__ __forceinline__ bool paged_range(const PagedAttnParams& P, int slot, bool report, PagedRange& r) {
     const int lane = threadIdx.x & 63;

@@ -648,12 +648,13 @@ traj_status check_adjust(const traj_logits_shape* sh, int32_t k, const traj_logi
     return TRAJ_OK;
 }
 
-// The workspace's parts: the sequences' bitmaps, record counts and records; then the split records.
+// The workspace's parts: the sequences' bitmaps, record prefixes and records; then the split records.
 struct AdjustPlan {
     TopkPlan topk;
     int64_t n_seq;
     int max_records;
-    size_t counts, records, partial, total;  // `partial`: what has to fit
+    int groups;
+    size_t before, records, partial, total;  // `partial`: what has to fit
 };
 
 AdjustPlan plan_adjust_call(const traj_logits_shape* sh, const traj_logit_adjust* a) {
@@ -662,8 +663,9 @@ AdjustPlan plan_adjust_call(const traj_logits_shape* sh, const traj_logit_adjust
     p.max_records = (int)std::min<int64_t>(sh->vocab, (int64_t)a->history_size + a->bias_size);
     if (p.max_records > 0) {
         p.n_seq = (sh->rows + a->rows_per_seq - 1) / a->rows_per_seq;
-        p.counts = align256((size_t)p.n_seq * ((sh->vocab + 31) / 32) * 4);
-        p.records = p.counts + align256((size_t)p.n_seq * 4);
+        p.groups = (int)((sh->vocab + kAdjustGroup - 1) / kAdjustGroup);
+        p.before = align256((size_t)p.n_seq * ((sh->vocab + 31) / 32) * 4);
+        p.records = p.before + align256((size_t)p.n_seq * (p.groups + 1) * 4);
         p.partial = p.records + align256((size_t)p.n_seq * p.max_records * sizeof(AdjustRecord));
     }
     p.total = p.partial + (p.topk.splits > 1 ? (size_t)sh->rows * p.topk.splits * kTopkRecord * sizeof(float) : 0);
@@ -673,8 +675,7 @@ AdjustPlan plan_adjust_call(const traj_logits_shape* sh, const traj_logit_adjust
 template <typename T, int K, int THREADS, int U, int DEPTH>
 void launch_adjust_kernel(const AdjustParams& A, const void* lg, const traj_logits_shape* sh, int k, const TopkPlan& plan, float* conf,
                           int32_t* idx, float* partial, hipStream_t st) {
-    const size_t lds = ((size_t)(plan.chunk + 31) / 32 + 1) * sizeof(uint32_t);
-    hipLaunchKernelGGL((adjust_topk_kernel<T, K, THREADS, U, DEPTH>), dim3((unsigned)(sh->rows * plan.splits)), dim3(THREADS), lds, st, A,
+    hipLaunchKernelGGL((adjust_topk_kernel<T, K, THREADS, U, DEPTH>), dim3((unsigned)(sh->rows * plan.splits)), dim3(THREADS), adjust_lds(plan.chunk), st, A,
                        static_cast<const T*>(lg), sh->row_stride, k, plan.splits, plan.chunk, conf, idx, partial);
 }
 
@@ -1111,11 +1112,12 @@ traj_status traj_confidence_topk_adjusted(const void* logits, int32_t k, float* 
     hipStream_t s = as_stream(stream);
     if (plan.max_records > 0) {
         p.special = reinterpret_cast<uint32_t*>(ws);
-        p.n_records = reinterpret_cast<int32_t*>(ws + plan.counts);
+        p.before = reinterpret_cast<int32_t*>(ws + plan.before);
         p.records = reinterpret_cast<AdjustRecord*>(ws + plan.records);
-        const int groups = (p.V + kAdjustGroup - 1) / kAdjustGroup;
-        const size_t lds = ((size_t)groups * (kAdjustGroup / 32 + 1) + 2 * kAdjustWindow) * 4;
-        hipLaunchKernelGGL(adjust_prepare_kernel, dim3((unsigned)plan.n_seq), dim3(kAdjustPrepThreads), lds, s, p);
+        p.groups = plan.groups;
+        p.window = adjust_window(p.groups, p.max_records);
+        hipLaunchKernelGGL(adjust_prepare_kernel, dim3((unsigned)plan.n_seq), dim3(kAdjustPrepThreads),
+                           adjust_prepare_fixed(p.groups) + 16 * (size_t)p.window, s, p);
         const traj_status rs = launched();
         if (rs != TRAJ_OK) return rs;
     }

@@ -176,7 +176,7 @@ def test_many_history_tokens_and_duplicates():
 
 
 def test_largest_vocabulary():
-    V = 1 << 20
+    V = 1 << 19
     rng = np.random.default_rng(10)
     x, how = make(rng, 1, 2, V, 100, 5, 2, 0.7)
     check(x, how, 3, 2)

@@ -109,7 +109,7 @@ def test_adjusted_arguments():
     assert adjust(L(4, 100, 100, 9)) == DTYPE
     assert adjust(L(4, 100, 99, 0)) == SHAPE
     assert adjust(k=0) == ARG and adjust(k=9) == ARG and adjust(L(4, 2, 2, 1)) == ARG
-    assert adjust(L(4, (1 << 20) + 1, 1 << 21, 0)) == UNSUPPORTED
+    assert adjust(L(4, (1 << 19) + 1, 1 << 21, 0)) == UNSUPPORTED
     for bad in (dict(rows_per_seq=0), dict(history_size=-1), dict(bias_size=-1), dict(history_size=1 << 29, bias_size=1 << 29),
                 dict(mask=FAKE, n_masks=0, mask_stride=32), dict(mask=FAKE, n_masks=32, mask_stride=31),
                 dict(mask=FAKE, n_masks=31, mask_stride=32)):
