@@ -6,6 +6,7 @@ If the library is not built the calls raise -- there is no fallback.
 """
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -582,50 +583,65 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _paged_shape(B, T, Hq, k_pages, v_pages, page_table):
-    """The shape of a paged call; checks the pools and the table."""
+def _arg(t, name, dtype, shape):
+    """Checks a contiguous device tensor of this type and shape; returns its address.  One condition for what is right
+    (a decoding step makes such checks some thirty times), the reasons for what is not."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    p = _dev(t, name, dtype)
+    _expect_shape(t, name, shape)
+    return p
+
+
+@functools.lru_cache(maxsize=1024)
+def _paged_struct(B, T, Hq, pages, strides, table, table_strides):
+    """The C shape of a paged call, by sizes and strides alone: (structure, reference to it)."""
+    if len(pages) != 4 or strides[3] != 1:
+        raise ValueError("k_pages and v_pages must be [pages, page_size, Hkv, D] with a contiguous last dimension")
+    if len(table) != 2 or table[0] != B or table_strides[1] != 1 and table[1] > 1:
+        raise ValueError("page_table must be [B, max_pages] with contiguous rows")
+    # a dimension of one entry has no stride that matters
+    sh = PagedShape(B, T, Hq, pages[2], pages[3], pages[0], pages[1], table[1], max(table_strides[0], table[1]) if B <= 1 else table_strides[0],
+                    strides[0] if pages[0] > 1 else 8, strides[1] if pages[1] > 1 else 8, strides[2] if pages[2] > 1 else 8)
+    return sh, ctypes.byref(sh)
+
+
+@functools.lru_cache(maxsize=1024)
+def _paged_workspace(*sizes):
+    return int(_lib().traj_paged_attn_workspace_size(_paged_struct(*sizes)[1]))
+
+
+def _paged_sizes(B, T, Hq, k_pages, v_pages, page_table):
+    """Checks the pools and the table; returns what :func:`_paged_struct` takes."""
+    bf16 = torch.bfloat16
     for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages")):
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise TypeError(f"{n} must be a CUDA (HIP) tensor")
-        if t.dtype != torch.bfloat16:
-            raise TypeError(f"{n} must be {torch.bfloat16}, got {t.dtype}")
-        if t.dim() != 4 or t.stride(3) != 1:
-            raise ValueError(f"{n} must be [pages, page_size, Hkv, D] with a contiguous last dimension")
-    if k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride():
+        if t.dtype is not bf16:
+            raise TypeError(f"{n} must be {bf16}, got {t.dtype}")
+    pages, strides = k_pages.shape, k_pages.stride()
+    if v_pages.shape != pages or v_pages.stride() != strides:
         raise ValueError("k_pages and v_pages must have the same shape and strides")
-    if not isinstance(page_table, torch.Tensor) or not page_table.is_cuda or page_table.dtype != torch.int32:
+    if not isinstance(page_table, torch.Tensor) or not page_table.is_cuda or page_table.dtype is not torch.int32:
         raise TypeError("page_table must be a CUDA (HIP) tensor of torch.int32")
-    if page_table.dim() != 2 or page_table.shape[0] != B or page_table.stride(1) != 1 and page_table.shape[1] > 1:
-        raise ValueError("page_table must be [B, max_pages] with contiguous rows")
     _here(k_pages, "k_pages")
-    pages, page_size, Hkv, D = k_pages.shape
-    st = k_pages.stride()
-    cols = page_table.shape[1]
-    # a dimension of one entry has no stride that matters
-    return PagedShape(B, T, Hq, Hkv, D, pages, page_size, cols, max(page_table.stride(0), cols) if B <= 1 else page_table.stride(0),
-                      st[0] if pages > 1 else 8, st[1] if page_size > 1 else 8, st[2] if Hkv > 1 else 8)
+    return B, T, Hq, pages, strides, page_table.shape, page_table.stride()
 
 
-def _token_rows(t, name, B, T, heads, D):
+def _token_rows(t, name, shape):
     """Checks a [B, T, heads, D] tensor whose token rows hold their heads side by side; returns (address, row stride)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
-    _expect_shape(t, name, (B, T, heads, D))
+    if t.shape != shape:
+        _expect_shape(t, name, shape)
+    B, T, heads, D = shape
     sb, st, sh, sd = t.stride()
     row = st if T > 1 else sb if B > 1 else heads * D
     if sd != 1 or (heads > 1 and sh != D) or (B > 1 and T > 1 and sb != T * st):
         raise ValueError(f"{name} must have evenly spaced token rows of contiguous heads")
-    return t.data_ptr() if t.numel() > 0 else None, row
-
-
-def _per_seq(t, name, B, dtype=torch.int32):
-    if t is None:
-        return None
-    p = _dev(t, name, dtype)
-    _expect_shape(t, name, (B,))
-    return p
+    return t.data_ptr(), row
 
 
 def paged_append(k, v, k_pages, v_pages, page_table, start, q=None, q_out=None, n_new=None, pos0=None,
@@ -639,99 +655,105 @@ def paged_append(k, v, k_pages, v_pages, page_table, start, q=None, q_out=None, 
     None; its padding rows are then zero), or None without q."""
     B, T, Hkv, D = k.shape
     Hq = q.shape[2] if q is not None else Hkv
-    sh = _paged_shape(B, T, Hq, k_pages, v_pages, page_table)
-    if (sh.Hkv, sh.D) != (Hkv, D):
+    sh, ref = _paged_struct(*_paged_sizes(B, T, Hq, k_pages, v_pages, page_table))
+    if sh.Hkv != Hkv or sh.D != D:
         raise ValueError(f"k has {Hkv} heads of {D}, the pages {sh.Hkv} of {sh.D}")
-    kp, ks = _token_rows(k, "k", B, T, Hkv, D)
-    vp, vs = _token_rows(v, "v", B, T, Hkv, D)
-    qp, qs, qop = None, 0, None
+    shape = (B, T, Hkv, D)
+    kp, ks = _token_rows(k, "k", shape)
+    vp, vs = _token_rows(v, "v", shape)
+    qp, qs, qop, i32, per_seq = None, 0, None, torch.int32, (B,)
     if q is not None:
-        qp, qs = _token_rows(q, "q", B, T, Hq, D)
+        shape = (B, T, Hq, D)
+        qp, qs = _token_rows(q, "q", shape)
         if q_out is None:
             if n_new is None:
-                q_out = _empty((B, T, Hq, D), torch.bfloat16, q.device, stream)
+                q_out = _empty(shape, torch.bfloat16, q.device, stream)
             else:
                 with torch.cuda.stream(stream):  # None: the current one
-                    q_out = torch.zeros((B, T, Hq, D), dtype=torch.bfloat16, device=q.device)
-        qop = _dev(q_out, "q_out", torch.bfloat16)
-        _expect_shape(q_out, "q_out", (B, T, Hq, D))
+                    q_out = torch.zeros(shape, dtype=torch.bfloat16, device=q.device)
+        qop = _arg(q_out, "q_out", torch.bfloat16, shape)
     elif q_out is not None:
         raise ValueError("q_out needs q")
     st = _lib().traj_paged_append(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
-                                  _per_seq(start, "start", B), _per_seq(n_new, "n_new", B), _per_seq(pos0, "pos0", B),
-                                  ctypes.byref(sh), float(rope_theta), _stream(stream))
-    _check(st, "traj_paged_append")
+                                  _arg(start, "start", i32, per_seq),
+                                  None if n_new is None else _arg(n_new, "n_new", i32, per_seq),
+                                  None if pos0 is None else _arg(pos0, "pos0", i32, per_seq), ref, rope_theta, _stream(stream))
+    if st != TRAJ_OK:
+        _check(st, "traj_paged_append")
     return q_out
 
 
 def paged_attn_workspace_size(q, k_pages, v_pages, page_table):
-    return int(_lib().traj_paged_attn_workspace_size(ctypes.byref(_paged_shape(*q.shape[:3], k_pages, v_pages, page_table))))
+    return _paged_workspace(*_paged_sizes(*q.shape[:3], k_pages, v_pages, page_table))
 
 
 def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causal=False, workspace=None, stream=None):
     """Attention of T new tokens per sequence, q [B,T,Hq,D] (bf16), over the first lens[b] cached keys of each
     (causal: the new tokens are the last T of them and see those up to themselves).  Pages and table as
     :func:`paged_append`; lens [B] int32.  Returns ``out`` [B,T,Hq,D]; a row that sees no key is zero."""
-    B, T, Hq, D = q.shape
-    qp = _dev(q, "q", torch.bfloat16)
-    sh = _paged_shape(B, T, Hq, k_pages, v_pages, page_table)
+    shape = B, T, Hq, D = q.shape
+    bf16 = torch.bfloat16
+    qp = _arg(q, "q", bf16, shape)
+    sizes = _paged_sizes(B, T, Hq, k_pages, v_pages, page_table)
+    sh, ref = _paged_struct(*sizes)
     if sh.D != D:
         raise ValueError(f"q has heads of {D}, the pages of {sh.D}")
     if out is None:
-        out = _empty((B, T, Hq, D), torch.bfloat16, q.device, stream)
-    else:
-        _expect_shape(out, "out", (B, T, Hq, D))
-    outp = _dev(out, "out", torch.bfloat16)
-    lib = _lib()
+        out = _empty(shape, bf16, q.device, stream)
+    ws, ws_bytes = None, 0
     if workspace is None:
-        need = lib.traj_paged_attn_workspace_size(ctypes.byref(sh))
-        if need > 0:
-            workspace = _empty(need, torch.uint8, q.device, stream)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    st = lib.traj_paged_attn(qp, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), _per_seq(lens, "lens", B), outp,
-                             ctypes.byref(sh), float(scale), 1 if causal else 0, _ptr(workspace), ws_bytes, _stream(stream))
-    _check(st, "traj_paged_attn")
+        ws_bytes = _paged_workspace(*sizes)
+        if ws_bytes > 0:
+            workspace = _empty((ws_bytes,), torch.uint8, q.device, stream)
+            ws = workspace.data_ptr()
+    else:
+        ws, ws_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
+    st = _lib().traj_paged_attn(qp, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), _arg(lens, "lens", torch.int32, (B,)),
+                                _arg(out, "out", bf16, shape), ref, scale, 1 if causal else 0, ws, ws_bytes, _stream(stream))
+    if st != TRAJ_OK:
+        _check(st, "traj_paged_attn")
     return out
 
 
 # ---------------------------------------------------------------- adjusted logits
-def _logit_adjust(logits, rows_per_seq, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index):
-    R, V = logits.shape
-    per = int(rows_per_seq)
+def _logit_adjust(R, V, per, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index):
     if per < 1:
         raise ValueError("rows_per_seq must be at least 1")
-    n = -(-R // per)
-    a = LogitAdjust(rows_per_seq=per)
     f32, i32 = torch.float32, torch.int32
+    n = -(-R // per)
+    H = NB = masks = mask_stride = 0
+    hp = lp = rp = fp = pp = ip = bp = mp = xp = None
     if history is not None:
-        a.history = _dev(history, "history", i32)
-        _expect_shape(history, "history", (n, history.shape[-1]))
-        a.history_size = history.shape[-1]
-    for name, t, dt in (("history_len", history_len, i32), ("repetition", repetition, f32), ("frequency", frequency, f32),
-                        ("presence", presence, f32)):
-        if t is not None:
-            if history is None:
-                raise ValueError(f"{name} needs history")
-            setattr(a, name, _per_seq(t, name, n, dt))
+        H = history.shape[-1]
+        hp = _arg(history, "history", i32, (n, H))
+    for name, t in (("history_len", history_len), ("repetition", repetition), ("frequency", frequency), ("presence", presence)):
+        if t is not None and history is None:
+            raise ValueError(f"{name} needs history")
+    if history_len is not None:
+        lp = _arg(history_len, "history_len", i32, (n,))
+    if repetition is not None:
+        rp = _arg(repetition, "repetition", f32, (n,))
+    if frequency is not None:
+        fp = _arg(frequency, "frequency", f32, (n,))
+    if presence is not None:
+        pp = _arg(presence, "presence", f32, (n,))
     if (bias_ids is None) != (bias is None):
         raise ValueError("bias_ids and bias go together")
     if bias is not None:
-        a.bias_ids, a.bias = _dev(bias_ids, "bias_ids", i32), _dev(bias, "bias", f32)
-        _expect_shape(bias, "bias", (n, bias.shape[-1]))
-        _expect_shape(bias_ids, "bias_ids", bias.shape)
-        a.bias_size = bias.shape[-1]
+        NB = bias.shape[-1]
+        ip, bp = _arg(bias_ids, "bias_ids", i32, (n, NB)), _arg(bias, "bias", f32, (n, NB))
     if mask is not None:
-        a.mask = _dev(mask, "mask", i32)
+        mp = _arg(mask, "mask", i32, mask.shape)
         if mask.dim() != 2 or mask.shape[0] < 1 or mask.shape[1] < -(-V // 32):
             raise ValueError(f"mask must be [n_masks, at least {-(-V // 32)}] words")
-        a.n_masks, a.mask_stride = mask.shape
-        if mask_index is None and mask.shape[0] < R:
+        masks, mask_stride = mask.shape
+        if mask_index is None and masks < R:
             raise ValueError("mask must have a row for every row of logits, or mask_index one entry")
     if mask_index is not None:
         if mask is None:
             raise ValueError("mask_index needs mask")
-        a.mask_index = _per_seq(mask_index, "mask_index", R)
-    return a
+        xp = _arg(mask_index, "mask_index", i32, (R,))
+    return LogitAdjust(per, H, NB, masks, hp, lp, rp, fp, pp, ip, bp, mp, xp, mask_stride)
 
 
 def _logit_rows(logits):
@@ -745,11 +767,17 @@ def _logit_rows(logits):
     return sh
 
 
+@functools.lru_cache(maxsize=1024)
+def _adjust_workspace(rows, vocab, row_stride, dtype, k, per, H, NB):
+    return int(_lib().traj_confidence_topk_adjusted_workspace_size(ctypes.byref(LogitsShape(rows, vocab, row_stride, dtype)), k,
+                                                                   ctypes.byref(LogitAdjust(per, H, NB))))
+
+
 def confidence_topk_adjusted_workspace_size(logits, k, rows_per_seq, history=None, bias=None):
     """Bytes for a call with these logits and lists (their sizes count)."""
-    a = LogitAdjust(rows_per_seq=int(rows_per_seq), history_size=0 if history is None else history.shape[-1],
-                    bias_size=0 if bias is None else bias.shape[-1])
-    return int(_lib().traj_confidence_topk_adjusted_workspace_size(ctypes.byref(_logit_rows(logits)), int(k), ctypes.byref(a)))
+    sh = _logit_rows(logits)
+    return _adjust_workspace(sh.rows, sh.vocab, sh.row_stride, sh.dtype, int(k), int(rows_per_seq),
+                             0 if history is None else history.shape[-1], 0 if bias is None else bias.shape[-1])
 
 
 def confidence_topk_adjusted(logits, k, rows_per_seq, history=None, history_len=None, repetition=None, frequency=None,
@@ -763,26 +791,27 @@ def confidence_topk_adjusted(logits, k, rows_per_seq, history=None, history_len=
     mask r).  Slots without an allowed token hold confidence 0 and index -1."""
     sh = _logit_rows(logits)
     _here(logits, "logits")
-    a = _logit_adjust(logits, rows_per_seq, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index)
-    R, k = logits.shape[0], int(k)
-    dev = logits.device
+    k, per = int(k), int(rows_per_seq)
+    R = sh.rows
+    a = _logit_adjust(R, sh.vocab, per, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index)
+    dev, shape = logits.device, (R, k)
     if conf is None:
-        conf = _empty((R, k), torch.float32, dev, stream)
+        conf = _empty(shape, torch.float32, dev, stream)
     if idx is None:
-        idx = _empty((R, k), torch.int32, dev, stream)
-    _dev(conf, "conf", torch.float32)
-    _dev(idx, "idx", torch.int32)
-    _expect_shape(conf, "conf", (R, k))
-    _expect_shape(idx, "idx", (R, k))
-    lib = _lib()
+        idx = _empty(shape, torch.int32, dev, stream)
+    ws, ws_bytes = None, 0
     if workspace is None:
-        need = lib.traj_confidence_topk_adjusted_workspace_size(ctypes.byref(sh), k, ctypes.byref(a))
-        if need > 0:
-            workspace = _empty(need, torch.uint8, dev, stream)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    st = lib.traj_confidence_topk_adjusted(_ptr(logits), k, _ptr(conf), _ptr(idx), ctypes.byref(sh), ctypes.byref(a),
-                                           _ptr(workspace), ws_bytes, _stream(stream))
-    _check(st, "traj_confidence_topk_adjusted")
+        ws_bytes = _adjust_workspace(R, sh.vocab, sh.row_stride, sh.dtype, k, per, a.history_size, a.bias_size)
+        if ws_bytes > 0:
+            workspace = _empty((ws_bytes,), torch.uint8, dev, stream)
+            ws = workspace.data_ptr()
+    else:
+        ws, ws_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
+    st = _lib().traj_confidence_topk_adjusted(logits.data_ptr(), k, _arg(conf, "conf", torch.float32, shape),
+                                              _arg(idx, "idx", torch.int32, shape), ctypes.byref(sh), ctypes.byref(a), ws, ws_bytes,
+                                              _stream(stream))
+    if st != TRAJ_OK:
+        _check(st, "traj_confidence_topk_adjusted")
     return conf, idx
 
 
