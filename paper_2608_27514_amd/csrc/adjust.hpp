@@ -413,25 +413,30 @@ __global__ __launch_bounds__(THREADS) void adjust_topk_kernel(AdjustParams A, co
                 b[u] = __builtin_nontemporal_load(vp + (!masked || vec_bits(v0) != 0u ? v : 0));
             }
         };
+        // the values of a vector, forbidden ones -inf; false where the wave has none
+        auto values = [&](int v0, const u32x4_t& b, float (&x)[NV]) {
+            const uint32_t ok = any_bits ? vec_bits(v0) : v0 + tid < nvec ? kAll : 0u;
+            if (ballot64(ok != 0u) == 0ull) return false;
+            unpack(b, x);
+            if (ballot64(ok != kAll) != 0ull) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    const int m = (int)(ok << (31 - j)) >> 31;
+                    const int xi = __builtin_bit_cast(int, x[j]);
+                    x[j] = __builtin_bit_cast(float, (xi & m) | ((int)0xff800000 & ~m));
+                }
+            }
+            return true;
+        };
         auto absorb_sweep = [&](int sweep, const u32x4_t (&b)[U]) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int v0 = sweep * SW + u * THREADS;
-                const uint32_t ok = any_bits ? vec_bits(v0) : v0 + tid < nvec ? kAll : 0u;
-                if (ballot64(ok != 0u) == 0ull) continue;
                 float x[NV];
-                unpack(b[u], x);
-                if (ballot64(ok != kAll) != 0ull) {
-#pragma unroll
-                    for (int j = 0; j < NV; ++j) {
-                        const int m = (int)(ok << (31 - j)) >> 31;
-                        const int xi = __builtin_bit_cast(int, x[j]);
-                        x[j] = __builtin_bit_cast(float, (xi & m) | ((int)0xff800000 & ~m));
-                    }
-                }
+                if (!values(v0, b[u], x)) continue;
                 adjust_absorb<K, NV>(x, vec_max<NV>(x), vbegin + (v0 + tid) * NV, st, floor_bits);
             }
-            if ((sweep & (sweep + 1)) == 0) {
+            if (sweep != 0 && (sweep & (sweep + 1)) == 0) {
                 const uint32_t own = wave_kth_floor<K>(st.lmax, k);
                 floor_bits = share_floor(own > floor_bits ? own : floor_bits);
                 st.refresh(floor_bits);
@@ -448,6 +453,17 @@ __global__ __launch_bounds__(THREADS) void adjust_topk_kernel(AdjustParams A, co
             if (masked) {
 #pragma unroll
                 for (int d = 0; d + 1 < DEPTH; ++d) load(d, buf[d]);
+            }
+            {  // a first floor from sweep 0's lane maxima, so that sweep 0 already inserts rarely
+                float lm = kNegInf;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float x[NV];
+                    if (values(u * THREADS, buf[0][u], x)) lm = __builtin_elementwise_maximum(lm, vec_max<NV>(x));
+                }
+                const uint32_t own = wave_kth_floor<K>(lm, k);
+                floor_bits = share_floor(own > floor_bits ? own : floor_bits);
+                st.refresh(floor_bits);
             }
             for (int it = 0; it < nsw; it += DEPTH) {
 #pragma unroll
