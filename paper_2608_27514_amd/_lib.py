@@ -569,10 +569,17 @@ def linear(x, w, y=None, accumulate=False, workspace=None, stream=None):
 
 
 # ---------------------------------------------------------------- paged cache
-def _here(t, name):
-    """The library launches on the current device: a tensor of another one is refused."""
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+def _current():
+    """Index of the current device, on which the library launches."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+
+
+def _here(t, name, dev):
+    """A tensor of another device than the current one is refused."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
 
 
 def _empty(shape, dtype, device, stream):
@@ -583,13 +590,14 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _arg(t, name, dtype, shape):
-    """Checks a contiguous device tensor of this type and shape; returns its address.  One condition for what is right
-    (a decoding step makes such checks some thirty times), the reasons for what is not."""
-    if type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous():
+def _arg(t, name, dtype, shape, dev):
+    """Checks a contiguous tensor of this type and shape on device `dev`; returns its address.  One condition for what
+    is right (a decoding step makes such checks some thirty times), the reasons for what is not."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
         return t.data_ptr()
     p = _dev(t, name, dtype)
     _expect_shape(t, name, shape)
+    _here(t, name, dev)
     return p
 
 
@@ -611,27 +619,24 @@ def _paged_workspace(*sizes):
     return int(_lib().traj_paged_attn_workspace_size(_paged_struct(*sizes)[1]))
 
 
-def _paged_sizes(B, T, Hq, k_pages, v_pages, page_table):
+def _paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev):
     """Checks the pools and the table; returns what :func:`_paged_struct` takes."""
     bf16 = torch.bfloat16
-    for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages")):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{n} must be a CUDA (HIP) tensor")
-        if t.dtype is not bf16:
-            raise TypeError(f"{n} must be {bf16}, got {t.dtype}")
+    for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages"), (page_table, "page_table")):
+        _here(t, n, dev)
+    if k_pages.dtype is not bf16 or v_pages.dtype is not bf16:
+        raise TypeError(f"k_pages and v_pages must be {bf16}")
+    if page_table.dtype is not torch.int32:
+        raise TypeError("page_table must be torch.int32")
     pages, strides = k_pages.shape, k_pages.stride()
     if v_pages.shape != pages or v_pages.stride() != strides:
         raise ValueError("k_pages and v_pages must have the same shape and strides")
-    if not isinstance(page_table, torch.Tensor) or not page_table.is_cuda or page_table.dtype is not torch.int32:
-        raise TypeError("page_table must be a CUDA (HIP) tensor of torch.int32")
-    _here(k_pages, "k_pages")
     return B, T, Hq, pages, strides, page_table.shape, page_table.stride()
 
 
-def _token_rows(t, name, shape):
+def _token_rows(t, name, shape, dev):
     """Checks a [B, T, heads, D] tensor whose token rows hold their heads side by side; returns (address, row stride)."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    _here(t, name, dev)
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
     if t.shape != shape:
@@ -655,36 +660,37 @@ def paged_append(k, v, k_pages, v_pages, page_table, start, q=None, q_out=None, 
     None; its padding rows are then zero), or None without q."""
     B, T, Hkv, D = k.shape
     Hq = q.shape[2] if q is not None else Hkv
-    sh, ref = _paged_struct(*_paged_sizes(B, T, Hq, k_pages, v_pages, page_table))
+    dev = _current()
+    sh, ref = _paged_struct(*_paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev))
     if sh.Hkv != Hkv or sh.D != D:
         raise ValueError(f"k has {Hkv} heads of {D}, the pages {sh.Hkv} of {sh.D}")
     shape = (B, T, Hkv, D)
-    kp, ks = _token_rows(k, "k", shape)
-    vp, vs = _token_rows(v, "v", shape)
+    kp, ks = _token_rows(k, "k", shape, dev)
+    vp, vs = _token_rows(v, "v", shape, dev)
     qp, qs, qop, i32, per_seq = None, 0, None, torch.int32, (B,)
     if q is not None:
         shape = (B, T, Hq, D)
-        qp, qs = _token_rows(q, "q", shape)
+        qp, qs = _token_rows(q, "q", shape, dev)
         if q_out is None:
             if n_new is None:
                 q_out = _empty(shape, torch.bfloat16, q.device, stream)
             else:
                 with torch.cuda.stream(stream):  # None: the current one
                     q_out = torch.zeros(shape, dtype=torch.bfloat16, device=q.device)
-        qop = _arg(q_out, "q_out", torch.bfloat16, shape)
+        qop = _arg(q_out, "q_out", torch.bfloat16, shape, dev)
     elif q_out is not None:
         raise ValueError("q_out needs q")
     st = _lib().traj_paged_append(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
-                                  _arg(start, "start", i32, per_seq),
-                                  None if n_new is None else _arg(n_new, "n_new", i32, per_seq),
-                                  None if pos0 is None else _arg(pos0, "pos0", i32, per_seq), ref, rope_theta, _stream(stream))
+                                  _arg(start, "start", i32, per_seq, dev),
+                                  None if n_new is None else _arg(n_new, "n_new", i32, per_seq, dev),
+                                  None if pos0 is None else _arg(pos0, "pos0", i32, per_seq, dev), ref, rope_theta, _stream(stream))
     if st != TRAJ_OK:
         _check(st, "traj_paged_append")
     return q_out
 
 
 def paged_attn_workspace_size(q, k_pages, v_pages, page_table):
-    return _paged_workspace(*_paged_sizes(*q.shape[:3], k_pages, v_pages, page_table))
+    return _paged_workspace(*_paged_sizes(*q.shape[:3], k_pages, v_pages, page_table, _current()))
 
 
 def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causal=False, workspace=None, stream=None):
@@ -693,8 +699,9 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causa
     :func:`paged_append`; lens [B] int32.  Returns ``out`` [B,T,Hq,D]; a row that sees no key is zero."""
     shape = B, T, Hq, D = q.shape
     bf16 = torch.bfloat16
-    qp = _arg(q, "q", bf16, shape)
-    sizes = _paged_sizes(B, T, Hq, k_pages, v_pages, page_table)
+    dev = _current()
+    qp = _arg(q, "q", bf16, shape, dev)
+    sizes = _paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev)
     sh, ref = _paged_struct(*sizes)
     if sh.D != D:
         raise ValueError(f"q has heads of {D}, the pages of {sh.D}")
@@ -708,15 +715,15 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causa
             ws = workspace.data_ptr()
     else:
         ws, ws_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
-    st = _lib().traj_paged_attn(qp, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), _arg(lens, "lens", torch.int32, (B,)),
-                                _arg(out, "out", bf16, shape), ref, scale, 1 if causal else 0, ws, ws_bytes, _stream(stream))
+    st = _lib().traj_paged_attn(qp, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), _arg(lens, "lens", torch.int32, (B,), dev),
+                                _arg(out, "out", bf16, shape, dev), ref, scale, 1 if causal else 0, ws, ws_bytes, _stream(stream))
     if st != TRAJ_OK:
         _check(st, "traj_paged_attn")
     return out
 
 
 # ---------------------------------------------------------------- adjusted logits
-def _logit_adjust(R, V, per, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index):
+def _logit_adjust(dev, R, V, per, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index):
     if per < 1:
         raise ValueError("rows_per_seq must be at least 1")
     f32, i32 = torch.float32, torch.int32
@@ -725,25 +732,25 @@ def _logit_adjust(R, V, per, history, history_len, repetition, frequency, presen
     hp = lp = rp = fp = pp = ip = bp = mp = xp = None
     if history is not None:
         H = history.shape[-1]
-        hp = _arg(history, "history", i32, (n, H))
+        hp = _arg(history, "history", i32, (n, H), dev)
     for name, t in (("history_len", history_len), ("repetition", repetition), ("frequency", frequency), ("presence", presence)):
         if t is not None and history is None:
             raise ValueError(f"{name} needs history")
     if history_len is not None:
-        lp = _arg(history_len, "history_len", i32, (n,))
+        lp = _arg(history_len, "history_len", i32, (n,), dev)
     if repetition is not None:
-        rp = _arg(repetition, "repetition", f32, (n,))
+        rp = _arg(repetition, "repetition", f32, (n,), dev)
     if frequency is not None:
-        fp = _arg(frequency, "frequency", f32, (n,))
+        fp = _arg(frequency, "frequency", f32, (n,), dev)
     if presence is not None:
-        pp = _arg(presence, "presence", f32, (n,))
+        pp = _arg(presence, "presence", f32, (n,), dev)
     if (bias_ids is None) != (bias is None):
         raise ValueError("bias_ids and bias go together")
     if bias is not None:
         NB = bias.shape[-1]
-        ip, bp = _arg(bias_ids, "bias_ids", i32, (n, NB)), _arg(bias, "bias", f32, (n, NB))
+        ip, bp = _arg(bias_ids, "bias_ids", i32, (n, NB), dev), _arg(bias, "bias", f32, (n, NB), dev)
     if mask is not None:
-        mp = _arg(mask, "mask", i32, mask.shape)
+        mp = _arg(mask, "mask", i32, mask.shape, dev)
         if mask.dim() != 2 or mask.shape[0] < 1 or mask.shape[1] < -(-V // 32):
             raise ValueError(f"mask must be [n_masks, at least {-(-V // 32)}] words")
         masks, mask_stride = mask.shape
@@ -752,7 +759,7 @@ def _logit_adjust(R, V, per, history, history_len, repetition, frequency, presen
     if mask_index is not None:
         if mask is None:
             raise ValueError("mask_index needs mask")
-        xp = _arg(mask_index, "mask_index", i32, (R,))
+        xp = _arg(mask_index, "mask_index", i32, (R,), dev)
     return LogitAdjust(per, H, NB, masks, hp, lp, rp, fp, pp, ip, bp, mp, xp, mask_stride)
 
 
@@ -790,25 +797,26 @@ def confidence_topk_adjusted(logits, k, rows_per_seq, history=None, history_len=
     (bit v % 32 of word v // 32; 0 forbids) and mask_index [R] int32 each row's mask (-1: none; without it row r takes
     mask r).  Slots without an allowed token hold confidence 0 and index -1."""
     sh = _logit_rows(logits)
-    _here(logits, "logits")
+    dev = _current()
+    _here(logits, "logits", dev)
     k, per = int(k), int(rows_per_seq)
     R = sh.rows
-    a = _logit_adjust(R, sh.vocab, per, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index)
-    dev, shape = logits.device, (R, k)
+    a = _logit_adjust(dev, R, sh.vocab, per, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index)
+    shape = (R, k)
     if conf is None:
-        conf = _empty(shape, torch.float32, dev, stream)
+        conf = _empty(shape, torch.float32, logits.device, stream)
     if idx is None:
-        idx = _empty(shape, torch.int32, dev, stream)
+        idx = _empty(shape, torch.int32, logits.device, stream)
     ws, ws_bytes = None, 0
     if workspace is None:
         ws_bytes = _adjust_workspace(R, sh.vocab, sh.row_stride, sh.dtype, k, per, a.history_size, a.bias_size)
         if ws_bytes > 0:
-            workspace = _empty((ws_bytes,), torch.uint8, dev, stream)
+            workspace = _empty((ws_bytes,), torch.uint8, logits.device, stream)
             ws = workspace.data_ptr()
     else:
         ws, ws_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
-    st = _lib().traj_confidence_topk_adjusted(logits.data_ptr(), k, _arg(conf, "conf", torch.float32, shape),
-                                              _arg(idx, "idx", torch.int32, shape), ctypes.byref(sh), ctypes.byref(a), ws, ws_bytes,
+    st = _lib().traj_confidence_topk_adjusted(logits.data_ptr(), k, _arg(conf, "conf", torch.float32, shape, dev),
+                                              _arg(idx, "idx", torch.int32, shape, dev), ctypes.byref(sh), ctypes.byref(a), ws, ws_bytes,
                                               _stream(stream))
     if st != TRAJ_OK:
         _check(st, "traj_confidence_topk_adjusted")

@@ -151,6 +151,9 @@ constexpr int kPagedGranule = kPagedWaves * kPagedTile;
 // kPagedMostWgs of them: finer ones balance lengths and CUs better (32 sequences of up to 8192 keys: 4224 keys
 // 377 us, 2112 keys 359).
 constexpr int kPagedFillWgs = 256, kPagedChunk = 1024, kPagedMostWgs = 2048;
+// More sequences than this fill the chip by themselves and are never split: every workgroup of a split call looks at all
+// lengths.
+constexpr int kPagedSplitBatch = 2048;
 // Caches up to this many keys are never split: a join takes longer (192 keys: 4.2 us whole, 7.7 split).
 constexpr int kPagedWhole = 256;
 

@@ -604,7 +604,7 @@ PagedPlan plan_paged(const traj_paged_shape* sh) {
     const auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
     const int64_t most = std::max(up(kPagedFillWgs, units), std::min(up(kPagedMostWgs, units), sh->B * up(cap, kPagedChunk)));
     p.slots = std::min<int64_t>(most + sh->B, sh->B * up(cap, kPagedGranule));
-    p.workspace = cap <= kPagedWhole ? 0 : (size_t)p.slots * (size_t)units * p.tile_rows * (sh->D + 2) * sizeof(float) + (size_t)sh->B * sizeof(int2);
+    p.workspace = cap <= kPagedWhole || sh->B > kPagedSplitBatch ? 0 : (size_t)p.slots * (size_t)units * p.tile_rows * (sh->D + 2) * sizeof(float) + (size_t)sh->B * sizeof(int2);
     return p;
 }
 

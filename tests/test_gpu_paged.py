@@ -208,7 +208,7 @@ def test_attention_unsplit_and_in_a_larger_workspace_agree():
     import ctypes
     from paper_2608_27514_amd import _lib
     q, kp, vp, table, lens = t
-    sh = _lib._paged_struct(*_lib._paged_sizes(2, 2, 8, kp, vp, table))[0]
+    sh = _lib._paged_struct(*_lib._paged_sizes(2, 2, 8, kp, vp, table, 0))[0]
     whole = torch.empty_like(q)
     ptr = [x.data_ptr() for x in (q, kp, vp, table, lens, whole)]
     assert lib.traj_paged_attn(*ptr, ctypes.byref(sh), 0.0, 0, None, 0, torch.cuda.current_stream().cuda_stream) == 0
