@@ -461,8 +461,8 @@ traj_status traj_paged_append(const void* q, int64_t q_stride, const void* k, in
 /* Attention of T new tokens per sequence over its cached keys (its own, once appended, among them):
  *     out[b,t,h,:] = softmax_s( scale * q[b,t,h,:] . key_s ) * value_s,   g = h / (Hq / Hkv),
  * over s < lens[b], or with causal != 0 over s < lens[b] - T + t + 1 (the new tokens are the sequence's
- * last T).  A row that sees no key is 0.  Softmax and accumulation in fp32, weights rounded to bf16 for the
- * matrix product, out rounded to bf16.  q, out: [B, T, Hq, D] bf16, contiguous, 16-byte aligned; out must
+ * last T).  A row that sees no key is 0.  Softmax and accumulation in fp32; for the matrix product the weights
+ * are rounded to 16 bits where T * Hq / Hkv <= 32, else to bf16 (8 bits); out rounded to bf16.  q, out: [B, T, Hq, D] bf16, contiguous, 16-byte aligned; out must
  * not overlap any input.
  * lens [B] int32 (device); a length outside [0, max_pages * page_size] is clamped (TRAJ_DEV_BAD_LENGTH),
  * keys of a page outside the pool are not visible (TRAJ_DEV_BAD_PAGE).  Rows of a page behind lens[b]

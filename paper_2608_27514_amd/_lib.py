@@ -621,13 +621,14 @@ def _paged_workspace(*sizes):
 
 def _paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev):
     """Checks the pools and the table; returns what :func:`_paged_struct` takes."""
-    bf16 = torch.bfloat16
-    for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages"), (page_table, "page_table")):
-        _here(t, n, dev)
-    if k_pages.dtype is not bf16 or v_pages.dtype is not bf16:
-        raise TypeError(f"k_pages and v_pages must be {bf16}")
-    if page_table.dtype is not torch.int32:
-        raise TypeError("page_table must be torch.int32")
+    tensor, bf16 = torch.Tensor, torch.bfloat16
+    if not (isinstance(k_pages, tensor) and k_pages.dtype is bf16 and k_pages.get_device() == dev and isinstance(v_pages, tensor)
+            and v_pages.dtype is bf16 and v_pages.get_device() == dev and isinstance(page_table, tensor)
+            and page_table.dtype is torch.int32 and page_table.get_device() == dev):
+        for t, n, dt in ((k_pages, "k_pages", bf16), (v_pages, "v_pages", bf16), (page_table, "page_table", torch.int32)):
+            _here(t, n, dev)
+            if t.dtype is not dt:
+                raise TypeError(f"{n} must be {dt}, got {t.dtype}")
     pages, strides = k_pages.shape, k_pages.stride()
     if v_pages.shape != pages or v_pages.stride() != strides:
         raise ValueError("k_pages and v_pages must have the same shape and strides")
@@ -636,10 +637,10 @@ def _paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev):
 
 def _token_rows(t, name, shape, dev):
     """Checks a [B, T, heads, D] tensor whose token rows hold their heads side by side; returns (address, row stride)."""
-    _here(t, name, dev)
-    if t.dtype is not torch.bfloat16:
-        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
-    if t.shape != shape:
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.get_device() == dev and t.shape == shape):
+        _here(t, name, dev)
+        if t.dtype is not torch.bfloat16:
+            raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
         _expect_shape(t, name, shape)
     B, T, heads, D = shape
     sb, st, sh, sd = t.stride()
@@ -733,9 +734,8 @@ def _logit_adjust(dev, R, V, per, history, history_len, repetition, frequency, p
     if history is not None:
         H = history.shape[-1]
         hp = _arg(history, "history", i32, (n, H), dev)
-    for name, t in (("history_len", history_len), ("repetition", repetition), ("frequency", frequency), ("presence", presence)):
-        if t is not None and history is None:
-            raise ValueError(f"{name} needs history")
+    elif not (history_len is None and repetition is None and frequency is None and presence is None):
+        raise ValueError("history_len, repetition, frequency and presence need history")
     if history_len is not None:
         lp = _arg(history_len, "history_len", i32, (n,), dev)
     if repetition is not None:
