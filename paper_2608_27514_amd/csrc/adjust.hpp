@@ -10,6 +10,8 @@
 // ones by their records.  So the stream's cost does not depend on the lists, and every sum runs in a fixed order.
 #pragma once
 
+#include <algorithm>
+
 #include "conf_topk.hpp"
 #include "layer.hpp"
 
@@ -612,9 +614,20 @@ inline int adjust_window(int groups, int max_records) {
 
 // Launch shape: threads per row slice and its register ring, slices per row (as plan_conf_topk; one wave per row
 // would hold the allowed bits of a row per wave in LDS, so rows take 4 waves at least).
+constexpr int64_t kAdjustFewRows = 64, kAdjustSlices = 256;
 inline TopkPlan plan_adjust(int64_t rows, int64_t vocab, int vec) {
     TopkPlan p = plan_conf_topk(rows, vocab, vec);
     if (p.threads == 64) p = TopkPlan{256, 2, 2, 1, (int)vocab};
+    // Few rows that are split are split further, down to two vectors per lane: a slice is a chain of latencies beside its
+    // stream (1 row of 126464 16.3 -> 15.4 us, 32 rows 20.1 -> 17.7; 100 rows 31.6 against 32.4, so not those; rows
+    // that one workgroup takes in four vectors per lane stay whole, 5 of 9000 12.0 against 13.8).
+    if (p.splits > 1 && rows <= kAdjustFewRows) {
+        const int64_t align = (int64_t)p.threads * vec;
+        int64_t splits = std::min<int64_t>((kAdjustSlices + rows - 1) / rows, (vocab + 2 * align - 1) / (2 * align));
+        splits = std::min<int64_t>(splits, 64);
+        p.chunk = (int)(((vocab + splits - 1) / splits + align - 1) / align * align);
+        p.splits = (int)((vocab + p.chunk - 1) / p.chunk);
+    }
     return p;
 }
 
