@@ -460,13 +460,15 @@ traj_status traj_paged_append(const void* q, int64_t q_stride, const void* k, in
 
 /* Attention of T new tokens per sequence over its cached keys (its own, once appended, among them):
  *     out[b,t,h,:] = softmax_s( scale * q[b,t,h,:] . key_s ) * value_s,   g = h / (Hq / Hkv),
- * over s < lens[b], or with causal != 0 over s < lens[b] - T + t + 1 (the new tokens are the sequence's
- * last T).  A row that sees no key is 0.  Softmax and accumulation in fp32; for the matrix product the weights
- * are rounded to 16 bits where T * Hq / Hkv <= 32, else to bf16 (8 bits); out rounded to bf16.  q, out: [B, T, Hq, D] bf16, contiguous, 16-byte aligned; out must
- * not overlap any input.
+ * over s < lens[b], or with causal != 0 over s < lens[b] - n_new[b] + t + 1 (the new tokens are the
+ * sequence's last n_new[b]; n_new NULL: T).  A row that sees no key is 0, and so are the padding rows
+ * t >= n_new[b], whose q may hold anything.  Softmax and accumulation in fp32; for the matrix product
+ * the weights are rounded to 16 bits where T * Hq / Hkv <= 32, else to bf16 (8 bits); out rounded to
+ * bf16.  q, out: [B, T, Hq, D] bf16, contiguous, 16-byte aligned; out must not overlap any input.
  * lens [B] int32 (device); a length outside [0, max_pages * page_size] is clamped (TRAJ_DEV_BAD_LENGTH),
- * keys of a page outside the pool are not visible (TRAJ_DEV_BAD_PAGE).  Rows of a page behind lens[b]
- * may hold anything.  scale <= 0 selects 1/sqrt(D).
+ * keys of a page outside the pool are not visible (TRAJ_DEV_BAD_PAGE); n_new[b] outside [0, T] is clamped
+ * (TRAJ_DEV_BAD_LENGTH).  Rows of a page behind lens[b] may hold anything; those before it are finite (a
+ * value that only causality hides from a row still has weight 0 in its sum).  scale <= 0 selects 1/sqrt(D).
  * workspace: traj_paged_attn_workspace_size() bytes, 16-byte aligned, for the partial results of
  * sequences whose keys are split over workgroups (0: the shape is never split).  With NULL nothing is
  * split.  Calls that may run at the same time (graphs among them) need workspaces of their own.
@@ -474,8 +476,8 @@ traj_status traj_paged_append(const void* q, int64_t q_stride, const void* k, in
 size_t traj_paged_attn_workspace_size(const traj_paged_shape* shape);
 
 traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table,
-                            const int32_t* lens, void* out, const traj_paged_shape* shape, float scale,
-                            int32_t causal, void* workspace, size_t workspace_bytes, void* stream);
+                            const int32_t* lens, const int32_t* n_new, void* out, const traj_paged_shape* shape,
+                            float scale, int32_t causal, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------
  * 8. Confidence and candidates of adjusted logits

@@ -37,7 +37,7 @@ def paged_append(q, k, v, k_pages, v_pages, page_table, start, n_new=None, pos0=
     return out, k_pages, v_pages
 
 
-def paged_attention(q, k_pages, v_pages, page_table, lens, causal=False, scale=None):
+def paged_attention(q, k_pages, v_pages, page_table, lens, causal=False, scale=None, n_new=None):
     """Returns (out, weight) [B, T, Hq, D]: the attention and the same sums over |v| (what rounding the weights can move)."""
     B, T, Hq, D = q.shape
     pages, ps, Hkv = k_pages.shape[:3]
@@ -45,13 +45,14 @@ def paged_attention(q, k_pages, v_pages, page_table, lens, causal=False, scale=N
     out, weight = np.zeros(q.shape), np.zeros(q.shape)
     for b in range(B):
         n = min(max(int(lens[b]), 0), page_table.shape[1] * ps)
+        new = T if n_new is None else min(max(int(n_new[b]), 0), T)
         s = np.arange(n)
         page = page_table[b, s // ps]
         good = (page >= 0) & (page < pages)
         s, page = s[good], page[good]
         k, v = k_pages[page, s % ps], v_pages[page, s % ps]
-        for t in range(T):
-            seen = s < n - T + t + 1 if causal else np.ones(len(s), bool)
+        for t in range(new):
+            seen = s < n - new + t + 1 if causal else np.ones(len(s), bool)
             if not seen.any():
                 continue
             for h in range(Hq):

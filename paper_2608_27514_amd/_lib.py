@@ -129,7 +129,7 @@ EXPORTS = {
     "traj_paged_append": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p] * 7 +
                           [ctypes.POINTER(PagedShape), ctypes.c_float, ctypes.c_void_p]),
     "traj_paged_attn_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(PagedShape)]),
-    "traj_paged_attn": (ctypes.c_int32, [ctypes.c_void_p] * 6 + [ctypes.POINTER(PagedShape), ctypes.c_float, ctypes.c_int32,
+    "traj_paged_attn": (ctypes.c_int32, [ctypes.c_void_p] * 7 + [ctypes.POINTER(PagedShape), ctypes.c_float, ctypes.c_int32,
                                                                  ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "traj_confidence_topk_adjusted_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(LogitsShape), ctypes.c_int32,
                                                                        ctypes.POINTER(LogitAdjust)]),
@@ -694,10 +694,11 @@ def paged_attn_workspace_size(q, k_pages, v_pages, page_table):
     return _paged_workspace(*_paged_sizes(*q.shape[:3], k_pages, v_pages, page_table, _current()))
 
 
-def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causal=False, workspace=None, stream=None):
+def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causal=False, n_new=None, workspace=None, stream=None):
     """Attention of T new tokens per sequence, q [B,T,Hq,D] (bf16), over the first lens[b] cached keys of each
-    (causal: the new tokens are the last T of them and see those up to themselves).  Pages and table as
-    :func:`paged_append`; lens [B] int32.  Returns ``out`` [B,T,Hq,D]; a row that sees no key is zero."""
+    (causal: the new tokens are the last n_new[b] of them and see those up to themselves).  Pages and table as
+    :func:`paged_append`; lens and n_new (None: T each) [B] int32.  Returns ``out`` [B,T,Hq,D]; a row that sees no key
+    and the padding rows t >= n_new[b] are zero."""
     shape = B, T, Hq, D = q.shape
     bf16 = torch.bfloat16
     dev = _current()
@@ -717,7 +718,7 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causa
     else:
         ws, ws_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
     st = _lib().traj_paged_attn(qp, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), _arg(lens, "lens", torch.int32, (B,), dev),
-                                _arg(out, "out", bf16, shape, dev), ref, scale, 1 if causal else 0, ws, ws_bytes, _stream(stream))
+                                None if n_new is None else _arg(n_new, "n_new", torch.int32, (B,), dev), _arg(out, "out", bf16, shape, dev), ref, scale, 1 if causal else 0, ws, ws_bytes, _stream(stream))
     if st != TRAJ_OK:
         _check(st, "traj_paged_attn")
     return out

@@ -160,7 +160,7 @@ constexpr int kPagedWhole = 256;
 struct PagedAttnParams {
     const uint16_t* q;
     PagedCache cache;
-    const int32_t* lens;
+    const int32_t *lens, *n_new;  // [B]; n_new null: T
     uint16_t* out;
     float *part_o, *part_ml;  // partial results per (slot, unit, row): D values; maximum and sum
     int2* ranges;             // [B] number of ranges, first slot
@@ -182,6 +182,17 @@ __device__ __forceinline__ int paged_length(const PagedAttnParams& P, int b, boo
         return len < 0 ? 0 : P.cache.capacity;
     }
     return len;
+}
+
+// New tokens of a sequence; the rows behind them are padding.
+__device__ __forceinline__ int paged_new(const PagedAttnParams& P, int b, bool report) {
+    if (P.n_new == nullptr) return P.T;
+    const int n = P.n_new[b];
+    if (n < 0 || n > P.T) {
+        if (report) flag_device_status(kDevBadLength);
+        return n < 0 ? 0 : P.T;
+    }
+    return n;
 }
 
 // Keys per workgroup.  Every wave computes the same from the same lengths (whole numbers, quotients by powers of two).
@@ -327,13 +338,13 @@ struct PagedRows {
     f32x4_t o[NR][D / 16];       // O^T: head dims 16 db + 4 (lane / 16) ..
     float m[NR], neg_mc[NR], lsum[NR];  // the reference is the maximum itself: the largest weight is 1 and exact in bf16
 
-    __device__ __forceinline__ void init(const PagedAttnParams& P, int b, int g, int len, int row0) {
+    __device__ __forceinline__ void init(const PagedAttnParams& P, int b, int g, int len, int n_new, int row0) {
         const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int f = 0; f < NR; ++f) {
             const int row = min(row0 + 16 * f + (lane & 15), P.rows - 1);  // rows past the last repeat it and are not stored
             const int t = P.by_group.div(row), h = g * P.group + row - t * P.group;
-            limit[f] = P.causal ? len - P.T + t + 1 : len;
+            limit[f] = P.causal ? len - n_new + t + 1 : len;
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks)
                 qf[f][ks] = __builtin_bit_cast(bf16x8_t, ldg16(P.q + (((int64_t)b * P.T + t) * P.Hq + h) * D + 32 * ks + 8 * (lane >> 4)));
@@ -462,7 +473,7 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams& P) {
 // Joins the SETS states of each of a workgroup's ROWS rows and writes the result, or its part of a sequence in several
 // ranges.
 template <int D, int ROWS, int SETS>
-__device__ __forceinline__ void paged_store(const PagedAttnParams& P, const PagedRange& r, const PagedPlace& w, const float* buf,
+__device__ __forceinline__ void paged_store(const PagedAttnParams& P, const PagedRange& r, const PagedPlace& w, int n_new, const float* buf,
                                             const float* sm, const float* sl) {
     constexpr int kRow = PagedLds<D>::kMergeRow, LPR = D / 4, STEP = kPagedThreads / LPR;
     const int d = 4 * (threadIdx.x % LPR), first = threadIdx.x / LPR;
@@ -482,9 +493,14 @@ __device__ __forceinline__ void paged_store(const PagedAttnParams& P, const Page
             l += scale * sl[e * ROWS + rr];
             acc += scale * *reinterpret_cast<const f32x4_t*>(buf + (e * ROWS + rr) * kRow + d);
         }
+        const int t = P.by_group.div(qrow), h = w.g * P.group + qrow - t * P.group;
+        if (t >= n_new) {  // padding, whose query may hold anything
+            M = kNegInf;
+            l = 0.f;
+            acc = f32x4_t{};
+        }
         if (r.n == 1) {
             const float inv = l > 0.f ? 1.0f / l : 0.f;  // a row that sees nothing: 0
-            const int t = P.by_group.div(qrow), h = w.g * P.group + qrow - t * P.group;
             u32x2_t x;
             x[0] = (uint32_t)f2bf(acc[0] * inv) | ((uint32_t)f2bf(acc[1] * inv) << 16);
             x[1] = (uint32_t)f2bf(acc[2] * inv) | ((uint32_t)f2bf(acc[3] * inv) << 16);
@@ -514,7 +530,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnP
     if (!paged_range(P, w.slot, blockIdx.x == 0, r)) return;
     const int len = r.len;
     const int begin = r.split * r.chunk, end = len - begin > r.chunk ? begin + r.chunk : len;
-    const int min_limit = P.causal ? len - P.T + 1 : len;
+    const int n_new = paged_new(P, r.b, w.unit == 0 && r.split == 0 && threadIdx.x == 0);
+    const int min_limit = P.causal ? len - n_new + 1 : len;  // of a row that is not padding
 
     // one LDS tile per wave, K's and then V's
     uint16_t* tile = reinterpret_cast<uint16_t*>(lds + wave * kTileBytes);
@@ -580,7 +597,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnP
         p1 = fetch(DEPTH - 1);
         pages = fetch(DEPTH);
     }
-    st.init(P, r.b, w.g, len, w.row_tile * ROWS);
+    st.init(P, r.b, w.g, len, n_new, w.row_tile * ROWS);
     int left = first < end ? (end - first + kPagedGranule - 1) / kPagedGranule : 0;  // tiles of this wave
     if (left > 0) {
         using Slot0 = std::integral_constant<int, 0>;
@@ -624,7 +641,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnP
     float* buf = reinterpret_cast<float*>(lds);
     st.leave(buf + wave * ROWS * L::kMergeRow, sh_m + wave * ROWS, sh_l + wave * ROWS);
     __syncthreads();
-    paged_store<D, ROWS, kPagedWaves>(P, r, w, buf, sh_m, sh_l);
+    paged_store<D, ROWS, kPagedWaves>(P, r, w, n_new, buf, sh_m, sh_l);
 }
 
 // More rows: RW waves of 32 rows each share the stages of 16 RW keys that they load into LDS together (a stage's K and
@@ -650,7 +667,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedAttnP
     if (!paged_range(P, w.slot, blockIdx.x == 0, r)) return;
     const int len = r.len;
     const int begin = r.split * r.chunk, end = len - begin > r.chunk ? begin + r.chunk : len;
-    const int min_limit = P.causal ? len - P.T + 1 : len;
+    const int n_new = paged_new(P, r.b, w.unit == 0 && r.split == 0 && threadIdx.x == 0);
+    const int min_limit = P.causal ? len - n_new + 1 : len;  // of a row that is not padding
 
     uint16_t* stage = reinterpret_cast<uint16_t*>(lds) + kg * 2 * kStage;  // two of them, K rows then V rows
     const int vrow = lane / (D / 8), vchunk = lane % (D / 8);
@@ -689,7 +707,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedAttnP
     };
     PagedRows<D, NR> st;
     if (rounds > 0) fetch(0);
-    st.init(P, r.b, w.g, len, w.row_tile * ROWS + 32 * rw);
+    st.init(P, r.b, w.g, len, n_new, w.row_tile * ROWS + 32 * rw);
     if (rounds > 0) {
         request(0);
         put(0);
@@ -724,7 +742,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedAttnP
     const int set = kg * ROWS + 32 * rw;
     st.leave(buf + set * L::kMergeRow, sh_m + set, sh_l + set);
     __syncthreads();
-    paged_store<D, ROWS, KW>(P, r, w, buf, sh_m, sh_l);
+    paged_store<D, ROWS, KW>(P, r, w, n_new, buf, sh_m, sh_l);
 }
 
 // THREADS threads per (sequence, new token, query head): each range by D / 4 lanes, THREADS * 4 / D ranges at a time,

@@ -1026,7 +1026,7 @@ size_t traj_paged_attn_workspace_size(const traj_paged_shape* shape) {
 }
 
 traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table, const int32_t* lens,
-                            void* out, const traj_paged_shape* shape, float scale, int32_t causal, void* workspace,
+                            const int32_t* n_new, void* out, const traj_paged_shape* shape, float scale, int32_t causal, void* workspace,
                             size_t workspace_bytes, void* stream) {
     if (shape == nullptr) return TRAJ_E_NULL;
     const traj_status st = check_paged(shape);
@@ -1041,6 +1041,7 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
     p.q = static_cast<const uint16_t*>(q);
     p.cache = paged_cache(shape, k_pages, v_pages, page_table);
     p.lens = lens;
+    p.n_new = n_new;
     p.out = static_cast<uint16_t*>(out);
     p.B = shape->B;
     p.T = shape->T;

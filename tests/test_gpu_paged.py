@@ -186,6 +186,53 @@ def test_attention_parity(T, Hq, Hkv, D, ps, lens, causal):
     attend(np.random.default_rng(T + ps), len(lens), T, Hq, Hkv, D, ps, lens, causal)
 
 
+PADDED = [
+    # T, Hq, Hkv, D, page_size, cached before, n_new: each kernel, in one range and in several
+    (7, 4, 2, 128, 16, [0, 20, 33, 0], [7, 0, 3, 1]),
+    (7, 4, 2, 64, 5, [4000, 20, 133, 2], [7, 0, 3, 6]),
+    (13, 4, 2, 128, 32, [3000, 0], [13, 4]),
+    (32, 2, 1, 128, 16, [100, 2500, 0], [0, 17, 32]),
+    (70, 8, 2, 64, 48, [0, 1200, 31], [69, 70, 1]),
+    (70, 8, 2, 128, 20, [5, 0], [33, 2]),
+]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("T,Hq,Hkv,D,ps,before,n_new", PADDED)
+def test_appended_and_attended_in_a_padded_batch(T, Hq, Hkv, D, ps, before, n_new, causal):
+    """Padding is NaN in q, k and v, and pages behind a sequence's last token are not in the table."""
+    rng = np.random.default_rng(T + Hq + ps)
+    B = len(before)
+    lens = np.add(before, n_new)
+    table, pages = make_table(rng, B, -(-int(lens.max()) // ps))
+    kp, vp = np.full((pages, ps, Hkv, D), np.nan), np.full((pages, ps, Hkv, D), np.nan)
+    for b in range(B):
+        s = np.arange(before[b])
+        kp[table[b, s // ps], s % ps], vp[table[b, s // ps], s % ps] = normal(rng, before[b], Hkv, D), normal(rng, before[b], Hkv, D)
+        table[b, -(-lens[b] // ps):] = -1
+    q, k, v = normal(rng, B, T, Hq, D), normal(rng, B, T, Hkv, D), normal(rng, B, T, Hkv, D)
+    for b in range(B):
+        for x in (q, k, v):
+            x[b, n_new[b]:] = np.nan
+    pools, new = (bf(kp), bf(vp)), i32(n_new)
+    tsp.paged_append(bf(k), bf(v), *pools, i32(table), i32(before), n_new=new, rope_theta=0.0)
+    _, kp, vp = oracle.paged_append(None, k, v, kp, vp, table, before, n_new, theta=0)
+    ref, weight = oracle.paged_attention(q, kp, vp, table, lens, causal, n_new=n_new)
+    out = f64(tsp.paged_attn(bf(q), *pools, i32(table), i32(lens), causal=causal, n_new=new))
+    assert tsp.device_status() == 0
+    assert (np.abs(out - ref) <= (HALF_STEP + 2.0 ** -10) * weight + HALF_STEP * np.abs(ref) + 1e-30).all()
+    for b in range(B):
+        assert (out[b, n_new[b]:] == 0).all()
+
+
+def test_attention_clamps_the_number_of_new_tokens():
+    rng = np.random.default_rng(12)
+    t, _ = attend(rng, 3, 4, 2, 1, 64, 16, [30, 300, 9], True)
+    out = tsp.paged_attn(*t, causal=True, n_new=i32([5, 4, -1]))
+    assert tsp.device_status() == tsp.DEV_BAD_LENGTH
+    assert torch.equal(out, tsp.paged_attn(*t, causal=True, n_new=i32([4, 4, 0]))) and tsp.device_status() == 0
+
+
 def test_attention_over_pages_of_heads_and_other_scales():
     rng = np.random.default_rng(8)
     for layout, ps in ((heads_first, 16), (heads_first, 20)):
@@ -210,7 +257,7 @@ def test_attention_unsplit_and_in_a_larger_workspace_agree():
     q, kp, vp, table, lens = t
     sh = _lib._paged_struct(*_lib._paged_sizes(2, 2, 8, kp, vp, table, 0))[0]
     whole = torch.empty_like(q)
-    ptr = [x.data_ptr() for x in (q, kp, vp, table, lens, whole)]
+    ptr = [x.data_ptr() for x in (q, kp, vp, table, lens)] + [None, whole.data_ptr()]
     assert lib.traj_paged_attn(*ptr, ctypes.byref(sh), 0.0, 0, None, 0, torch.cuda.current_stream().cuda_stream) == 0
     # both within half a step of the weights' rounding (of values near 1: some 2^-7) and of their own
     assert (whole.float() - out.float()).abs().max().item() <= 2.0 ** -6

@@ -35,7 +35,7 @@ def append(sh=None, theta=1e4, **kw):
 
 def attn(sh=None, scale=0.0, ws=None, ws_bytes=0, **kw):
     sh = sh or shape()
-    a = dict(q=FAKE, kp=FAKE, vp=FAKE, table=FAKE, lens=FAKE, out=FAKE)
+    a = dict(q=FAKE, kp=FAKE, vp=FAKE, table=FAKE, lens=FAKE, n=None, out=FAKE)
     a.update(kw)
     return _lib.load().traj_paged_attn(*a.values(), ctypes.byref(sh), scale, 0, ws, ws_bytes, None)
 
@@ -49,7 +49,7 @@ def test_paged_shapes():
         assert append(shape(**bad)) == UNSUPPORTED and attn(shape(**bad)) == UNSUPPORTED
     for none in (dict(B=0), dict(T=0)):
         assert append(shape(**none), k=None) == 0 and attn(shape(**none), q=None) == 0
-    assert _lib.load().traj_paged_attn(*[FAKE] * 6, None, 0.0, 0, None, 0, None) == NULL
+    assert _lib.load().traj_paged_attn(*[FAKE] * 7, None, 0.0, 0, None, 0, None) == NULL
 
 
 def test_append_arguments():
