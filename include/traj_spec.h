@@ -429,8 +429,8 @@ traj_status traj_linear(const void* x, const void* w, void* y, int64_t M, int64_
  * both serve, and a contiguous cache [B, S, Hkv, D] is a pool of B pages of S tokens.
  * page_table: int32, max_pages columns, table_stride elements from row to row; entries behind a
  * sequence's last page are never read.  Sequences may share pages that neither writes.
- * Limits (all entry points): B >= 0 and T >= 0 (0 = no-op) with B <= 65535; D in {64, 128};
- *   Hq % Hkv == 0; num_pages, page_size, max_pages >= 1 with max_pages * page_size < 2^31 - 256;
+ * Limits (all entry points): B >= 0 and T >= 0 (0 = no-op) with B <= 65535, T <= 2^24; D in {64, 128};
+ *   Hq % Hkv == 0; num_pages, page_size, max_pages >= 1 with max_pages * page_size <= 2^31 - 4096;
  *   strides positive multiples of 8 with token_stride <= 2^25; pools and q / k / v rows 16-byte
  *   aligned; table_stride >= max_pages.
  * ------------------------------------------------------------------------------------ */
@@ -496,11 +496,13 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
  * -inf), mask [n_masks, mask_stride] uint32, mask_index [rows] int32 (NULL: m = r; -1: every token is allowed;
  * any other value outside [0, n_masks): none is, TRAJ_DEV_BAD_MASK); n_seq = ceil(rows / rows_per_seq).
  * history_size == 0 / bias_size == 0 / mask == NULL leave that part out.
- * Limits: those of traj_confidence_topk; vocab <= 2^19 (else TRAJ_E_UNSUPPORTED); rows_per_seq >= 1;
+ * Limits: those of traj_confidence_topk; rows < 2^24, sequences with lists < 2^22; vocab <= 2^19 (else
+ *   TRAJ_E_UNSUPPORTED); rows_per_seq >= 1;
  *   history_size, bias_size >= 0, their sum < 2^30; mask_stride >= ceil(vocab / 32); without mask_index
  *   n_masks >= rows.
  * workspace: traj_confidence_topk_adjusted_workspace_size() bytes, 16-byte aligned; one sized for more rows
- * of the same kind serves too.  TRAJ_E_WORKSPACE where the sequences' records don't fit.
+ * of the same kind serves too.  TRAJ_E_WORKSPACE where the sequences' records don't fit; where only the split
+ * records don't, rows are not split, so one for several numbers of rows takes the largest of their sizes.
  * ------------------------------------------------------------------------------------ */
 typedef struct {
     int32_t rows_per_seq;

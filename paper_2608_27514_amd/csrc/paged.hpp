@@ -154,6 +154,8 @@ constexpr int kPagedFillWgs = 256, kPagedChunk = 1024, kPagedMostWgs = 2048;
 // More sequences than this fill the chip by themselves and are never split: every workgroup of a split call looks at all
 // lengths.
 constexpr int kPagedSplitBatch = 2048;
+// Nor are batches of so many query rows, of which a wave each would not go into the joining launch.
+constexpr int64_t kPagedSplitRows = 1 << 26;
 // Caches up to this many keys are never split: a join takes longer (192 keys: 4.2 us whole, 7.7 split).
 constexpr int kPagedWhole = 256;
 

@@ -550,10 +550,14 @@ traj_status run_layer(uint16_t* xs, const traj_layer_weights* w, const traj_laye
 }
 
 // ------------------------------------------------------------------ paged cache
+// Workgroups of 256 threads that a launch can have: 2^32 threads at most.
+constexpr int64_t kMostWgs = (1 << 24) - 1;
+
 traj_status check_paged(const traj_paged_shape* sh) {
-    if (sh->B < 0 || sh->B > 65535 || sh->T < 0 || sh->Hq < 1 || sh->Hkv < 1 || sh->Hq % sh->Hkv != 0) return TRAJ_E_SHAPE;
+    if (sh->B < 0 || sh->B > 65535 || sh->T < 0 || sh->T > (1 << 24) || sh->Hq < 1 || sh->Hkv < 1 || sh->Hq % sh->Hkv != 0) return TRAJ_E_SHAPE;
     if (sh->num_pages < 1 || sh->page_size < 1 || sh->max_pages < 1) return TRAJ_E_SHAPE;
-    if ((int64_t)sh->max_pages * sh->page_size >= (1ll << 31) - 256 || sh->table_stride < sh->max_pages) return TRAJ_E_SHAPE;
+    // keys past the last one are numbered too, up to a few tiles
+    if ((int64_t)sh->max_pages * sh->page_size > (1ll << 31) - 4096 || sh->table_stride < sh->max_pages) return TRAJ_E_SHAPE;
     for (int64_t s : {sh->page_stride, sh->token_stride, sh->head_stride})
         if (s < 8 || s % 8 != 0 || s > (1ll << 40)) return TRAJ_E_SHAPE;
     if ((int64_t)sh->T * (sh->Hq / sh->Hkv) > (1 << 30) || sh->table_stride > (1ll << 40)) return TRAJ_E_SHAPE;
@@ -604,7 +608,8 @@ PagedPlan plan_paged(const traj_paged_shape* sh) {
     const auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
     const int64_t most = std::max(up(kPagedFillWgs, units), std::min(up(kPagedMostWgs, units), sh->B * up(cap, kPagedChunk)));
     p.slots = std::min<int64_t>(most + sh->B, sh->B * up(cap, kPagedGranule));
-    p.workspace = cap <= kPagedWhole || sh->B > kPagedSplitBatch ? 0 : (size_t)p.slots * (size_t)units * p.tile_rows * (sh->D + 2) * sizeof(float) + (size_t)sh->B * sizeof(int2);
+    const bool whole = cap <= kPagedWhole || sh->B > kPagedSplitBatch || (int64_t)sh->B * sh->T * sh->Hq >= kPagedSplitRows;
+    p.workspace = whole ? 0 : (size_t)p.slots * (size_t)units * p.tile_rows * (sh->D + 2) * sizeof(float) + (size_t)sh->B * sizeof(int2);
     return p;
 }
 
@@ -645,6 +650,9 @@ traj_status check_adjust(const traj_logits_shape* sh, int32_t k, const traj_logi
     if (a->mask != nullptr && (a->n_masks < 1 || a->mask_stride < (sh->vocab + 31) / 32 || a->mask_stride > (1ll << 40) ||
                                (a->mask_index == nullptr && a->n_masks < sh->rows)))
         return TRAJ_E_SHAPE;
+    // a launch has fewer than 2^32 threads: 256 per row, 1024 per sequence with lists
+    if (sh->rows > kMostWgs) return TRAJ_E_SHAPE;
+    if (a->history_size + a->bias_size > 0 && (sh->rows + a->rows_per_seq - 1) / a->rows_per_seq > kMostWgs / 4) return TRAJ_E_SHAPE;
     return TRAJ_OK;
 }
 
@@ -1058,7 +1066,7 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
     p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)shape->D)) * 1.4426950408889634f;
     const int64_t slots = p.single ? p.B : plan.slots;
     const int64_t wgs = (slots * shape->Hkv + 7) / 8 * 8 * plan.tiles;
-    if (wgs > INT_MAX || (int64_t)p.B * p.T * p.Hq > INT_MAX) return TRAJ_E_SHAPE;
+    if (wgs > kMostWgs || (int64_t)p.B * p.T * p.Hq > INT_MAX) return TRAJ_E_SHAPE;
     p.part_o = static_cast<float*>(workspace);
     p.part_ml = p.part_o + (p.single ? 0 : (size_t)plan.slots * p.units * p.tile_rows * shape->D);
     p.ranges = reinterpret_cast<int2*>(p.part_ml + (p.single ? 0 : (size_t)plan.slots * p.units * p.tile_rows * 2));

@@ -22,7 +22,8 @@ def shape(**kw):
 
 
 BAD_SHAPES = [dict(B=-1), dict(B=65536), dict(T=-1), dict(Hq=0), dict(Hkv=0), dict(Hkv=3), dict(num_pages=0), dict(page_size=0), dict(max_pages=0),
-              dict(max_pages=1 << 20, page_size=1 << 11, table_stride=1 << 20), dict(table_stride=3), dict(page_stride=12), dict(token_stride=0),
+              dict(max_pages=1 << 20, page_size=1 << 11, table_stride=1 << 20), dict(T=(1 << 24) + 1),
+              dict(max_pages=(1 << 31) - 4095, page_size=1, table_stride=1 << 31), dict(table_stride=3), dict(page_stride=12), dict(token_stride=0),
               dict(head_stride=-8), dict(T=1 << 30)]
 
 
@@ -69,6 +70,10 @@ def test_attention_arguments():
     for name in ("q", "kp", "vp", "out"):
         assert attn(**{name: ODD}) == SHAPE, name
     assert attn(scale=float("nan")) == ARG and attn(scale=float("inf")) == ARG
+    # more workgroups than a launch can have
+    assert attn(shape(B=65535, T=16, Hq=512, Hkv=512)) == SHAPE
+    # many rows fill the chip unsplit
+    assert _lib.load().traj_paged_attn_workspace_size(ctypes.byref(shape(B=1024, T=8192, max_pages=4096, table_stride=4096))) == 0
     long = shape(max_pages=4096, table_stride=4096)
     need = _lib.load().traj_paged_attn_workspace_size(ctypes.byref(long))
     assert need > 0
@@ -119,6 +124,8 @@ def test_adjusted_arguments():
     assert adjust(history_size=4) == NULL
     assert adjust(bias_size=4, bias_ids=FAKE) == NULL and adjust(bias_size=4, bias=FAKE) == NULL
     assert adjust(history_size=4, history=FAKE) == WORKSPACE
+    assert adjust(L(1 << 24, 1000, 1000, 0)) == SHAPE
+    assert adjust(L(1 << 22, 1000, 1000, 0), rows_per_seq=1, history_size=4, history=FAKE) == SHAPE
     assert adjust(L(0, 1000, 1000, 0), logits=None, history_size=4) == 0
     lib = _lib.load()
     one = _lib.LogitAdjust(rows_per_seq=8, history_size=4)
