@@ -601,6 +601,14 @@ def _arg(t, name, dtype, shape, dev):
     return p
 
 
+def _room(workspace, dev):
+    """A caller's workspace as (address, bytes)."""
+    _here(workspace, "workspace", dev)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
 @functools.lru_cache(maxsize=1024)
 def _paged_struct(B, T, Hq, pages, strides, table, table_strides):
     """The C shape of a paged call, by sizes and strides alone: (structure, reference to it)."""
@@ -716,7 +724,7 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causa
             workspace = _empty((ws_bytes,), torch.uint8, q.device, stream)
             ws = workspace.data_ptr()
     else:
-        ws, ws_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
+        ws, ws_bytes = _room(workspace, dev)
     st = _lib().traj_paged_attn(qp, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), _arg(lens, "lens", torch.int32, (B,), dev),
                                 None if n_new is None else _arg(n_new, "n_new", torch.int32, (B,), dev), _arg(out, "out", bf16, shape, dev), ref, scale, 1 if causal else 0, ws, ws_bytes, _stream(stream))
     if st != TRAJ_OK:
@@ -815,7 +823,7 @@ def confidence_topk_adjusted(logits, k, rows_per_seq, history=None, history_len=
             workspace = _empty((ws_bytes,), torch.uint8, logits.device, stream)
             ws = workspace.data_ptr()
     else:
-        ws, ws_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
+        ws, ws_bytes = _room(workspace, dev)
     st = _lib().traj_confidence_topk_adjusted(logits.data_ptr(), k, _arg(conf, "conf", torch.float32, shape, dev),
                                               _arg(idx, "idx", torch.int32, shape, dev), ctypes.byref(sh), ctypes.byref(a), ws, ws_bytes,
                                               _stream(stream))

@@ -211,6 +211,12 @@ def test_what_the_binding_refuses():
     for bad in (dict(lens=n[:1]), dict(q=q[:, :, :, :32]), dict(out=q[:1]), dict(q=q.expand(2, 3, 4, 64))):
         with pytest.raises(ValueError):
             attn(**bad)
+    room = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    for bad, err in ((room.cpu(), TypeError), (room[:1].expand(1 << 20), ValueError), (room[::2], ValueError)):
+        with pytest.raises(err):
+            attn(workspace=bad)
+        with pytest.raises(err):
+            tsp.confidence_topk_adjusted(torch.zeros(4, 100, dtype=BF, device="cuda"), 2, 2, history=table, workspace=bad)
     with pytest.raises(tsp.TrajSpecError, match="SHAPE"):
         attn(q=q[:, :, :3].contiguous())  # 3 query heads over 2
     for bad in (dict(start=n[:1]), dict(n_new=n[:1]), dict(q_out=q), dict(q=q, q_out=q[:1]), dict(v=k[:1]),
