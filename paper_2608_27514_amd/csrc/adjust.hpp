@@ -24,6 +24,7 @@ constexpr int kAdjustMaxVocab = 1 << 19;  // a bit per token and two bytes per 3
 constexpr int kAdjustPrepThreads = 1024;
 constexpr int kAdjustGroup = 512;         // tokens per popcount prefix
 constexpr int kAdjustLds = 144 << 10;      // of adjust_prepare_kernel
+constexpr int kAdjustRounds = 4;          // entries per token of a bias list that are added by all threads together
 constexpr uint32_t kAdjustSeen = 0x80000000u;
 constexpr uint32_t kFloorFinite = 0x00800000u;  // order_bits of the lowest finite value: -inf is no candidate
 
@@ -61,6 +62,8 @@ __device__ __forceinline__ float adjust_add(float bias, float f, float p, int c)
 // One workgroup per sequence.  LDS: the bitmap (words), a prefix of popcounts per group of 512 tokens, and a window
 // of counts and biases.  A record's place is its token's rank among the set bits, so no order of atomics shows.
 // A chain of LDS latencies between barriers (a sequence of 500 ids 5.2 us, 64 of 2048 ids 7.8).
+// Biases of a token named more than kAdjustRounds times are added by one thread each (300 biases, 250 of them one token's:
+// the call 51 us, in rounds alone 128; 2048 with 1800: 237 and 3356).
 __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(AdjustParams P) {
     extern __shared__ uint32_t prep_lds[];
     __shared__ int sh_wave[kAdjustPrepThreads / 64];
@@ -179,7 +182,8 @@ __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(Adju
             const int id = ids[j];
             return in_vocab(id) ? rank(id) - w0 : -1;
         };
-        for (bool more = P.NB > 0; more;) {
+        bool more = P.NB > 0;
+        for (int round = 0; more && round < kAdjustRounds; ++round) {
             if (tid == 0) sh_more = 0;
             for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
                 const int r = rank_at(j);
@@ -203,6 +207,19 @@ __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(Adju
                     summed[r] = j;
                     turn[r] = INT32_MAX;
                 }
+            }
+            __syncthreads();
+        }
+        if (more) {  // tokens named more often than that: the last entry in each sum goes through the rest of the list alone
+            for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
+                const int r = rank_at(j);
+                if (r < 0 || r >= P.window || summed[r] != j) continue;
+                const int id = named_at(j);
+                float y = bias_sum[r];
+#pragma unroll 8
+                for (int i = j + 1; i < P.NB; ++i)
+                    if (ids[i] == id) y += bias[i];
+                bias_sum[r] = y;
             }
             __syncthreads();
         }

@@ -175,6 +175,21 @@ def test_many_history_tokens_and_duplicates():
     check(x, how, 3, 1)
 
 
+def test_a_list_padded_with_one_token():
+    """Some tokens are named once, some a few times and one in most of the list, as padding of a real token with 0 would."""
+    V, NB = 4099, 1500
+    rng = np.random.default_rng(12)
+    x, _ = make(rng, 3, 2, V)
+    ids = rng.integers(0, V, (3, NB)).astype(np.int32)
+    bias = rng.standard_normal((3, NB)).astype(np.float32)
+    ids[0, 100:], bias[0, 100:] = 0, 0
+    ids[1, ::2] = 17
+    ids[2, 200:] = np.tile(rng.permutation(V)[:130], 10)
+    check(x, dict(bias_ids=ids, bias=bias), 8, 2)
+    h = rng.integers(0, V, (3, 40)).astype(np.int32)
+    check(x, dict(bias_ids=ids, bias=bias, history=h, presence=np.full(3, 0.5, np.float32)), 4, 2)
+
+
 def test_largest_vocabulary():
     V = 1 << 19
     rng = np.random.default_rng(10)
