@@ -597,6 +597,7 @@ struct PagedPlan {
 
 PagedPlan plan_paged(const traj_paged_shape* sh) {
     PagedPlan p{};
+    if (sh->B == 0 || sh->T == 0) return p;
     const int rows = sh->T * (sh->Hq / sh->Hkv);
     p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;

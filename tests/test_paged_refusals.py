@@ -50,6 +50,8 @@ def test_paged_shapes():
         assert append(shape(**bad)) == UNSUPPORTED and attn(shape(**bad)) == UNSUPPORTED
     for none in (dict(B=0), dict(T=0)):
         assert append(shape(**none), k=None) == 0 and attn(shape(**none), q=None) == 0
+        for columns in (4, 4096):
+            assert _lib.load().traj_paged_attn_workspace_size(ctypes.byref(shape(max_pages=columns, table_stride=columns, **none))) == 0
     assert _lib.load().traj_paged_attn(*[FAKE] * 7, None, 0.0, 0, None, 0, None) == NULL
 
 
