@@ -463,8 +463,8 @@ traj_status traj_paged_append(const void* q, int64_t q_stride, const void* k, in
  * over s < lens[b], or with causal != 0 over s < lens[b] - n_new[b] + t + 1 (the new tokens are the
  * sequence's last n_new[b]; n_new NULL: T).  A row that sees no key is 0, and so are the padding rows
  * t >= n_new[b], whose q may hold anything.  Softmax and accumulation in fp32; for the matrix product
- * the weights are rounded to 16 bits where T * Hq / Hkv <= 32, else to bf16 (8 bits); out rounded to
- * bf16.  q, out: [B, T, Hq, D] bf16, contiguous, 16-byte aligned; out must not overlap any input.
+ * the weights are rounded to 16 bits, as the sum of two bf16 values; out rounded to bf16.
+ * q, out: [B, T, Hq, D] bf16, contiguous, 16-byte aligned; out must not overlap any input.
  * lens [B] int32 (device); a length outside [0, max_pages * page_size] is clamped (TRAJ_DEV_BAD_LENGTH),
  * keys of a page outside the pool are not visible (TRAJ_DEV_BAD_PAGE); n_new[b] outside [0, T] is clamped
  * (TRAJ_DEV_BAD_LENGTH).  Rows of a page behind lens[b] may hold anything; those before it are finite (a

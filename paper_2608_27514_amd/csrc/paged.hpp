@@ -136,6 +136,7 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(AppendPara
 //     drained the wave's whole queue once per tile.
 //   * Two tiles in flight per wave where the registers hold them; buffers for 16 visible rows each give uniform
 //     bases and zeros behind the last key.
+//   * Each weight takes part in two products, as bf16 and as what that leaves: up to 32 rows this costs under 1%.
 //   S^T = K Q^T, weights in the lane that has the scores, O^T += V^T P^T: layouts of the 16-row verification kernel.
 //
 // Splits: the device computes from the lengths how many keys a workgroup takes (`chunk`).  A slot is a (sequence, range)
@@ -390,10 +391,10 @@ struct PagedRows {
             }
     }
 
-    // Weights of the keys against the running reference, in the operand order of values().  PARTS == 2: what rounding to
-    // bf16 leaves goes into a second operand, so that the product has the weights to 16 bits.
-    template <int NK, int PARTS>
-    __device__ __forceinline__ void weights(const f32x4_t (&s)[NR][2 * NK], float c, bf16x8_t (&pf)[PARTS][NR][NK]) {
+    // Weights of the keys against the running reference, in the operand order of values().  What rounding to bf16 leaves
+    // goes into a second operand, so that the product has the weights to 16 bits.
+    template <int NK>
+    __device__ __forceinline__ void weights(const f32x4_t (&s)[NR][2 * NK], float c, bf16x8_t (&pf)[2][NR][NK]) {
 #pragma unroll
         for (int f = 0; f < NR; ++f) {
             float mx = s[f][0][0];
@@ -415,14 +416,14 @@ struct PagedRows {
                 const float p = fast_exp2(__builtin_fmaf(s[f][v >> 2][v & 3], c, neg_mc[f]));
                 lsum[f] += p;
                 pf[0][f][v / 8][v % 8] = (__bf16)p;
-                if (PARTS == 2) pf[PARTS - 1][f][v / 8][v % 8] = (__bf16)(p - (float)(__bf16)p);
+                pf[1][f][v / 8][v % 8] = (__bf16)(p - (float)(__bf16)p);
             }
         }
     }
 
     // O^T += V^T P^T over the 32 NK keys whose LDS rows start at v
-    template <int NK, int PARTS>
-    __device__ __forceinline__ void values(const uint16_t* v, const bf16x8_t (&pf)[PARTS][NR][NK]) {
+    template <int NK>
+    __device__ __forceinline__ void values(const uint16_t* v, const bf16x8_t (&pf)[2][NR][NK]) {
         const int lane = threadIdx.x & 63;
         const uint16_t* vread = v + (4 * (lane >> 4) + ((lane & 15) >> 2)) * PagedLds<D>::kVRow + 4 * (lane & 3);
 #pragma unroll
@@ -433,7 +434,7 @@ struct PagedRows {
                 const bf16x4_t a1 = lds_read_tr(vread + 16 * db + (32 * i + 16) * PagedLds<D>::kVRow);
                 const bf16x8_t va = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-                for (int e = 0; e < PARTS; ++e)
+                for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int f = 0; f < NR; ++f) o[f][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[e][f][i], o[f][db], 0, 0, 0);
             }
@@ -519,7 +520,6 @@ __device__ __forceinline__ void paged_store(const PagedAttnParams& P, const Page
 template <int D, int NR, bool UNIFORM, int DEPTH>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnParams P) {
     using L = PagedLds<D>;
-    constexpr int PARTS = 2;  // the stream of K and V bounds the call: a second matrix product of each weight costs under 1%
     constexpr int ROWS = 16 * NR, NVL = D / 16, RPI = 512 / D;
     constexpr int kTileBytes = kPagedTile * L::kVRow * 2, kMergeBytes = ROWS * L::kMergeRow * 4;
     constexpr int kTiles = kPagedWaves * kTileBytes, kMerge = kPagedWaves * kMergeBytes;
@@ -578,8 +578,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnP
                     if (((vis[u] >> (i * RPI + vrow)) & 1u) == 0u) vr[u][i] = u32x4_t{};
             }
         }
-        bf16x8_t pf[PARTS][NR][1];
-        st.template weights<1, PARTS>(s, c, pf);
+        bf16x8_t pf[2][NR][1];
+        st.template weights<1>(s, c, pf);
 #pragma unroll
         for (int i = 0; i < NVL; ++i) *reinterpret_cast<u32x4_t*>(vwrite + i * RPI * L::kVRow) = vr[u][i];
         if (!UNIFORM) __builtin_amdgcn_sched_barrier(0);
@@ -588,7 +588,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnP
             vis[u] = next.vis;
         }
         __builtin_amdgcn_sched_barrier(0);  // the next tile's products stay behind this one's: registers
-        st.template values<1, PARTS>(tile, pf);
+        st.template values<1>(tile, pf);
         __builtin_amdgcn_sched_barrier(0);
     };
 
@@ -649,9 +649,10 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnP
 // More rows: RW waves of 32 rows each share the stages of 16 RW keys that they load into LDS together (a stage's K and
 // V would otherwise pass from the L2 once per 32 rows); 4 / RW such groups of waves take the range's stages in turn.
 // While a stage is multiplied the next one lies in registers on its way to the other buffer.  Here the matrix products
-// and the LDS reads that feed them count too, and the weights are rounded to bf16 (in two parts as above: 8 to 14% more
-// time, error against 64 bits 2.2e-3 -> 1.7e-3 of the output, which is the output's own rounding).
-//   MI355X: 8 blocks of 32 tokens, 28 over 4 heads, up to 2048 keys 25.4 us; 2 of 64 tokens over 10000 keys 41.
+// and the LDS reads that feed them count too; the weights' second part costs 12% of the blocks below and 23% of 2 x 512
+// tokens over 4096 keys (104 us without it), where the products bound the call.  Without it the error against 64 bits is
+// 2.2e-3 of the output, with it 1.7e-3, which is the output's own rounding.
+//   MI355X: 8 blocks of 32 tokens, 28 over 4 heads, up to 2048 keys 28.3 us; 2 of 64 tokens over 10000 keys 66.
 template <int D, int RW, bool UNIFORM, bool ONCE>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedAttnParams P) {
     using L = PagedLds<D>;
@@ -731,9 +732,9 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedAttnP
                 st.template scores<NK>(k, s);
                 const int key0 = stage_key(n);
                 if (all != (NK == 1 ? 0xffffffffull : ~0ull) || key0 + STAGE > min_limit) st.template mask<NK>(s, all, key0);
-                bf16x8_t pf[1][NR][NK];
-                st.template weights<NK, 1>(s, c, pf);
-                st.template values<NK, 1>(k + STAGE * L::kKRow, pf);
+                bf16x8_t pf[2][NR][NK];
+                st.template weights<NK>(s, c, pf);
+                st.template values<NK>(k + STAGE * L::kKRow, pf);
             }
             __syncthreads();
         }
