@@ -207,14 +207,32 @@ __device__ __forceinline__ int paged_chunk(int64_t total, int units, int capacit
     return kPagedGranule * (granules < 1 ? 1 : granules);
 }
 
-// The range that `slot` stands for; false where the batch has fewer.  All lanes of the wave take part.
-__device__ __forceinline__ bool paged_range(const PagedAttnParams& P, int slot, bool report, PagedRange& r) {
-    const int lane = threadIdx.x & 63;
+// Workgroup i runs on XCD i % 8.  The row tiles of one (slot, kv head) follow each other on one XCD, whose L2
+// they share; the (slot, kv head) pairs go round the XCDs in order, so that slots without work, the last ones,
+// leave none of them idle.
+struct PagedPlace {
+    int slot, g, unit, row_tile;
+};
+__device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams& P) {
+    PagedPlace w;
+    const int turn = blockIdx.x / 8 / P.tiles, pair = turn * 8 + blockIdx.x % 8;
+    w.row_tile = blockIdx.x / 8 - turn * P.tiles;
+    w.slot = pair / P.Hkv;
+    w.g = pair - w.slot * P.Hkv;
+    w.unit = w.g * P.tiles + w.row_tile;
+    return w;
+}
+
+// The range that the workgroup's slot stands for; false where the batch has fewer.  All lanes of the wave take part.
+// Lengths out of range are reported once per sequence where each workgroup looks at its own alone, else by workgroup 0.
+__device__ __forceinline__ bool paged_range(const PagedAttnParams& P, const PagedPlace& w, PagedRange& r) {
+    const int lane = threadIdx.x & 63, slot = w.slot;
     if (P.single) {
         if (slot >= P.B) return false;
-        r = PagedRange{slot, 0, 1, slot, paged_length(P, slot, report), P.cache.capacity};
+        r = PagedRange{slot, 0, 1, slot, paged_length(P, slot, w.unit == 0 && threadIdx.x == 0), P.cache.capacity};
         return true;
     }
+    const bool report = blockIdx.x == 0;
     const int len0 = lane < P.B ? paged_length(P, lane, report) : 0;
     uint64_t total = len0;
     for (int i = lane + 64; i < P.B; i += 64) total += paged_length(P, i, report);
@@ -457,22 +475,6 @@ struct PagedRows {
     }
 };
 
-// Workgroup i runs on XCD i % 8.  The row tiles of one (slot, kv head) follow each other on one XCD, whose L2
-// they share; the (slot, kv head) pairs go round the XCDs in order, so that slots without work, the last ones,
-// leave none of them idle.
-struct PagedPlace {
-    int slot, g, unit, row_tile;
-};
-__device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams& P) {
-    PagedPlace w;
-    const int turn = blockIdx.x / 8 / P.tiles, pair = turn * 8 + blockIdx.x % 8;
-    w.row_tile = blockIdx.x / 8 - turn * P.tiles;
-    w.slot = pair / P.Hkv;
-    w.g = pair - w.slot * P.Hkv;
-    w.unit = w.g * P.tiles + w.row_tile;
-    return w;
-}
-
 // Joins the SETS states of each of a workgroup's ROWS rows and writes the result, or its part of a sequence in several
 // ranges.
 template <int D, int ROWS, int SETS>
@@ -529,7 +531,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(PagedAttnP
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const PagedPlace w = paged_place(P);
     PagedRange r;
-    if (!paged_range(P, w.slot, blockIdx.x == 0, r)) return;
+    if (!paged_range(P, w, r)) return;
     const int len = r.len;
     const int begin = r.split * r.chunk, end = len - begin > r.chunk ? begin + r.chunk : len;
     const int n_new = paged_new(P, r.b, w.unit == 0 && r.split == 0 && threadIdx.x == 0);
@@ -667,7 +669,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedAttnP
     const int kg = wave / RW, rw = wave % RW;
     const PagedPlace w = paged_place(P);
     PagedRange r;
-    if (!paged_range(P, w.slot, blockIdx.x == 0, r)) return;
+    if (!paged_range(P, w, r)) return;
     const int len = r.len;
     const int begin = r.split * r.chunk, end = len - begin > r.chunk ? begin + r.chunk : len;
     const int n_new = paged_new(P, r.b, w.unit == 0 && r.split == 0 && threadIdx.x == 0);
