@@ -23,8 +23,9 @@ constexpr int kDevBadHistory = 0x80; // TRAJ_DEV_BAD_HISTORY
 constexpr int kAdjustMaxVocab = 1 << 19;  // a bit per token and two bytes per 32 of them in LDS: 96 KB
 constexpr int kAdjustPrepThreads = 1024;
 constexpr int kAdjustGroup = 512;         // tokens per popcount prefix
-constexpr int kAdjustLds = 144 << 10;      // of adjust_prepare_kernel
-constexpr int kAdjustRounds = 4;          // entries per token of a bias list that are added by all threads together
+constexpr int kAdjustLds = 144 << 10;      // of adjust_prepare_kernel, beside 8.2 KB of fixed size
+constexpr int kAdjustRounds = 4;          // entries per token of a part of a bias list that are added by all threads together
+constexpr int kAdjustScan = 16;           // entries that a thread looks at together
 constexpr uint32_t kAdjustSeen = 0x80000000u;
 constexpr uint32_t kFloorFinite = 0x00800000u;  // order_bits of the lowest finite value: -inf is no candidate
 
@@ -62,8 +63,10 @@ __device__ __forceinline__ float adjust_add(float bias, float f, float p, int c)
 // One workgroup per sequence.  LDS: the bitmap (words), a prefix of popcounts per group of 512 tokens, and a window
 // of counts and biases.  A record's place is its token's rank among the set bits, so no order of atomics shows.
 // A chain of LDS latencies between barriers (a sequence of 500 ids 5.2 us, 64 of 2048 ids 7.8).
-// Biases of a token named more than kAdjustRounds times are added by one thread each (300 biases, 250 of them one token's:
-// the call 51 us, in rounds alone 128; 2048 with 1800: 237 and 3356).
+// A bias list is taken in parts of an entry per thread, so that its cost goes by its length whatever it names: a round adds
+// each token's first entry of the part that is not in its sum, and what a token has left after kAdjustRounds of them is added
+// by one thread each, from LDS (8 rows of 126464: 300 biases distinct 24 us, 250 of them one token's 41; 16384 distinct 54, one
+// token five times 76, one token in every second 402).
 __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(AdjustParams P) {
     extern __shared__ uint32_t prep_lds[];
     __shared__ int sh_wave[kAdjustPrepThreads / 64];
@@ -73,10 +76,11 @@ __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(Adju
     uint16_t* inside = reinterpret_cast<uint16_t*>(prep_lds + groups * WPG);             // set bits of the group before the word
     int* prefix = reinterpret_cast<int*>(prep_lds + groups * WPG + groups * (WPG / 2));  // and before the group
     int* count = prefix + groups;                       // times seen
-    int* summed = count + P.window;                     // the last entry of the bias list that is in the sum, -1: none
-    int* turn = summed + P.window;                      // the entry that is next
+    int* turn = count + P.window;                       // the thread whose entry is next
     float* bias_sum = reinterpret_cast<float*>(turn + P.window);
     __shared__ int sh_more;
+    __shared__ __align__(16) int sh_rank[kAdjustPrepThreads];  // of a part of the bias list
+    __shared__ __align__(16) float sh_bias[kAdjustPrepThreads];
     const int seq = blockIdx.x, tid = threadIdx.x;
     const int32_t* history = P.history + (int64_t)seq * P.H;
     const int32_t* ids = P.bias_ids + (int64_t)seq * P.NB;
@@ -95,16 +99,14 @@ __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(Adju
     const float f = P.frequency != nullptr ? P.frequency[seq] : 0.f;
     const float p = P.presence != nullptr ? P.presence[seq] : 0.f;
     auto seen_at = [&](int i) { return i < kAdjustPrepThreads ? h0 : history[i]; };
-    auto named_at = [&](int j) { return j < kAdjustPrepThreads ? b0 : ids[j]; };
     auto in_vocab = [&](int id) { return id >= 0 && id < P.V; };
 
     for (int w = tid; w < groups * (WPG / 4); w += kAdjustPrepThreads) reinterpret_cast<u32x4_t*>(bits)[w] = u32x4_t{};
     auto clear_window = [&] {
         for (int i = tid; i < P.window; i += kAdjustPrepThreads) {
             count[i] = 0;
-            summed[i] = -1;
             turn[i] = INT32_MAX;
-            bias_sum[i] = 0.f;
+            bias_sum[i] = -0.f;  // plus any value: that value
         }
     };
     clear_window();
@@ -114,7 +116,7 @@ __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(Adju
         if (in_vocab(id)) atomicOr(&bits[id >> 5], 1u << (id & 31));
     }
     for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
-        const int id = named_at(j);
+        const int id = j < kAdjustPrepThreads ? b0 : ids[j];
         if (in_vocab(id)) atomicOr(&bits[id >> 5], 1u << (id & 31));
     }
     __syncthreads();
@@ -173,55 +175,56 @@ __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(Adju
             const int r = rank(id) - w0;
             if (r >= 0 && r < P.window) atomicAdd(&count[r], 1);
         }
-        // Biases of one token add up in the order of the list: a round adds each token's first entry that is not in
-        // its sum (one round, unless a token is named twice).
-        const int id0 = named_at(tid);
-        const int r0 = tid < P.NB && in_vocab(id0) ? rank(id0) - w0 : -1;
-        auto rank_at = [&](int j) -> int {
-            if (j < kAdjustPrepThreads) return r0;
-            const int id = ids[j];
-            return in_vocab(id) ? rank(id) - w0 : -1;
-        };
-        bool more = P.NB > 0;
-        for (int round = 0; more && round < kAdjustRounds; ++round) {
-            if (tid == 0) sh_more = 0;
-            for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
-                const int r = rank_at(j);
-                if (r >= 0 && r < P.window && j > summed[r]) atomicMin(&turn[r], j);
+        // Biases of one token add up in the order of the list.
+        int id = b0;
+        float y = y0;
+        for (int j0 = 0; j0 < P.NB; j0 += kAdjustPrepThreads) {
+            int r = tid < P.NB - j0 && in_vocab(id) ? rank(id) - w0 : -1;
+            if (r >= P.window) r = -1;
+            bool open = r >= 0;
+            sh_rank[tid] = r;
+            sh_bias[tid] = y;
+            const int next = j0 + kAdjustPrepThreads + tid;
+            if (next < P.NB) {
+                id = ids[next];
+                y = bias[next];
             }
-            __syncthreads();
-            for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
-                const int r = rank_at(j);
-                if (r < 0 || r >= P.window) continue;
-                const int t = turn[r];
-                if (j > t) sh_more = 1;
-                if (j == t) {
-                    bias_sum[r] = summed[r] < 0 ? (j < kAdjustPrepThreads ? y0 : bias[j]) : bias_sum[r] + (j < kAdjustPrepThreads ? y0 : bias[j]);
+            bool more = true;
+            for (int round = 0; more && round <= kAdjustRounds; ++round) {
+                if (tid == 0) sh_more = 0;
+                if (open) atomicMin(&turn[r], tid);
+                __syncthreads();
+                const bool mine = open && turn[r] == tid;
+                if (mine) {
+                    float sum = bias_sum[r] + sh_bias[tid];
+                    if (round == kAdjustRounds) {
+                        for (int i = tid & ~(kAdjustScan - 1); i < kAdjustPrepThreads; i += kAdjustScan) {
+                            u32x4_t rank4[kAdjustScan / 4];
+                            u32x4_t bias4[kAdjustScan / 4];
+#pragma unroll
+                            for (int e = 0; e < kAdjustScan / 4; ++e) {
+                                rank4[e] = *reinterpret_cast<const u32x4_t*>(sh_rank + i + 4 * e);
+                                bias4[e] = *reinterpret_cast<const u32x4_t*>(sh_bias + i + 4 * e);
+                            }
+#pragma unroll
+                            for (int e = 0; e < kAdjustScan; ++e) {
+                                const uint32_t other = rank4[e / 4][e % 4], add = bias4[e / 4][e % 4];
+                                sum = other == (uint32_t)r && i + e > tid ? sum + __builtin_bit_cast(float, add) : sum;
+                            }
+                        }
+                    }
+                    bias_sum[r] = sum;
+                } else if (open) {
+                    sh_more = 1;
                 }
-            }
-            __syncthreads();
-            more = sh_more != 0;
-            for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
-                const int r = rank_at(j);
-                if (r >= 0 && r < P.window && turn[r] == j) {
-                    summed[r] = j;
+                __syncthreads();
+                more = sh_more != 0;
+                if (mine) {
                     turn[r] = INT32_MAX;
+                    open = false;
                 }
+                __syncthreads();
             }
-            __syncthreads();
-        }
-        if (more) {  // tokens named more often than that: the last entry in each sum goes through the rest of the list alone
-            for (int j = tid; j < P.NB; j += kAdjustPrepThreads) {
-                const int r = rank_at(j);
-                if (r < 0 || r >= P.window || summed[r] != j) continue;
-                const int id = named_at(j);
-                float y = bias_sum[r];
-#pragma unroll 8
-                for (int i = j + 1; i < P.NB; ++i)
-                    if (ids[i] == id) y += bias[i];
-                bias_sum[r] = y;
-            }
-            __syncthreads();
         }
         if (P.NB == 0) __syncthreads();
         for (int w = tid; w < words; w += kAdjustPrepThreads) {
@@ -622,10 +625,10 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(const float* __restric
 }
 
 inline size_t adjust_lds(int chunk) { return ((size_t)(chunk + 31) / 32 + 1 + kAdjustList) * sizeof(uint32_t); }
-// LDS of adjust_prepare_kernel: bits and prefixes, then 16 bytes per record of the window.
+// LDS of adjust_prepare_kernel: bits and prefixes, then 12 bytes per record of the window.
 inline size_t adjust_prepare_fixed(int groups) { return (size_t)groups * (kAdjustGroup / 32 * 6 + 4); }
 inline int adjust_window(int groups, int max_records) {
-    const int most = (int)((kAdjustLds - adjust_prepare_fixed(groups)) / 16);
+    const int most = (int)((kAdjustLds - adjust_prepare_fixed(groups)) / 12);
     return max_records < most ? max_records : most;
 }
 

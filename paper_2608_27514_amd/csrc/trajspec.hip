@@ -1127,7 +1127,7 @@ traj_status traj_confidence_topk_adjusted(const void* logits, int32_t k, float* 
         p.groups = plan.groups;
         p.window = adjust_window(p.groups, p.max_records);
         hipLaunchKernelGGL(adjust_prepare_kernel, dim3((unsigned)plan.n_seq), dim3(kAdjustPrepThreads),
-                           adjust_prepare_fixed(p.groups) + 16 * (size_t)p.window, s, p);
+                           adjust_prepare_fixed(p.groups) + 12 * (size_t)p.window, s, p);
         const traj_status rs = launched();
         if (rs != TRAJ_OK) return rs;
     }
