@@ -268,11 +268,14 @@ traj_status traj_accept(const float* conf, const int32_t* idx, const traj_drafts
  *   score = sum of log C over the candidates chosen on the path below the root (root: 0),
  *   accumulated in fp32 in path order.
  *   With H empty, node 0 is one threshold-decoding step of s0 (the top-1 fallback), so an
- *   exact-mode traj_accept of the tree always advances.
+ *   exact-mode traj_accept of the tree always advances (unless it has no node).
+ * A slot with I < 0 is no candidate (traj_confidence_topk_adjusted writes -1 and confidence 0 where a
+ *   row allows fewer than k tokens): it makes no child, and a position p with I[p,0] < 0 is in neither
+ *   H nor Low, so that it stays masked in every node.
  * Outputs (breadth first, each level in kept order; int32 unless stated):
  *   tokens[b,n,:]   block state of node n, -1 = masked            [B, n_max, L]
  *   parent[b,n]     -1 or the generating node's index (< n)       [B, n_max]
- *   n_nodes[b]      number of nodes (0 when s0 has no masked position)  [B]
+ *   n_nodes[b]      number of nodes (0 when no masked position of s0 has a candidate)  [B]
  *   score[b,n]      float32 path log-confidence (may be NULL)      [B, n_max]
  *   Slots n >= n_nodes[b] hold s0, parent -1 and score -inf: a copy of s0 is never a
  *   consistent child, so the outputs can be verified and accepted as an n_max-draft tree.

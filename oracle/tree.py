@@ -28,6 +28,8 @@ taken here are:
   order.
 * Widths: hybrid w_l = max(W - l + 1, 1) for l = 1..D (W2D2 -> 2+1 = 3 children blocks,
   W3D3 -> 3+2+1 = 6: the n of the paper's W x D(n) notation); full w_l = W (W3D3(9)).
+* A slot with a negative id is no candidate (a row whose allowed tokens are fewer than k ends in such slots, with
+  confidence 0): it makes no child, and a position whose first slot is none is in neither H nor Low.
 * Node order: breadth first, each level in kept order; parent = index of the generating node.
 """
 
@@ -67,7 +69,7 @@ def build_tree(s0, conf, idx, tau, width, depth, branch, full=False, branch_deep
     if not 1 <= branch <= max(k, 1) or not 1 <= branch_deep <= max(k, 1):
         raise ValueError("branch and branch_deep must be in 1..k")
     # Phase 1: confidence stratification
-    masked = [p for p in range(L) if s0[p] == MASK]
+    masked = [p for p in range(L) if s0[p] == MASK and idx[p][0] >= 0]
     high = [p for p in masked if conf[p][0] > tau]
     low = [p for p in masked if conf[p][0] <= tau]
     root = s0.copy()
@@ -95,6 +97,8 @@ def build_tree(s0, conf, idx, tau, width, depth, branch, full=False, branch_deep
                 continue
             n_children = branch if level == 1 else branch_deep  # GenerateTopK at the root, GenerateTop1 deeper
             for j in range(n_children):
+                if idx[p][j] < 0:
+                    continue
                 child = state.copy()
                 child[p] = idx[p][j]
                 next_frontier.append((node, child, sc + math.log(conf[p][j]) if conf[p][j] > 0 else -math.inf))

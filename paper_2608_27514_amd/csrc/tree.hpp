@@ -7,9 +7,9 @@
 // all of its nodes), so level l fills q_l, the l-th low-confidence position in rank order.
 // Level l's candidates are (kept node i of level l-1, candidate j of q_l) in generation order
 // (i major); each is ranked by score (sum of logf of the chosen confidences, fp32) with
-// generation order breaking ties, and the first w_l ranks become the level's nodes.  Node
-// states are built in LDS (a node's row = its parent's row plus one position) and written out
-// at the end.
+// generation order breaking ties, and the first w_l ranks become the level's nodes.  A slot with a
+// negative id is no candidate: its score is NaN, which ranks before nothing.  Node states are
+// built in LDS (a node's row = its parent's row plus one position) and written out at the end.
 #pragma once
 
 #include "common.hpp"
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kTreeThreads) void build_tree_kernel(TreeParams P) 
 
     const int s = in ? P.state[(int64_t)b * L + p] : 0;
     const float c0 = in ? C[p * k] : 0.f;
-    const bool masked = in && s == -1;
+    const bool masked = in && s == -1 && I[p * k] >= 0;  // and with a candidate
     const bool hi = masked && c0 > P.tau;
     const bool low = masked && !hi;
     const uint64_t hmask = ballot64(hi);
@@ -117,12 +117,13 @@ __global__ __launch_bounds__(kTreeThreads) void build_tree_kernel(TreeParams P) 
         for (int m = p; m < M; m += kTreeThreads) {
             const int i = m / bl, j = m - i * bl;
             const float base = (l == 1) ? 0.f : nsc[prev_first + i];
-            csc[m] = base + logf(cs[q][j]);
+            csc[m] = is[q][j] >= 0 ? base + logf(cs[q][j]) : __builtin_nanf("");
         }
         __syncthreads();
         for (int m = p; m < M; m += kTreeThreads) {
             const float sm = csc[m];
-            int r = 0;
+            const int i = m / bl;
+            int r = is[q][m - i * bl] >= 0 ? 0 : w;
             for (int m2 = 0; m2 < M; ++m2) {
                 const float s2 = csc[m2];
                 r += (s2 > sm || (s2 == sm && m2 < m)) ? 1 : 0;
@@ -130,7 +131,6 @@ __global__ __launch_bounds__(kTreeThreads) void build_tree_kernel(TreeParams P) 
             const int slot = r < w ? n + r : -1;
             cnode[m] = slot;
             if (slot >= 0) {
-                const int i = m / bl;
                 par[slot] = (l == 1) ? (has_root ? 0 : -1) : prev_first + i;
                 nsc[slot] = sm;
             }
@@ -147,7 +147,9 @@ __global__ __launch_bounds__(kTreeThreads) void build_tree_kernel(TreeParams P) 
             if (in) tok[slot][p] = t;
         }
         __syncthreads();
-        const int c = min(w, M);
+        int some = 0;  // candidates of q
+        for (int j = 0; j < bl; ++j) some += is[q][j] >= 0 ? 1 : 0;
+        const int c = min(w, prev_cnt * some);
         prev_first = n;
         prev_cnt = c;
         n += c;
