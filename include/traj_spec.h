@@ -200,7 +200,9 @@ traj_status traj_confidence_topk_noalloc(const void* logits, int32_t k, float* c
  * state(n)  = tokens[b,n]  with candidates conf/idx of draft n's rows.
  * step_tau(s, C, I): if s has no masked position there is no step; otherwise unmask every
  *   masked p with C[p,0] > threshold (strict) with token I[p,0]; if there is none, unmask
- *   only the masked p of largest C[p,0] (smallest p on equal values).
+ *   only the masked p of largest C[p,0] (smallest p on equal values).  A masked p with I[p,0] < 0
+ *   has no candidate (as traj_confidence_topk_adjusted reports a row that allows nothing) and is
+ *   left masked; if no masked p has one there is no step.
  * Draft c with parent q is consistent when
  *   TRAJ_MODE_EXACT: tokens[c] == step_tau(state(q)) at every position;
  *   TRAJ_MODE_TOP1 : it keeps every unmasked token of state(q), unmasks at least one new
@@ -214,7 +216,7 @@ traj_status traj_confidence_topk_noalloc(const void* logits, int32_t k, float* c
  *   on_path[b,n]       1 if draft n lies on the root path of leaf
  *   n_accepted[b]      #positions masked in committed[b] and unmasked in the leaf (0 if none)
  *   out_tokens[b,:]    tokens[b,leaf], or committed[b] when leaf = -1
- *   hi[b,n,p]          1 if tokens[b,n,p] is masked and conf[b,n,p,0] > threshold
+ *   hi[b,n,p]          1 if tokens[b,n,p] is masked, idx[b,n,p,0] >= 0 and conf[b,n,p,0] > threshold
  * conf/idx are traj_confidence_topk's outputs for rows ordered (b, n, p): [B,N,L,k].
  * Limits: 1 <= N <= 64; 1 <= L <= 64; 1 <= k <= 8; B >= 1.  All arrays are device arrays.
  * ------------------------------------------------------------------------------------ */
@@ -492,7 +494,8 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
  *                       z = frequency[q] * c + presence[q] where c > 0, else 0;
  *     x = -inf where bit v % 32 of mask[m, v / 32] is 0,   m = mask_index[r],
  * each operation in fp32.  A value of -inf is never a candidate: a row's slots without one hold idx -1 and conf 0 (all of
- * them where nothing is allowed).  Logits of forbidden tokens may hold anything; the others no NaN or +inf.
+ * them where nothing is allowed), which traj_accept and traj_build_tree take as no candidate.  Logits of forbidden tokens
+ * may hold anything; the others no NaN or +inf.
  * Ids outside [0, vocab) in history and bias_ids are padding.
  * history [n_seq, history_size] int32, history_len [n_seq] (NULL: history_size), repetition (> 0), frequency,
  * presence [n_seq] float32 (each NULL: 1, 0, 0), bias_ids / bias [n_seq, bias_size] int32 / float32 (finite or

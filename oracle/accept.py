@@ -11,7 +11,9 @@ Definitions followed:
   confident masked position is unmasked.  "Exceeds" is strict: Alg. 1 phase 1
   puts confidence > tau in the high set H and confidence <= tau in the low set.
   Equal fallback confidences go to the smallest position (not stated in the
-  paper).
+  paper).  A position whose first id is negative has no candidate (no token is
+  allowed there) and stays masked; without any other masked position there is
+  no step.
 * Logit reuse (Sec. 3.1): the confidences that decide a node's next step are
   the ones produced by verifying that node.  The children of the committed
   state (parent -1) are checked against the committed state's own conf/idx,
@@ -35,7 +37,7 @@ Definitions followed:
 * Outputs: accepted leaf (-1 if none), on-path flags, number of positions the
   leaf unmasks relative to the committed state, the accepted block state (the
   committed state when nothing is accepted), and hi[n,p] = (position p of draft
-  n is still masked and its confidence exceeds tau) -- the high-confidence set
+  n is still masked, has a candidate and its confidence exceeds tau) -- the high-confidence set
   H of Alg. 1 phase 1 that seeds the next root.
 
 Shapes for one sequence: tokens [N,L] (MASK = -1), parent [N], committed [L],
@@ -52,11 +54,11 @@ TRAVERSALS = ("greedy", "longest")
 def threshold_step(state, conf, idx, tau):
     """One threshold-decoding step from block ``state``.
 
-    Returns the new state (a copy), or None when the state has no masked
-    position left (the block is complete and cannot be stepped).
+    Returns the new state (a copy), or None when no masked position is left that
+    has a candidate (the block is complete or cannot be stepped).
     """
     state = np.asarray(state)
-    masked = [p for p in range(len(state)) if state[p] == MASK]
+    masked = [p for p in range(len(state)) if state[p] == MASK and idx[p][0] >= 0]
     if not masked:
         return None
     chosen = [p for p in masked if conf[p][0] > tau]
@@ -167,7 +169,7 @@ def accept_sequence(tokens, parent, committed, conf0, idx0, conf, idx, tau,
     hi = np.zeros((N, L), dtype=bool)
     for n in range(N):
         for p in range(L):
-            hi[n, p] = tokens[n][p] == MASK and conf[n][p][0] > tau
+            hi[n, p] = tokens[n][p] == MASK and idx[n][p][0] >= 0 and conf[n][p][0] > tau
     return {"leaf": leaf, "on_path": on_path, "n_accepted": n_acc,
             "out_tokens": out_tokens, "hi": hi}
 

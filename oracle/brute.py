@@ -90,12 +90,13 @@ def consistent_scalar(child, parent_state, conf, idx, tau, mode="exact"):
     if not unchanged_outside:
         return False
     if mode == "exact":
-        if not masked:
+        open_ = {p for p in masked if int(idx[p][0]) >= 0}  # a negative id: no token is allowed there
+        if not open_:
             return False  # a complete block has no next step
-        chosen = {p for p in masked if conf[p][0] > tau}
+        chosen = {p for p in open_ if conf[p][0] > tau}
         if not chosen:
-            best = max(float(conf[p][0]) for p in masked)
-            chosen = {min(p for p in masked if float(conf[p][0]) == best)}
+            best = max(float(conf[p][0]) for p in open_)
+            chosen = {min(p for p in open_ if float(conf[p][0]) == best)}
         return newly == chosen and all(child[p] == idx[p][0] for p in chosen)
     width = {"top1": 1, "topk": len(idx[0])}[mode]
     return len(newly) >= 1 and all(child[p] in [idx[p][j] for j in range(width)] for p in newly)

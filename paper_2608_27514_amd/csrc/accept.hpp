@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(AcceptParams P) 
                 t1 = top_t[q * L + lane];
             }
         }
-        const bool masked = lane_in && s == MASK;
+        const bool masked = lane_in && s == MASK && t1 >= 0;  // and with a candidate
         const bool over = masked && c > P.tau;
         const uint64_t mmask = ballot64(masked);
         const uint64_t hmask = ballot64(over);

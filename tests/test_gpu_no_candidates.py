@@ -81,3 +81,58 @@ def test_a_tree_behind_adjusted_logits():
     check_tree(out, build_tree_batch(state, None, None, None, c, i, tau, 3, 3, 3, False, out["parent"].shape[1]))
     assert out["n_nodes"][0] == 0 and (out["tokens"][0] == -1).all()
     assert torch.equal(out["conf_next"], conf) and torch.equal(out["idx_next"], idx)
+
+
+def check_accept(out, ref):
+    for name in ("leaf", "n_accepted", "out_tokens", "on_path", "hi"):
+        got = out[name].cpu().numpy()
+        assert np.array_equal(got.astype(bool) if ref[name].dtype == bool else got, ref[name]), name
+
+
+@pytest.mark.parametrize("traversal", ["greedy", "longest"])
+@pytest.mark.parametrize("mode", ["exact", "top1", "topk"])
+@pytest.mark.parametrize("most", [0, 1, 2, 3])
+@pytest.mark.parametrize("tau", [0.6, -1.0])
+def test_acceptance_of_rows_with_few_tokens(mode, traversal, most, tau):
+    """Drafts among them that copy their parent, and the step that the oracle takes."""
+    rng = np.random.default_rng(most)
+    B, N, L, k = 12, 9, 8, 3
+    tau = float(np.float32(tau))
+    committed = np.where(rng.random((B, L)) < 0.8, -1, 50).astype(np.int32)
+    conf0, idx0 = table(rng, (B, L), k, most)
+    conf, idx = table(rng, (B, N, L), k, most)
+    parent = np.array([-1, -1, 0, 1, 1, 2, -1, 6, 3], np.int32)
+    tokens = np.empty((B, N, L), np.int32)
+    for b in range(B):
+        for n in range(N):
+            q = parent[n]
+            s, C, I = (committed[b], conf0[b], idx0[b]) if q < 0 else (tokens[b, q], conf[b, q], idx[b, q])
+            step = oracle.threshold_step(s, C, I, tau)
+            tokens[b, n] = s if n in (0, 4) or step is None else step
+            if n == 5:
+                tokens[b, n] = np.where((s == -1) & (rng.random(L) < 0.5), I[:, 0], s)
+    parents = np.broadcast_to(parent, (B, N)).copy()
+    out = tsp.accept(cuda(conf), cuda(idx), cuda(tokens), cuda(parents), cuda(committed), cuda(conf0), cuda(idx0), tau, mode, traversal)
+    check_accept(out, oracle.accept_batch(tokens, parents, committed, conf0, idx0, conf, idx, tau, mode, traversal))
+
+
+def test_a_block_decoded_under_a_grammar():
+    """Adjusted logits -> tree -> acceptance, step after step: positions that allow nothing stay masked, all others are
+    filled, and what is accepted is what the oracles accept."""
+    rng = np.random.default_rng(2)
+    B, L, k, tau = 4, 12, 3, float(np.float32(0.6))
+    conf, idx = adjusted_candidates(rng, B, L, k, 300)
+    c, i = conf.cpu().numpy(), idx.cpu().numpy()
+    state = np.full((B, L), -1, np.int32)
+    for _ in range(L):
+        tree = tsp.build_tree(cuda(state), conf, idx, tau, 2, 2, 2)
+        n = tree["parent"].shape[1]
+        drafts = [x.cpu().numpy() for x in (tree["tokens"], tree["parent"])]
+        many = [x[:, None].expand(B, n, L, k).contiguous() for x in (conf, idx)]  # the model says the same of every draft
+        out = tsp.accept(*many, tree["tokens"], tree["parent"], cuda(state), conf, idx, tau)
+        ref = oracle.accept_batch(*drafts, state, c, i, *(x.cpu().numpy() for x in many), tau)
+        check_accept(out, ref)
+        left = (state == -1) & (i[..., 0] >= 0)
+        assert ((ref["n_accepted"] > 0) == left.any(1)).all()
+        state = ref["out_tokens"].astype(np.int32)
+    assert ((state == -1) == (i[..., 0] < 0)).all()
