@@ -601,6 +601,13 @@ def _arg(t, name, dtype, shape, dev):
     return p
 
 
+def _int32(**sizes):
+    """A size past 31 bits would be another one in the C structures."""
+    for name, n in sizes.items():
+        if n >= 1 << 31:
+            raise ValueError(f"{name} must be below 2^31, got {n}")
+
+
 def _room(workspace, dev):
     """A caller's workspace as (address, bytes)."""
     _here(workspace, "workspace", dev)
@@ -616,6 +623,7 @@ def _paged_struct(B, T, Hq, pages, strides, table, table_strides):
         raise ValueError("k_pages and v_pages must be [pages, page_size, Hkv, D] with a contiguous last dimension")
     if len(table) != 2 or table[0] != B or table_strides[1] != 1 and table[1] > 1:
         raise ValueError("page_table must be [B, max_pages] with contiguous rows")
+    _int32(B=B, T=T, heads=Hq, pages=pages[0], page_size=pages[1], kv_heads=pages[2], head_size=pages[3], max_pages=table[1])
     # a dimension of one entry has no stride that matters
     sh = PagedShape(B, T, Hq, pages[2], pages[3], pages[0], pages[1], table[1], max(table_strides[0], table[1]) if B <= 1 else table_strides[0],
                     strides[0] if pages[0] > 1 else 8, strides[1] if pages[1] > 1 else 8, strides[2] if pages[2] > 1 else 8)
@@ -769,6 +777,8 @@ def _logit_adjust(dev, R, V, per, history, history_len, repetition, frequency, p
         if mask is None:
             raise ValueError("mask_index needs mask")
         xp = _arg(mask_index, "mask_index", i32, (R,), dev)
+    if max(per, H, NB, masks) >= 1 << 31:
+        _int32(rows_per_seq=per, history=H, biases=NB, masks=masks)
     return LogitAdjust(per, H, NB, masks, hp, lp, rp, fp, pp, ip, bp, mp, xp, mask_stride)
 
 
@@ -785,6 +795,7 @@ def _logit_rows(logits):
 
 @functools.lru_cache(maxsize=1024)
 def _adjust_workspace(rows, vocab, row_stride, dtype, k, per, H, NB):
+    _int32(k=k, rows_per_seq=per, history=H, biases=NB)
     return int(_lib().traj_confidence_topk_adjusted_workspace_size(ctypes.byref(LogitsShape(rows, vocab, row_stride, dtype)), k,
                                                                    ctypes.byref(LogitAdjust(per, H, NB))))
 
@@ -809,6 +820,8 @@ def confidence_topk_adjusted(logits, k, rows_per_seq, history=None, history_len=
     dev = _current()
     _here(logits, "logits", dev)
     k, per = int(k), int(rows_per_seq)
+    if k >= 1 << 31:
+        _int32(k=k)
     R = sh.rows
     a = _logit_adjust(dev, R, sh.vocab, per, history, history_len, repetition, frequency, presence, bias_ids, bias, mask, mask_index)
     shape = (R, k)
