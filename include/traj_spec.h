@@ -435,7 +435,7 @@ traj_status traj_linear(const void* x, const void* w, void* y, int64_t M, int64_
  * page_table: int32, max_pages columns, table_stride elements from row to row; entries behind a
  * sequence's last page are never read.  Sequences may share pages that neither writes.
  * Limits (all entry points): B >= 0 and T >= 0 (0 = no-op) with B <= 65535, T <= 2^24; D in {64, 128};
- *   Hq % Hkv == 0; num_pages, page_size, max_pages >= 1 with max_pages * page_size <= 2^31 - 4096;
+ *   Hq % Hkv == 0, Hq <= 65536; num_pages, page_size, max_pages >= 1 with max_pages * page_size <= 2^31 - 4096;
  *   strides positive multiples of 8 with token_stride <= 2^25; pools and q / k / v rows 16-byte
  *   aligned; table_stride >= max_pages.
  * ------------------------------------------------------------------------------------ */

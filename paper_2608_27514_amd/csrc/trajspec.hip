@@ -554,7 +554,9 @@ traj_status run_layer(uint16_t* xs, const traj_layer_weights* w, const traj_laye
 constexpr int64_t kMostWgs = (1 << 24) - 1;
 
 traj_status check_paged(const traj_paged_shape* sh) {
-    if (sh->B < 0 || sh->B > 65535 || sh->T < 0 || sh->T > (1 << 24) || sh->Hq < 1 || sh->Hkv < 1 || sh->Hq % sh->Hkv != 0) return TRAJ_E_SHAPE;
+    if (sh->B < 0 || sh->B > 65535 || sh->T < 0 || sh->T > (1 << 24)) return TRAJ_E_SHAPE;
+    // B T Hq and what is made of it stays within 64 bits, a token's values within 31
+    if (sh->Hq < 1 || sh->Hq > 65536 || sh->Hkv < 1 || sh->Hq % sh->Hkv != 0) return TRAJ_E_SHAPE;
     if (sh->num_pages < 1 || sh->page_size < 1 || sh->max_pages < 1) return TRAJ_E_SHAPE;
     // keys past the last one are numbered too, up to a few tiles
     if ((int64_t)sh->max_pages * sh->page_size > (1ll << 31) - 4096 || sh->table_stride < sh->max_pages) return TRAJ_E_SHAPE;
