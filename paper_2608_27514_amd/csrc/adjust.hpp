@@ -241,11 +241,9 @@ __global__ __launch_bounds__(kAdjustPrepThreads) void adjust_prepare_kernel(Adju
     }
 }
 
-// Absorbs NV values x (-inf: forbidden) of vocabulary indices id0 .. whose maximum is vmax, as absorb() does, with two
-// differences.  A lane's reference stays at or above kRefFloor, so that values at the type's lowest add 0 and not NaN
-// (a row of nothing else is summed again).  And the sum is kept relative to 2^(-nrl), nrl being the
-// rounded product, which lane_sum() corrects once at the end: no error grows with the logits' size.
-constexpr float kRefFloor = -1e30f;
+// Absorbs NV values x (-inf: forbidden) of vocabulary indices id0 .. whose maximum is vmax, as absorb() does, but the sum is
+// kept relative to 2^(-nrl), nrl being the rounded product, which lane_sum() corrects once at the end: no error grows
+// with the logits' size.
 template <int K, int NV>
 __device__ __forceinline__ void adjust_absorb(const float (&x)[NV], float vmax, int id0, TopkLane<K>& st, uint32_t floor_bits) {
     const bool up = vmax > st.rthr;
@@ -277,13 +275,6 @@ __device__ __forceinline__ void adjust_absorb(const float (&x)[NV], float vmax, 
 template <int K>
 __device__ __forceinline__ float lane_sum(const TopkLane<K>& st) {
     return st.s != 0.f ? st.s * fast_exp2(-__builtin_fmaf(st.ref, kLog2e, st.nrl)) : 0.f;
-}
-
-// Two (reference, sum) pairs whose references may be of any finite size; -inf: nothing.
-__device__ __forceinline__ void adjust_merge_ms(float& m, float& s, float m2, float s2) {
-    const float M = fmaxf(m, m2), Ms = M == kNegInf ? 0.f : M;
-    s = s * fast_exp2((m - Ms) * kLog2e) + s2 * fast_exp2((m2 - Ms) * kLog2e);
-    m = M;
 }
 
 // conf / idx of a row from its (reference, sum) and its keys; a slot without a candidate: 0 and -1.
@@ -605,7 +596,7 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(const float* __restric
     tl.clear();
     for (int sp = lane; sp < splits; sp += 64) {
         const float* rec = partial + ((int64_t)row * splits + sp) * kTopkRecord;
-        adjust_merge_ms(m, s, rec[0], rec[1]);
+        merge_ms(m, s, rec[0], rec[1]);
         const uint64_t* rk = reinterpret_cast<const uint64_t*>(rec + 2);
         uint64_t o[K];
 #pragma unroll

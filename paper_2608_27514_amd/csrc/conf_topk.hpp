@@ -127,11 +127,10 @@ __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
     return v;
 }
 
-// Merge two (reference, sum) pairs, each sum relative to its own reference; the result is
-// relative to the larger reference.
+// Merge two (reference, sum) pairs, each sum relative to its own reference (of any finite size; -inf: nothing); the
+// result is relative to the larger reference.
 __device__ __forceinline__ void merge_ms(float& m, float& s, float m2, float s2) {
-    const float M = fmaxf(m, m2);
-    const float Ms = fmaxf(M, -1e30f);
+    const float M = fmaxf(m, m2), Ms = M == kNegInf ? 0.f : M;
     s = s * fast_exp2((m - Ms) * kLog2e) + s2 * fast_exp2((m2 - Ms) * kLog2e);
     m = M;
 }
@@ -193,7 +192,7 @@ __device__ __forceinline__ void wave_top_keys(TopList<K>& tl, uint64_t (&best)[K
 // Running state of one lane.
 template <int K>
 struct TopkLane {
-    float ref;   // reference: an element value of this lane (-inf before the first finite one)
+    float ref;   // reference: an element value of this lane, or kRefFloor (-inf before the first finite one)
     float nrl;   // -ref * log2(e) (0 before the first reference)
     float rthr;  // ref + kTopkLazyLog2 / log2(e): a larger vector maximum moves the reference
     float s;     // sum of exp2(x log2e + nrl) over the lane's values
@@ -227,18 +226,23 @@ __device__ __forceinline__ float vec_max(const float (&x)[NV]) {
     return m;
 }
 
+// A lane's reference stays at or above this, so that values far below it, which masks by -1e10 or by the type's lowest value
+// leave, add 0: relative to such a value itself the rounding of its product with log2(e) alone gives weights beyond fp32 (a
+// slice of nothing else is summed again).
+constexpr float kRefFloor = -1e6f;
+
 // Absorbs NV values x (vocabulary indices id0 ..) whose maximum is vmax.  Values are never NaN
 // (an ABI precondition), so the NaN-propagating maxima above are exact.
 template <int K, int NV>
 __device__ __forceinline__ void absorb(const float (&x)[NV], float vmax, int id0, TopkLane<K>& st, uint32_t floor_bits) {
     const bool up = vmax > st.rthr;
     if (ballot64(up) != 0ull) {  // wave-uniform branch, rare after the first vectors
-        const float nr = -vmax * kLog2e;
+        const float ref = fmaxf(vmax, kRefFloor), nr = -ref * kLog2e;
         const float f = fast_exp2(__builtin_fmaf(st.ref, kLog2e, nr));  // 0 while ref is -inf
         st.s = up ? st.s * f : st.s;
-        st.ref = up ? vmax : st.ref;
+        st.ref = up ? ref : st.ref;
         st.nrl = up ? nr : st.nrl;
-        st.rthr = up ? vmax + kTopkLazyLog2 / kLog2e : st.rthr;
+        st.rthr = up ? ref + kTopkLazyLog2 / kLog2e : st.rthr;
     }
     st.lmax = __builtin_elementwise_maximum(st.lmax, vmax);
     float acc = fast_exp2(__builtin_fmaf(x[0], kLog2e, st.nrl));
@@ -478,6 +482,20 @@ __global__ __launch_bounds__(THREADS) void conf_topk_kernel(const T* __restrict_
 #pragma unroll
             for (int j = 0; j < K; ++j) lane_pair64(t, tl.key[j], tl.key[j], b[j]);
             tl.merge(b);
+        }
+    }
+    // Weights that came to nothing (or overflowed): all of the slice's values are at the lowest end of their type, or its
+    // maximum is at the highest.  The sum is taken again, relative to the maximum and subtracting first.
+    const float s0 = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, s)));
+    if (!(s0 > 0.f && s0 < -kNegInf)) {
+        const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(tl.key[0] >> 32));
+        const float top = value_of_bits(hi);
+        if (hi != 0u && top != kNegInf) {  // a slice of -inf has no sum
+            m = top;
+            s = 0.f;
+            for (int e = begin + lane; e < end; e += 64) s += fast_exp2((load_scalar(base + e) - top) * kLog2e);
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
         }
     }
     if (lane != 0) return;
