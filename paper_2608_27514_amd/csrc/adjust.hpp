@@ -294,7 +294,7 @@ __device__ __forceinline__ void adjust_finish(const uint64_t (&key)[K], float m,
 // grid.x = rows * splits, slices and register ring as conf_topk_kernel.  LDS: the slice's allowed bits, and the list of
 // a slice with few allowed tokens.
 //   * Vectors without an allowed token are not read (their lanes load the slice's first vector), and a slice with at
-//     most kAdjustList allowed ones gathers just those (256 rows of 126464 under masks of 250 tokens: 22.5 -> 8.3 us).
+//     most kAdjustList allowed ones gathers just those (256 rows of 126464 under masks of 250 tokens: 22.5 -> 10.0 us).
 //   * The special tokens are gathered behind the stream, several per lane at a time.  Each costs a 64-byte sector of
 //     its row: 2048 rows of 126464 bf16 take 87 us with nothing to adjust (6.0 TB/s), 100 with a mask of 97%, 129 with
 //     1800 special tokens each besides (222 MB of sectors).  Gathered along the way, with the lines just streamed, they

@@ -142,22 +142,25 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(AppendPara
 // Splits: the device computes from the lengths how many keys a workgroup takes (`chunk`).  A slot is a (sequence, range)
 // pair in order; the partial results of a sequence in several ranges are joined by a second kernel.
 //   MI355X: 32 sequences of up to 8192 keys x 32 heads of 128 (2.2 GB) 359 us = 6.2 TB/s, one of 2^20 keys x 8 heads
-//   6.7 TB/s, one of 65536 47.5 us = 5.6 TB/s (the read-only logit pass streams 6.2 TB/s).
+//   6.7 TB/s, one of 65536 49.2 us = 5.5 TB/s (the read-only logit pass streams 6.2 TB/s).
 constexpr int kPagedWaves = 4;
 constexpr int kPagedThreads = kPagedWaves * 64;
 constexpr int kPagedTile = 32;
 constexpr int kPagedGranule = kPagedWaves * kPagedTile;
 // Chunks make about kPagedFillWgs workgroups at least (one per CU), then stay at kPagedChunk keys, under which filling and
-// joining costs more than the shorter chain saves (65536 keys x 8 heads: 512 keys 49.0 us, 1024 47.5), and grow once there are
-// kPagedMostWgs of them: finer ones balance lengths and CUs better (32 sequences of up to 8192 keys: 4224 keys
-// 377 us, 2112 keys 359).
+// joining costs more than the shorter chain saves (65536 keys x 8 heads: 512 keys take 1.5 us longer than 1024), and grow once
+// there are kPagedMostWgs of them: finer ones balance lengths and CUs better (32 sequences of up to 8192 keys: 4224 keys
+// 377 us, 2112 keys 359).  All three were measured on calls of one token a sequence and hold for the kernels of more rows too.
 constexpr int kPagedFillWgs = 256, kPagedChunk = 1024, kPagedMostWgs = 2048;
 // More sequences than this fill the chip by themselves and are never split: every workgroup of a split call looks at all
 // lengths.
 constexpr int kPagedSplitBatch = 2048;
 // Nor are batches of so many query rows, of which a wave each would not go into the joining launch.
 constexpr int64_t kPagedSplitRows = 1 << 26;
-// Caches up to this many keys are never split: a join takes longer (192 keys: 4.2 us whole, 7.7 split).
+// Caches up to this many keys are never split: a join takes longer.  One token each, whole and split: 192 keys 4.2 and 7.4 us
+// (4 heads of 64), 5.4 and 7.6 (32 over 8 of 128); 272 keys 5.0 and 6.4, 6.6 and 7.1; 512 keys 5.9 and 6.6, 8.2 and 7.2.
+// Blocks of 32 tokens, 28 over 4 heads: 192 keys 12.5 and 13.9, 272 keys 16.9 and 14.8.  `capacity` decides, as the launch
+// knows no length: short sequences in a wide table pay the split's price.
 constexpr int kPagedWhole = 256;
 
 struct PagedAttnParams {
