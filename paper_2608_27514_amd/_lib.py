@@ -360,7 +360,8 @@ def confidence_topk_noalloc(logits, k, conf=None, idx=None, stream=None):
 def accept(conf, idx, tokens, parent, committed, conf0, idx0, threshold, mode="exact", traversal="greedy",
            out=None, stream=None):
     """Acceptance; returns a dict of device tensors (leaf, on_path, n_accepted,
-    out_tokens, hi).  conf/idx may be [B*N*L, k] or [B,N,L,k]."""
+    out_tokens, hi).  conf/idx may be [B*N*L, k] or [B,N,L,k]; a position whose first idx is
+    negative has no candidate and is left masked."""
     B, N, L = tokens.shape
     k = conf0.shape[-1]
     if conf.numel() != B * N * L * k or idx.numel() != B * N * L * k:
@@ -412,7 +413,8 @@ def build_tree(state, conf0, idx0, threshold, width, depth, branch, full=False, 
     """Next step's draft tree (Alg. 1) from the accepted state; returns a dict of device
     tensors tokens [B,n_max,L], parent [B,n_max], n_nodes [B], score [B,n_max],
     conf_next / idx_next [B,L,k].  With ``leaf`` (traj_accept's leaf) the candidates come
-    from conf/idx [B,N,L,k] (or [B*N*L,k]) of the verified tree, else from conf0/idx0."""
+    from conf/idx [B,N,L,k] (or [B*N*L,k]) of the verified tree, else from conf0/idx0.  A slot with a
+    negative idx is no candidate (:func:`confidence_topk_adjusted`)."""
     B, L = state.shape
     k = conf0.shape[-1]
     for name, t, dt in (("state", state, torch.int32), ("conf0", conf0, torch.float32), ("idx0", idx0, torch.int32)):
