@@ -1,0 +1,435 @@
+"""Operators of a serving step in 8 bits, each in its plain form and as the framework's call.
+
+Where few tokens are new, a serving step reads the cache and the weights and little else.  Here both are held in 8 bits
+(e4m3) with a power-of-two scale (a biased exponent in a byte) for each block: of some tokens and one head in the paged
+cache ("append8" writes it, "attend8" reads it), of 128 x 128 values of a weight matrix ("quantize8" makes it once,
+"linear8" multiplies by it, taking each row of activations to 8 bits in blocks of 128).
+
+Everywhere a block's scale is the smallest power of two, 2^-100 at least, that brings its values to 448 at most.  An append
+that begins inside a block of tokens keeps the block's rows before it: the scale never falls there, and where it grows they are
+rounded again.
+
+Head layouts and matrices are those of the benchmark's and the tests' models: 32 heads of 128, 28 over 4 heads, 32 over 8,
+small ones with heads of 64; hidden sizes of 4096 and 3584 with their projections.
+"""
+
+import math
+
+import torch
+import torch.nn.functional as F
+
+own = False
+
+DEV = "cuda"
+BF, F32, F64, I32, U8 = torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.uint8
+E4, E8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+THETA = 500000.0
+BLOCK, LARGEST, LOWEST = 128, 448.0, 27  # values of a weight block's side; the largest e4m3; the byte of 2^-100
+
+
+def listed():
+    return [
+        # one token of one sequence, inside a block: the launch is all there is
+        dict(name="append8 one token", kind="append8", B=1, T=1, Hq=32, Hkv=8, D=128, ps=16, sb=16, near=700, ragged=False),
+        # a denoising step of a batch: blocks of up to 32 tokens, written again at every step
+        dict(name="append8 blocks", kind="append8", B=16, T=32, Hq=32, Hkv=32, D=128, ps=32, sb=16, near=4096, ragged=True),
+        # prompts of four sequences, pages of an odd size
+        dict(name="append8 prompts", kind="append8", B=4, T=4096, Hq=28, Hkv=4, D=128, ps=48, sb=24, near=0, ragged=False),
+        # one new token of one long sequence: few rows, a long axis
+        dict(name="attend8 long", kind="attend8", B=1, T=1, Hq=32, Hkv=8, D=128, S=65536, ps=64, sb=64, causal=False),
+        # five drafted tokens each of three sequences, pages and scales that end inside every tile
+        dict(name="attend8 drafted", kind="attend8", B=3, T=5, Hq=16, Hkv=16, D=64, S=777, ps=24, sb=8, causal=True),
+        # a denoising step's block of 32 tokens, queries of seven heads per key
+        dict(name="attend8 blocks", kind="attend8", B=8, T=32, Hq=28, Hkv=4, D=128, S=2048, ps=16, sb=16, causal=False),
+        # one new token each of 32 sequences of very different lengths
+        dict(name="attend8 batch", kind="attend8", B=32, T=1, Hq=32, Hkv=32, D=128, S=8192, ps=32, sb=32, causal=False),
+        # a small odd matrix, as an adapter has them
+        dict(name="quantize8 small", kind="quantize8", K=1000, N=712),
+        # the input projection of a layer, once at load
+        dict(name="quantize8 projection", kind="quantize8", K=4096, N=12288),
+        # the next token of one sequence: the weights' bytes are all there is
+        dict(name="linear8 one token", kind="linear8", M=1, K=4096, N=12288),
+        # three drafts of 32 tokens of one sequence, the projection of 28 over 4 heads
+        dict(name="linear8 drafts", kind="linear8", M=96, K=3584, N=4608),
+        # prompts: the matrix cores bound it
+        dict(name="linear8 prompts", kind="linear8", M=4096, K=4096, N=12288),
+    ]
+
+
+def _log_uniform(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.49)))))))
+
+
+def _eights(rng, lo, hi):
+    return 8 * _log_uniform(rng, lo // 8, hi // 8)
+
+
+def draw(rng):
+    kind = rng.choice(["append8", "attend8", "attend8", "quantize8", "linear8", "linear8"])
+    if kind == "quantize8":
+        K = rng.choice([4096, 3584, 10752, _eights(rng, 64, 12288)])
+        return dict(kind=kind, K=K, N=_eights(rng, 64, 50331648 // K))
+    if kind == "linear8":
+        K = rng.choice([4096, 3584, 10752, 12288, _eights(rng, 64, 16384)])
+        N = rng.choice([4096, 3584, 4608, _eights(rng, 64, 50331648 // K)])
+        N = min(N, 50331648 // K)
+        return dict(kind=kind, M=_log_uniform(rng, 1, 4096), K=K, N=N)
+    Hq, Hkv, D = rng.choice([(32, 32, 128), (32, 8, 128), (28, 4, 128), (16, 16, 64), (4, 4, 64), (8, 1, 64)])
+    ps, sb = rng.choice([(16, 16), (16, 16), (32, 32), (32, 8), (64, 64), (128, 32), (256, 16), (24, 24), (24, 8), (48, 48), (5, 5), (16, 1), (1, 1)])
+    if kind == "append8":
+        B = _log_uniform(rng, 1, 64)
+        return dict(kind=kind, B=B, T=_log_uniform(rng, 1, 8192 // B), Hq=Hq, Hkv=Hkv, D=D, ps=ps, sb=sb,
+                    near=rng.choice([0, _log_uniform(rng, 1, 100000)]), ragged=rng.random() < 0.5)
+    T = rng.choice([1, 1, 1, 2, 4, 5, 8, 16, 24, 32, 64])
+    S = _log_uniform(rng, 1, 65536)
+    # at most as many keys and scores as the largest listed cases have
+    most = max(1, min(64, 33000000 // (S * Hkv * D) * 8, 64000000 // (S * T * Hq)))
+    return dict(kind=kind, B=_log_uniform(rng, 1, most), T=T, Hq=Hq, Hkv=Hkv, D=D, S=S, ps=ps, sb=sb, causal=rng.random() < 0.4)
+
+
+# ---------------------------------------------------------------- 8 bits, in plain operations
+
+def _pow2(byte):
+    """2^(byte - 127) in 32 bits."""
+    return (byte.to(I32) << 23).view(F32)
+
+
+def _scale_byte(amax):
+    """Biased exponent of the smallest power of two that brings `amax` to 448 (in 64 bits: next to a border)."""
+    m, e = torch.frexp(amax.double() / LARGEST)
+    return torch.where(amax > 0, (e.to(I32) - (m == 0.5).to(I32) + 127).clamp(LOWEST, 247), LOWEST).to(U8)
+
+
+def _to8(x, byte):
+    return (x.float() / _pow2(byte)).to(E4)
+
+
+def _blocks8(w):
+    """w [K, N] in blocks of 128 x 128: e4m3 values [N, KP] and the blocks' bytes [ceil(N / 128), KP / 128]."""
+    K, N = w.shape
+    p = F.pad(w.t().float(), (0, -K % BLOCK, 0, -N % BLOCK))
+    p = p.view(p.shape[0] // BLOCK, BLOCK, -1, BLOCK)
+    byte = _scale_byte(p.abs().amax((1, 3)))
+    return _to8(p, byte[:, None, :, None]).view(-1, K + -K % BLOCK)[:N].contiguous(), byte
+
+
+# ---------------------------------------------------------------- inputs
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed))
+    return g
+
+
+def _normal(g, shape, dtype=BF):
+    return torch.randn(shape, generator=g, device=DEV, dtype=dtype)
+
+
+def _ints(g, lo, hi, shape, dtype=I32):
+    return torch.randint(lo, hi, shape, generator=g, device=DEV, dtype=dtype)
+
+
+def _pool8(g, pages, ps, sb, Hkv, D):
+    """Pages as appends leave them: normal values of a size of each block's own, to 448 at most after scaling."""
+    values = torch.empty(pages, ps // sb, sb, Hkv, D, dtype=E4, device=DEV)
+    byte = torch.empty(pages, ps // sb, Hkv, dtype=U8, device=DEV)
+    part = max(1, (1 << 27) // (ps * Hkv * D))
+    for i in range(0, pages, part):
+        n = min(part, pages - i)
+        x = _normal(g, (n, ps // sb, sb, Hkv, D), F32)
+        x *= 2 ** (torch.rand(n, ps // sb, 1, Hkv, 1, generator=g, device=DEV) - 0.5)
+        byte[i:i + n] = _scale_byte(x.abs().amax((2, 4)))
+        values[i:i + n] = _to8(x, byte[i:i + n, :, None, :, None])
+    return values.view(pages, ps, Hkv, D), byte.view(E8)
+
+
+def prepare(case, seed):
+    c, g = case, _gen(seed)
+    s = {"case": c}
+    if c["kind"] == "quantize8":
+        s["w"] = (_normal(g, (c["K"], c["N"]), F32) * c["K"] ** -0.5).to(BF)
+        return s
+    if c["kind"] == "linear8":
+        M, K, N = c["M"], c["K"], c["N"]
+        # activations: rows and channels differ in size, a few channels by far
+        x = _normal(g, (M, K), F32) * 2 ** _normal(g, (M, 1), F32) * 2 ** (0.5 * _normal(g, (1, K), F32))
+        x[:, _ints(g, 0, K, (max(1, K // 500),), torch.int64)] *= 20
+        s["x"] = x.to(BF)
+        s["w8"], byte = _blocks8((_normal(g, (K, N), F32) * K ** -0.5).to(BF))
+        s["w_scale"] = byte.view(E8)
+        return s
+    B, T, Hq, Hkv, D, ps, sb = (c[n] for n in ("B", "T", "Hq", "Hkv", "D", "ps", "sb"))
+    columns = -(-(T + ps if c["kind"] == "append8" else c["S"]) // ps)
+    pages = B * columns + 3  # in random order, a few left free
+    s["table"] = torch.randperm(pages, generator=g, device=DEV)[:B * columns].view(B, columns).to(I32)
+    s["k_pages"], s["k_scale"] = _pool8(g, pages, ps, sb, Hkv, D)
+    s["v_pages"], s["v_scale"] = _pool8(g, pages, ps, sb, Hkv, D)
+    if c["kind"] == "append8":
+        s["qkv"] = _normal(g, (B, T, (Hq + 2 * Hkv) * D))  # the projection's rows: q, k and v heads side by side
+        s["start"] = _ints(g, 0, ps, (B,))
+        s["pos0"] = s["start"] + _ints(g, 0, c["near"] + 1, (B,))
+        s["new"] = _ints(g, 0, T + 1, (B,)) if c["ragged"] else None
+        s["q_out"] = torch.zeros(B, T, Hq, D, dtype=BF, device=DEV)
+        return s
+    s["q"] = _normal(g, (B, T, Hq, D))
+    # the first sequence is the longest, the others have any length up to it
+    s["lens"] = (c["S"] * torch.rand(B, generator=g, device=DEV)).to(I32) + 1
+    s["lens"][0] = c["S"]
+    used = torch.arange(columns, device=DEV) * ps < s["lens"][:, None]
+    s["table"] = torch.where(used, s["table"], -1).to(I32)
+    return s
+
+
+# ---------------------------------------------------------------- one pass
+
+def run(state):
+    kind = state["case"]["kind"]
+    if kind == "append8":
+        return _append_own(state) if own else _append_plain(state)
+    if kind == "attend8":
+        return _attend_own(state) if own else _attend_plain(state)
+    if kind == "quantize8":
+        return _quantize_own(state) if own else _quantize_plain(state)
+    return _linear_own(state) if own else _linear_plain(state)
+
+
+def _split(s):
+    c = s["case"]
+    B, T, Hq, Hkv, D = (c[n] for n in ("B", "T", "Hq", "Hkv", "D"))
+    return (x.view(B, T, -1, D) for x in s["qkv"].split([Hq * D, Hkv * D, Hkv * D], -1))
+
+
+def _cache(s):
+    return {"q": s["q_out"], "k_pages": s["k_pages"], "v_pages": s["v_pages"], "k_scale": s["k_scale"], "v_scale": s["v_scale"]}
+
+
+def _append_own(s):
+    import paper_2608_27514_amd as tsp
+    q, k, v = _split(s)
+    tsp.paged_append8(k, v, s["k_pages"], s["v_pages"], s["k_scale"], s["v_scale"], s["table"], s["start"], q=q, q_out=s["q_out"],
+                      n_new=s["new"], pos0=s["pos0"], rope_theta=THETA)
+    return _cache(s)
+
+
+def _attend_own(s):
+    import paper_2608_27514_amd as tsp
+    return tsp.paged_attn8(s["q"], s["k_pages"], s["v_pages"], s["k_scale"], s["v_scale"], s["table"], s["lens"], causal=s["case"]["causal"])
+
+
+def _quantize_own(s):
+    import paper_2608_27514_amd as tsp
+    return tsp.quantize8(s["w"])
+
+
+def _linear_own(s):
+    import paper_2608_27514_amd as tsp
+    return tsp.linear8(s["x"], s["w8"], s["w_scale"])
+
+
+def _append_plain(s):
+    B, T, Hkv, D, ps, sb = (s["case"][n] for n in ("B", "T", "Hkv", "D", "ps", "sb"))
+    q, k, v = _split(s)
+    t = torch.arange(T, device=DEV)
+    half = D // 2
+    # far positions: the angle needs 64 bits
+    angle = (s["pos0"][:, None] + t)[..., None].double() * THETA ** (-torch.arange(half, device=DEV, dtype=F64) / half)
+    cos, sin = angle.cos().float()[:, :, None], angle.sin().float()[:, :, None]
+
+    def rotate(x):
+        a, b = x[..., :half].float(), x[..., half:].float()
+        return torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+
+    start, table = s["start"][:, None].long(), s["table"].long()
+    new = s["new"][:, None] if s["new"] is not None else torch.full((B, 1), T, device=DEV)
+    valid = t < new
+    s["q_out"][valid] = rotate(q)[valid].to(BF)
+    # blocks of tokens that the call touches, counted from the sequence's first; the rows of the first one before the call's
+    at = start + t
+    blocks = (T + sb - 2) // sb + 1
+    j = torch.arange(blocks, device=DEV)
+    block = start // sb + j
+    touched = (new > 0) & (block * sb < start + new)
+    page_of = table.gather(1, (block * sb // ps).clamp(max=table.shape[1] - 1))
+    row = torch.arange(sb, device=DEV)
+    before = (new > 0) & (start // sb * sb + row < start)
+    first_row = start // sb * sb % ps + row
+
+    def store(x, pages, scale):
+        pages, scale = pages.view(U8), scale.view(U8)
+        size = torch.where(valid[..., None], x.abs().amax(-1), 0.0)
+        amax = torch.zeros(B, blocks, Hkv, device=DEV)
+        amax.scatter_reduce_(1, (at // sb - start // sb)[..., None].expand(-1, -1, Hkv), size, "amax")
+        byte = _scale_byte(amax)
+        old = scale[page_of, block * sb % ps // sb]
+        byte = torch.where((before.any(1)[:, None] & (j == 0))[..., None], torch.maximum(byte, old), byte)
+        kept = pages[page_of[:, :1], first_row]
+        ratio = (_pow2(old[:, :1]) / _pow2(byte[:, :1]))[..., None]
+        kept = (kept.view(E4).float() * ratio).to(E4).view(U8)
+        pages[page_of[:, :1].expand(-1, sb)[before], first_row[before]] = kept[before]
+        values = _to8(x, byte.gather(1, (at // sb - start // sb)[..., None].expand(-1, -1, Hkv))[..., None])
+        pages[table.gather(1, at // ps)[valid], (at % ps)[valid]] = values.view(U8)[valid]
+        scale[page_of[touched], (block * sb % ps // sb)[touched]] = byte[touched]
+
+    store(rotate(k), s["k_pages"], s["k_scale"])
+    store(v.float(), s["v_pages"], s["v_scale"])
+    return _cache(s)
+
+
+def _gathered(s, pages, scale):
+    """The sequences' values [B, S, Hkv, D] in 32 bits."""
+    B, Hkv, D, S, sb = (s["case"][n] for n in ("B", "Hkv", "D", "S", "sb"))
+    page = s["table"].clamp(min=0).long()
+    x = pages.view(U8)[page].view(E4).float().view(B, -1, sb, Hkv, D)
+    return (x * scale.view(U8)[page].view(E8).float().view(B, -1, 1, Hkv, 1)).view(B, -1, Hkv, D)[:, :S]
+
+
+def _attend_plain(s):
+    B, T, Hq, Hkv, D, S = (s["case"][n] for n in ("B", "T", "Hq", "Hkv", "D", "S"))
+    G = Hq // Hkv
+    k = _gathered(s, s["k_pages"], s["k_scale"]).permute(0, 2, 3, 1).contiguous()
+    v = _gathered(s, s["v_pages"], s["v_scale"]).permute(0, 2, 1, 3).contiguous()
+    q = s["q"].view(B, T, Hkv, G, D).permute(0, 2, 1, 3, 4).reshape(B, Hkv, T * G, D).float()
+    seen = s["lens"][:, None].expand(B, T)
+    if s["case"]["causal"]:
+        seen = seen - T + 1 + torch.arange(T, device=DEV)
+    hidden = torch.arange(S, device=DEV) >= seen.repeat_interleave(G, 1)[:, None, :, None]  # [B, 1, T G, S]
+    x = (q @ k).mul_(D ** -0.5).masked_fill_(hidden, -math.inf)
+    top = x.amax(-1, keepdim=True)
+    x.sub_(torch.where(top == -math.inf, 0.0, top)).exp_()
+    out = (x @ v) / x.sum(-1, keepdim=True).clamp(min=1e-30)  # a row that sees nothing: 0
+    return out.view(B, Hkv, T, G, D).permute(0, 2, 1, 3, 4).reshape(B, T, Hq, D).to(BF)
+
+
+def _quantize_plain(s):
+    w8, byte = _blocks8(s["w"])
+    return w8, byte.view(E8)
+
+
+def _linear_plain(s):
+    K, N = s["case"]["K"], s["case"]["N"]
+    x = F.pad(s["x"].float(), (0, -K % BLOCK)).unflatten(-1, (-1, BLOCK))
+    byte = _scale_byte(x.abs().amax(-1))[..., None]
+    x = (_to8(x, byte).float() * _pow2(byte)).flatten(-2)
+    w = s["w8"].float() * s["w_scale"].float().repeat_interleave(BLOCK, 0)[:N].repeat_interleave(BLOCK, 1)
+    return (x @ w.t()).to(BF)
+
+
+# ---------------------------------------------------------------- what a pass cannot do without
+
+def work(case):
+    c = case
+    if c["kind"] == "quantize8":
+        return dict(bytes=3 * c["K"] * c["N"], flops=2 * c["K"] * c["N"])
+    if c["kind"] == "linear8":
+        M, K, N = c["M"], c["K"], c["N"]
+        return dict(bytes=2 * M * K + K * N + 2 * M * N, flops=2 * M * K * N)
+    B, T, Hq, Hkv, D, ps, sb = (c[n] for n in ("B", "T", "Hq", "Hkv", "D", "ps", "sb"))
+    if c["kind"] == "append8":
+        tokens = B * T // 2 if c["ragged"] else B * T
+        return dict(bytes=tokens * (4 * Hq + 6 * Hkv) * D + B * (12 + 4 * -(-T // ps)) + 2 * tokens // sb * Hkv, flops=3 * tokens * (Hq + 2 * Hkv) * D)
+    keys = c["S"] + (B - 1) * c["S"] // 2
+    return dict(bytes=2 * keys * Hkv * D + 4 * B * T * Hq * D + 4 * (B + keys // ps) + 2 * keys // sb * Hkv, flops=4 * keys * T * Hq * D)
+
+
+# ---------------------------------------------------------------- the definition, in 64 bits
+
+def exact(case, seed):
+    if case["kind"] == "linear8" and case["M"] * case["K"] * case["N"] > 300e9:
+        return None
+    s = prepare(case, seed)
+    return {"append8": _append_exact, "attend8": _attend_exact, "quantize8": _quantize_exact, "linear8": _linear_exact}[case["kind"]](s)
+
+
+def _two(e):
+    """2^e, exactly (a power's last bit may be off, and many values lie halfway between two of e4m3)."""
+    return ((e.long() + 1023) << 52).view(F64)
+
+
+def _exponent(x):
+    """The smallest e, -100 at least, with every |value| of the tensor's last axis at 448 2^e at most."""
+    e = torch.full(x.shape[:-1], -100, device=DEV)
+    amax = x.abs().max(-1).values
+    for up in (64, 32, 16, 8, 4, 2, 1):  # by halving: e + up - 1 does not do
+        e = torch.where(amax > LARGEST * _two(e + (up - 1)), e + up, e)
+    return e
+
+
+def _e4m3(x):
+    """Nearest value with 4 significant bits, even on ties, multiples of 2^-9 at least."""
+    step = _two(torch.frexp(x).exponent.clamp(min=-5) - 4)
+    return torch.round(x / step) * step
+
+
+def _append_exact(s):
+    c = s["case"]
+    B, T, Hq, Hkv, D, ps, sb = (c[n] for n in ("B", "T", "Hq", "Hkv", "D", "ps", "sb"))
+    rows = s["qkv"].double().view(B, T, Hq + 2 * Hkv, D)
+    out = {n: t.double() for n, t in _cache(s).items()}
+    freq = torch.tensor([THETA ** (-2.0 * d / D) for d in range(D // 2)], dtype=F64, device=DEV)
+    for b in range(B):
+        new, start = T if s["new"] is None else int(s["new"][b]), int(s["start"][b])
+        if new == 0:
+            continue
+        turn = torch.outer(torch.arange(T, device=DEV).double() + float(s["pos0"][b]), freq)
+        z = torch.complex(rows[b, :, :Hq + Hkv, :D // 2].contiguous(), rows[b, :, :Hq + Hkv, D // 2:].contiguous())
+        z = z * torch.polar(torch.ones_like(turn), turn)[:, None]
+        z = torch.cat([z.real, z.imag], -1)[:new]
+        out["q"][b, :new] = z[:, :Hq]
+        # whole blocks: the rows before the call's, its own, nothing behind them
+        lead, n = start % sb, -(-(start % sb + new) // sb)
+        cell = torch.arange(start - lead, start - lead + n * sb, device=DEV)
+        page, r = s["table"][b].long()[(cell // ps).clamp(max=s["table"].shape[1] - 1)], cell % ps
+        for name, x in (("k", z[:, Hq:]), ("v", rows[b, :new, Hq + Hkv:])):
+            pages, scale = out[name + "_pages"], out[name + "_scale"]
+            x = F.pad(x, (0, 0, 0, 0, lead, n * sb - lead - new))
+            e = _exponent(x.view(n, sb, Hkv, D).transpose(1, 2).flatten(2))
+            if lead:
+                was = scale[page[0], r[0] // sb]
+                e[0] = torch.maximum(e[0], torch.frexp(was).exponent - 1)
+                x[:lead] = pages[page[:lead], r[:lead]] * was[:, None]
+            x = _e4m3(x / _two(e).repeat_interleave(sb, 0)[..., None])
+            pages[page[:lead + new], r[:lead + new]] = x[:lead + new]
+            scale[page[::sb], r[::sb] // sb] = _two(e)
+    return out
+
+
+def _attend_exact(s):
+    B, T, Hq, Hkv, D, ps, sb = (s["case"][n] for n in ("B", "T", "Hq", "Hkv", "D", "ps", "sb"))
+    out = torch.zeros(B, T, Hq, D, dtype=F64, device=DEV)
+    for b in range(B):
+        n = int(s["lens"][b])
+        pages = s["table"][b, :-(-n // ps)].long()
+        k, v = ((x.view(U8)[pages].view(E4).double() * z.view(U8)[pages].view(E8).double().repeat_interleave(sb, 1)[..., None]).flatten(0, 1)[:n]
+                for x, z in ((s["k_pages"], s["k_scale"]), (s["v_pages"], s["v_scale"])))
+        for h in range(Hq):
+            g = h * Hkv // Hq
+            x = s["q"][b, :, h].double() @ k[:, g].t().contiguous() / math.sqrt(D)
+            if s["case"]["causal"]:  # query t is the sequence's token n - T + t
+                x[torch.arange(n, device=DEV)[None] > torch.arange(n - T, n, device=DEV)[:, None]] = -math.inf
+            out[b, :, h] = torch.softmax(x, -1).nan_to_num(0.0) @ v[:, g]
+    return out
+
+
+def _quantize_exact(s):
+    w = s["w"].double()
+    K, N = w.shape
+    w8 = torch.zeros(N, -(-K // BLOCK) * BLOCK, dtype=F64, device=DEV)
+    scale = torch.zeros(-(-N // BLOCK), -(-K // BLOCK), dtype=F64, device=DEV)
+    for n in range(0, N, BLOCK):
+        for k in range(0, K, BLOCK):
+            part = w[k:k + BLOCK, n:n + BLOCK]
+            unit = _two(_exponent(part.flatten()))
+            scale[n // BLOCK, k // BLOCK] = unit
+            w8[n:n + BLOCK, k:k + BLOCK][:, :part.shape[0]] = _e4m3(part / unit).t()
+    return w8, scale
+
+
+def _linear_exact(s):
+    K, N = s["case"]["K"], s["case"]["N"]
+    y = torch.zeros(s["x"].shape[0], N, dtype=F64, device=DEV)
+    for k in range(0, K, BLOCK):
+        x = s["x"][:, k:k + BLOCK].double()
+        unit = _two(_exponent(x))[:, None]
+        column = s["w_scale"][:, k // BLOCK].double().repeat_interleave(BLOCK)[:N]
+        y += (_e4m3(x / unit) * unit) @ s["w8"][:, k:k + x.shape[1]].double().t().contiguous() * column
+    return y
