@@ -24,7 +24,7 @@ DEV = "cuda"
 BF, F32, F64, I32, U8 = torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.uint8
 E4, E8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 THETA = 500000.0
-BLOCK, LARGEST, LOWEST = 128, 448.0, 27  # values of a weight block's side; the largest e4m3; the byte of 2^-100
+BLOCK, SLAB, LARGEST, LOWEST = 128, 64, 448.0, 27  # a weight block's side; a slab's k; the largest e4m3; the byte of 2^-100
 
 
 def listed():
@@ -105,12 +105,13 @@ def _to8(x, byte):
 
 
 def _blocks8(w):
-    """w [K, N] in blocks of 128 x 128: e4m3 values [N, KP] and the blocks' bytes [ceil(N / 128), KP / 128]."""
+    """w [K, N] in blocks of 128 x 128: e4m3 values in slabs of 64 of k, [KP / 64, N, 64], and the blocks' bytes [ceil(N / 128), KP / 128]."""
     K, N = w.shape
     p = F.pad(w.t().float(), (0, -K % BLOCK, 0, -N % BLOCK))
     p = p.view(p.shape[0] // BLOCK, BLOCK, -1, BLOCK)
     byte = _scale_byte(p.abs().amax((1, 3)))
-    return _to8(p, byte[:, None, :, None]).view(-1, K + -K % BLOCK)[:N].contiguous(), byte
+    values = _to8(p, byte[:, None, :, None]).view(-1, K + -K % BLOCK)[:N]
+    return values.view(U8).unflatten(1, (-1, SLAB)).transpose(0, 1).contiguous().view(E4), byte
 
 
 # ---------------------------------------------------------------- inputs
@@ -310,7 +311,7 @@ def _linear_plain(s):
     x = F.pad(s["x"].float(), (0, -K % BLOCK)).unflatten(-1, (-1, BLOCK))
     byte = _scale_byte(x.abs().amax(-1))[..., None]
     x = (_to8(x, byte).float() * _pow2(byte)).flatten(-2)
-    w = s["w8"].float() * s["w_scale"].float().repeat_interleave(BLOCK, 0)[:N].repeat_interleave(BLOCK, 1)
+    w = s["w8"].float().transpose(0, 1).reshape(N, -1) * s["w_scale"].float().repeat_interleave(BLOCK, 0)[:N].repeat_interleave(BLOCK, 1)
     return (x @ w.t()).to(BF)
 
 
@@ -421,7 +422,7 @@ def _quantize_exact(s):
             unit = _two(_exponent(part.flatten()))
             scale[n // BLOCK, k // BLOCK] = unit
             w8[n:n + BLOCK, k:k + BLOCK][:, :part.shape[0]] = _e4m3(part / unit).t()
-    return w8, scale
+    return w8.unflatten(1, (-1, SLAB)).transpose(0, 1), scale
 
 
 def _linear_exact(s):
@@ -431,5 +432,6 @@ def _linear_exact(s):
         x = s["x"][:, k:k + BLOCK].double()
         unit = _two(_exponent(x))[:, None]
         column = s["w_scale"][:, k // BLOCK].double().repeat_interleave(BLOCK)[:N]
-        y += (_e4m3(x / unit) * unit) @ s["w8"][:, k:k + x.shape[1]].double().t().contiguous() * column
+        w = torch.cat([s["w8"][i].double() for i in range(k // SLAB, k // SLAB + BLOCK // SLAB)], 1)
+        y += (_e4m3(x / unit) * unit) @ w[:, :x.shape[1]].t().contiguous() * column
     return y
