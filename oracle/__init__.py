@@ -22,6 +22,8 @@ Decoding for Diffusion LLMs):
   same layer over whole sequences that refreshes the dual cache (App. A).
 * :mod:`oracle.paged`      -- appending rotated keys to a paged key-value cache, and
   attention over it.
+* :mod:`oracle.eight`      -- values in 8 bits with power-of-two scales: the paged cache,
+  weight matrices and the product with them.
 * :mod:`oracle.adjust`     -- confidences and candidates of logits under penalties,
   biases and masks.
 * :mod:`oracle.brute`      -- scalar-loop re-derivations used only to pin the
@@ -53,6 +55,7 @@ from .tree import build_tree, build_tree_batch, gather_state_scores, level_width
 from .layer import bf16_round, full_attention, linear, refresh_layer, verify_layer  # noqa: E402
 from .interblock import block_top1_confidence, interblock_trigger, interblock_trigger_batch, joint_peers  # noqa: E402
 from .paged import paged_append, paged_attention, rotate  # noqa: E402
+from . import eight  # noqa: E402
 from .adjust import adjust_logits, confidence_topk_adjusted  # noqa: E402
 
 __all__ = [
@@ -80,6 +83,7 @@ __all__ = [
     "rotate",
     "paged_append",
     "paged_attention",
+    "eight",
     "adjust_logits",
     "confidence_topk_adjusted",
 ]

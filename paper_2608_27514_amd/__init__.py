@@ -33,6 +33,11 @@ For serving sequences of different lengths and requests with their own rules:
   paged key-value cache; :func:`paged_attn` attends to it.
 * :func:`confidence_topk_adjusted` -- :func:`confidence_topk` under penalties for repeated tokens,
   biases and grammar masks.
+
+and in 8 bits (e4m3 with a power-of-two scale per block), for steps that the cache's and the weights' bytes bound:
+
+* :func:`paged_append8` and :func:`paged_attn8` -- the paged cache with a scale per block of tokens and head.
+* :func:`quantize8` -- a weight matrix with a scale per block of 128 x 128, once; :func:`linear8` multiplies by it.
 """
 
 from ._lib import (  # noqa: F401
@@ -60,14 +65,20 @@ from ._lib import (  # noqa: F401
     joint_peers,
     layer_workspace_size,
     linear,
+    linear8,
+    linear8_workspace_size,
     linear_workspace_size,
     refresh_layer,
     refresh_layer_workspace_size,
     verify_layer,
     load,
     paged_append,
+    paged_append8,
     paged_attn,
+    paged_attn8,
+    paged_attn8_workspace_size,
     paged_attn_workspace_size,
+    quantize8,
     tree_max_nodes,
     verify_attn,
     verify_attn_workspace_size,

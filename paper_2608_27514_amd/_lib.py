@@ -136,6 +136,16 @@ EXPORTS = {
     "traj_confidence_topk_adjusted": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
                                                        ctypes.POINTER(LogitsShape), ctypes.POINTER(LogitAdjust),
                                                        ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "traj_paged_append_eight": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p] * 9 +
+                           [ctypes.POINTER(PagedShape), ctypes.c_int32, ctypes.c_float, ctypes.c_void_p]),
+    "traj_paged_attn_eight_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(PagedShape), ctypes.c_int32]),
+    "traj_paged_attn_eight": (ctypes.c_int32, [ctypes.c_void_p] * 9 + [ctypes.POINTER(PagedShape), ctypes.c_int32, ctypes.c_float,
+                                                                  ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t,
+                                                                  ctypes.c_void_p]),
+    "traj_quantize_eight": (ctypes.c_int32, [ctypes.c_void_p] * 3 + [ctypes.c_int64] * 2 + [ctypes.c_void_p]),
+    "traj_linear_eight_workspace_size": (ctypes.c_size_t, [ctypes.c_int64] * 3),
+    "traj_linear_eight": (ctypes.c_int32, [ctypes.c_void_p] * 4 + [ctypes.c_int64] * 3 +
+                     [ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "traj_status_string": (ctypes.c_char_p, [ctypes.c_int32]),
     "traj_version": (ctypes.c_char_p, []),
     "traj_get_device_status": (ctypes.c_int32, [ctypes.POINTER(ctypes.c_int32), ctypes.c_int32, ctypes.c_void_p]),
@@ -628,7 +638,7 @@ def _paged_struct(B, T, Hq, pages, strides, table, table_strides):
     _int32(B=B, T=T, heads=Hq, pages=pages[0], page_size=pages[1], kv_heads=pages[2], head_size=pages[3], max_pages=table[1])
     # a dimension of one entry has no stride that matters
     sh = PagedShape(B, T, Hq, pages[2], pages[3], pages[0], pages[1], table[1], max(table_strides[0], table[1]) if B <= 1 else table_strides[0],
-                    strides[0] if pages[0] > 1 else 8, strides[1] if pages[1] > 1 else 8, strides[2] if pages[2] > 1 else 8)
+                    strides[0] if pages[0] > 1 else 16, strides[1] if pages[1] > 1 else 16, strides[2] if pages[2] > 1 else 16)
     return sh, ctypes.byref(sh)
 
 
@@ -637,13 +647,13 @@ def _paged_workspace(*sizes):
     return int(_lib().traj_paged_attn_workspace_size(_paged_struct(*sizes)[1]))
 
 
-def _paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev):
+def _paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev, element=torch.bfloat16):
     """Checks the pools and the table; returns what :func:`_paged_struct` takes."""
-    tensor, bf16 = torch.Tensor, torch.bfloat16
-    if not (isinstance(k_pages, tensor) and k_pages.dtype is bf16 and k_pages.get_device() == dev and isinstance(v_pages, tensor)
-            and v_pages.dtype is bf16 and v_pages.get_device() == dev and isinstance(page_table, tensor)
+    tensor = torch.Tensor
+    if not (isinstance(k_pages, tensor) and k_pages.dtype is element and k_pages.get_device() == dev and isinstance(v_pages, tensor)
+            and v_pages.dtype is element and v_pages.get_device() == dev and isinstance(page_table, tensor)
             and page_table.dtype is torch.int32 and page_table.get_device() == dev):
-        for t, n, dt in ((k_pages, "k_pages", bf16), (v_pages, "v_pages", bf16), (page_table, "page_table", torch.int32)):
+        for t, n, dt in ((k_pages, "k_pages", element), (v_pages, "v_pages", element), (page_table, "page_table", torch.int32)):
             _here(t, n, dev)
             if t.dtype is not dt:
                 raise TypeError(f"{n} must be {dt}, got {t.dtype}")
@@ -668,6 +678,27 @@ def _token_rows(t, name, shape, dev):
     return t.data_ptr(), row
 
 
+def _append_rows(k, v, q, q_out, n_new, dev, stream):
+    """Checks the new tokens' rows of an append call; returns their addresses and strides, and q_out (allocated when None)."""
+    shape = k.shape
+    kp, ks = _token_rows(k, "k", shape, dev)
+    vp, vs = _token_rows(v, "v", shape, dev)
+    qp, qs, qop = None, 0, None
+    if q is not None:
+        shape = shape[:2] + q.shape[2:3] + shape[3:]
+        qp, qs = _token_rows(q, "q", shape, dev)
+        if q_out is None:
+            if n_new is None:
+                q_out = _empty(shape, torch.bfloat16, q.device, stream)
+            else:
+                with torch.cuda.stream(stream):  # None: the current one
+                    q_out = torch.zeros(shape, dtype=torch.bfloat16, device=q.device)
+        qop = _arg(q_out, "q_out", torch.bfloat16, shape, dev)
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    return kp, ks, vp, vs, qp, qs, qop, q_out
+
+
 def paged_append(k, v, k_pages, v_pages, page_table, start, q=None, q_out=None, n_new=None, pos0=None,
                  rope_theta=500000.0, stream=None):
     """Rotates the new tokens' keys (and queries) by position and writes keys and values into the pages.
@@ -683,22 +714,8 @@ def paged_append(k, v, k_pages, v_pages, page_table, start, q=None, q_out=None, 
     sh, ref = _paged_struct(*_paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev))
     if sh.Hkv != Hkv or sh.D != D:
         raise ValueError(f"k has {Hkv} heads of {D}, the pages {sh.Hkv} of {sh.D}")
-    shape = (B, T, Hkv, D)
-    kp, ks = _token_rows(k, "k", shape, dev)
-    vp, vs = _token_rows(v, "v", shape, dev)
-    qp, qs, qop, i32, per_seq = None, 0, None, torch.int32, (B,)
-    if q is not None:
-        shape = (B, T, Hq, D)
-        qp, qs = _token_rows(q, "q", shape, dev)
-        if q_out is None:
-            if n_new is None:
-                q_out = _empty(shape, torch.bfloat16, q.device, stream)
-            else:
-                with torch.cuda.stream(stream):  # None: the current one
-                    q_out = torch.zeros(shape, dtype=torch.bfloat16, device=q.device)
-        qop = _arg(q_out, "q_out", torch.bfloat16, shape, dev)
-    elif q_out is not None:
-        raise ValueError("q_out needs q")
+    kp, ks, vp, vs, qp, qs, qop, q_out = _append_rows(k, v, q, q_out, n_new, dev, stream)
+    i32, per_seq = torch.int32, (B,)
     st = _lib().traj_paged_append(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
                                   _arg(start, "start", i32, per_seq, dev),
                                   None if n_new is None else _arg(n_new, "n_new", i32, per_seq, dev),
@@ -740,6 +757,142 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, out=None, scale=0.0, causa
     if st != TRAJ_OK:
         _check(st, "traj_paged_attn")
     return out
+
+
+# ---------------------------------------------------------------- 8 bits
+E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
+def _scale_block(pages, k_scale, v_scale, dev):
+    """Checks the scales of pools of this shape; returns (address, address, tokens of a scale)."""
+    blocks = k_scale.shape[1] if k_scale.dim() == 3 else 0
+    if blocks < 1 or pages[1] % blocks:
+        raise ValueError(f"k_scale must be [pages, blocks, Hkv] with blocks dividing the page's {pages[1]} tokens")
+    shape = (pages[0], blocks, pages[2])
+    return _arg(k_scale, "k_scale", E8M0, shape, dev), _arg(v_scale, "v_scale", E8M0, shape, dev), pages[1] // blocks
+
+
+def paged_append8(k, v, k_pages, v_pages, k_scale, v_scale, page_table, start, q=None, q_out=None, n_new=None, pos0=None,
+                  rope_theta=500000.0, stream=None):
+    """:func:`paged_append` to a cache in 8 bits: k_pages / v_pages [pages, page_size, Hkv, D] float8_e4m3fn, and k_scale /
+    v_scale [pages, blocks, Hkv] float8_e8m0fnu, a scale for each block of page_size / blocks tokens (at most 64) and head.
+    A block's scale is the smallest power of two that brings its rows to 448 at most.  Rows of a block before start[b] keep
+    their values (rounded again where the scale grows), rows behind the call's last token do not."""
+    B, T, Hkv, D = k.shape
+    Hq = q.shape[2] if q is not None else Hkv
+    dev = _current()
+    sh, ref = _paged_struct(*_paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev, E4M3))
+    ksp, vsp, sb = _scale_block(k_pages.shape, k_scale, v_scale, dev)
+    if sh.Hkv != Hkv or sh.D != D:
+        raise ValueError(f"k has {Hkv} heads of {D}, the pages {sh.Hkv} of {sh.D}")
+    kp, ks, vp, vs, qp, qs, qop, q_out = _append_rows(k, v, q, q_out, n_new, dev, stream)
+    i32, per_seq = torch.int32, (B,)
+    st = _lib().traj_paged_append_eight(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), ksp, vsp, page_table.data_ptr(),
+                                   _arg(start, "start", i32, per_seq, dev),
+                                   None if n_new is None else _arg(n_new, "n_new", i32, per_seq, dev),
+                                   None if pos0 is None else _arg(pos0, "pos0", i32, per_seq, dev), ref, sb, rope_theta, _stream(stream))
+    if st != TRAJ_OK:
+        _check(st, "traj_paged_append_eight")
+    return q_out
+
+
+@functools.lru_cache(maxsize=1024)
+def _paged8_workspace(sb, *sizes):
+    return int(_lib().traj_paged_attn_eight_workspace_size(_paged_struct(*sizes)[1], sb))
+
+
+def paged_attn8_workspace_size(q, k_pages, v_pages, k_scale, v_scale, page_table):
+    dev = _current()
+    sizes = _paged_sizes(*q.shape[:3], k_pages, v_pages, page_table, dev, E4M3)
+    return _paged8_workspace(_scale_block(k_pages.shape, k_scale, v_scale, dev)[2], *sizes)
+
+
+def paged_attn8(q, k_pages, v_pages, k_scale, v_scale, page_table, lens, out=None, scale=0.0, causal=False, n_new=None,
+                workspace=None, stream=None):
+    """:func:`paged_attn` over a cache in 8 bits (pools and scales as :func:`paged_append8`)."""
+    shape = B, T, Hq, D = q.shape
+    bf16 = torch.bfloat16
+    dev = _current()
+    qp = _arg(q, "q", bf16, shape, dev)
+    sizes = _paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev, E4M3)
+    sh, ref = _paged_struct(*sizes)
+    ksp, vsp, sb = _scale_block(k_pages.shape, k_scale, v_scale, dev)
+    if sh.D != D:
+        raise ValueError(f"q has heads of {D}, the pages of {sh.D}")
+    if out is None:
+        out = _empty(shape, bf16, q.device, stream)
+    ws, ws_bytes = None, 0
+    if workspace is None:
+        ws_bytes = _paged8_workspace(sb, *sizes)
+        if ws_bytes > 0:
+            workspace = _empty((ws_bytes,), torch.uint8, q.device, stream)
+            ws = workspace.data_ptr()
+    else:
+        ws, ws_bytes = _room(workspace, dev)
+    st = _lib().traj_paged_attn_eight(qp, k_pages.data_ptr(), v_pages.data_ptr(), ksp, vsp, page_table.data_ptr(),
+                                 _arg(lens, "lens", torch.int32, (B,), dev), None if n_new is None else _arg(n_new, "n_new", torch.int32, (B,), dev),
+                                 _arg(out, "out", bf16, shape, dev), ref, sb, scale, 1 if causal else 0, ws, ws_bytes, _stream(stream))
+    if st != TRAJ_OK:
+        _check(st, "traj_paged_attn_eight")
+    return out
+
+
+def _weight8_shapes(K, N):
+    KP = -(-K // 128) * 128
+    return (KP // 64, N, 64), (-(-N // 128), KP // 128)
+
+
+def quantize8(w, w8=None, w_scale=None, stream=None):
+    """A weight matrix w [K, N] (bf16) in 8 bits for :func:`linear8`: returns (w8, w_scale), w8 [KP / 64, N, 64]
+    float8_e4m3fn holding value (k, n) at [k // 64, n, k % 64] (KP: K rounded up to a multiple of 128), w_scale
+    [ceil(N / 128), KP / 128] float8_e8m0fnu a power of two per block of 128 x 128."""
+    dev = _current()
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+        raise ValueError("w must be [K, N]")
+    K, N = w.shape
+    wp = _arg(w, "w", torch.bfloat16, w.shape, dev)
+    values, scales = _weight8_shapes(K, N)
+    if w8 is None:
+        w8 = _empty(values, E4M3, w.device, stream)
+    if w_scale is None:
+        w_scale = _empty(scales, E8M0, w.device, stream)
+    _check(_lib().traj_quantize_eight(wp, _arg(w8, "w8", E4M3, values, dev), _arg(w_scale, "w_scale", E8M0, scales, dev), K, N, _stream(stream)),
+           "traj_quantize_eight")
+    return w8, w_scale
+
+
+@functools.lru_cache(maxsize=1024)
+def linear8_workspace_size(M, K, N):
+    return int(_lib().traj_linear_eight_workspace_size(M, K, N))
+
+
+def linear8(x, w8, w_scale, y=None, accumulate=False, workspace=None, stream=None):
+    """:func:`linear` with weights in 8 bits, as :func:`quantize8` makes them: y = x @ w (+ y when accumulate) for bf16 x
+    [..., K], each row's blocks of 128 of k taken to 8 bits with a power of two; returns y [..., N] bf16."""
+    dev = _current()
+    xp = _arg(x, "x", torch.bfloat16, x.shape, dev)
+    if x.dim() < 1 or w8.dim() != 3:
+        raise ValueError("x must be [..., K] and w8 [KP / 64, N, 64]")
+    K, N = x.shape[-1], w8.shape[1]
+    values, scales = _weight8_shapes(K, N)
+    wp, sp = _arg(w8, "w8", E4M3, values, dev), _arg(w_scale, "w_scale", E8M0, scales, dev)
+    M = x.numel() // max(K, 1)
+    shape = x.shape[:-1] + (N,)
+    if y is None:
+        if accumulate:
+            raise ValueError("accumulate needs y")
+        y = _empty(shape, torch.bfloat16, x.device, stream)
+    yp = _arg(y, "y", torch.bfloat16, shape, dev)
+    if workspace is None:
+        ws_bytes = linear8_workspace_size(M, K, N)
+        workspace = _empty((ws_bytes,), torch.uint8, x.device, stream)
+        ws = workspace.data_ptr()
+    else:
+        ws, ws_bytes = _room(workspace, dev)
+    st = _lib().traj_linear_eight(xp, wp, sp, yp, M, K, N, 1 if accumulate else 0, ws, ws_bytes, _stream(stream))
+    if st != TRAJ_OK:
+        _check(st, "traj_linear_eight")
+    return y
 
 
 # ---------------------------------------------------------------- adjusted logits

@@ -201,13 +201,15 @@ __device__ __forceinline__ int paged_new(const PagedAttnParams& P, int b, bool r
     return n;
 }
 
-// Keys per workgroup.  Every wave computes the same from the same lengths (whole numbers, quotients by powers of two).
+// Keys per workgroup, a multiple of GRANULE.  Every wave computes the same from the same lengths (whole numbers, quotients
+// by powers of two).
+template <int GRANULE>
 __device__ __forceinline__ int paged_chunk(int64_t total, int units, int capacity) {
-    const double work = (double)total * (double)units / kPagedGranule;
-    double per = fmax(work / kPagedMostWgs, fmin(work / kPagedFillWgs, (double)(kPagedChunk / kPagedGranule)));
-    per = fmin(per, (double)(capacity / kPagedGranule + 1));
+    const double work = (double)total * (double)units / GRANULE;
+    double per = fmax(work / kPagedMostWgs, fmin(work / kPagedFillWgs, (double)(kPagedChunk / GRANULE)));
+    per = fmin(per, (double)(capacity / GRANULE + 1));
     const int granules = (int)ceil(per);
-    return kPagedGranule * (granules < 1 ? 1 : granules);
+    return GRANULE * (granules < 1 ? 1 : granules);
 }
 
 // Workgroup i runs on XCD i % 8.  The row tiles of one (slot, kv head) follow each other on one XCD, whose L2
@@ -228,6 +230,7 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams& P) {
 
 // The range that the workgroup's slot stands for; false where the batch has fewer.  All lanes of the wave take part.
 // Lengths out of range are reported once per sequence where each workgroup looks at its own alone, else by workgroup 0.
+template <int GRANULE = kPagedGranule>
 __device__ __forceinline__ bool paged_range(const PagedAttnParams& P, const PagedPlace& w, PagedRange& r) {
     const int lane = threadIdx.x & 63, slot = w.slot;
     if (P.single) {
@@ -245,7 +248,7 @@ __device__ __forceinline__ bool paged_range(const PagedAttnParams& P, const Page
         lane_pair64(t, total, x, y);
         total = x + y;
     }
-    const int chunk = __builtin_amdgcn_readfirstlane(paged_chunk((int64_t)total, P.units, P.cache.capacity));
+    const int chunk = __builtin_amdgcn_readfirstlane(paged_chunk<GRANULE>((int64_t)total, P.units, P.cache.capacity));
     int base = 0;
     for (int i0 = 0; i0 < P.B; i0 += 64) {
         const int i = i0 + lane;

@@ -17,6 +17,8 @@
 #include "interblock.hpp"
 #include "layer.hpp"
 #include "paged.hpp"
+#include "paged8.hpp"
+#include "gemm8.hpp"
 #include "tree.hpp"
 #include "verify_attn.hpp"
 #include "verify_attn16.hpp"
@@ -633,14 +635,165 @@ void launch_paged_attn(const PagedAttnParams& p, int64_t wgs, hipStream_t st) {
 }
 
 template <int D>
-void launch_paged(const PagedAttnParams& p, int64_t wgs, int64_t slots, bool uniform, hipStream_t st) {
-    uniform ? launch_paged_attn<D, true>(p, wgs, st) : launch_paged_attn<D, false>(p, wgs, st);
+void launch_paged_join(const PagedAttnParams& p, int64_t slots, hipStream_t st) {
     if (p.single) return;
     const int64_t rows = (int64_t)p.B * p.T * p.Hq;
     if (slots >= kPagedWideJoin * p.B && rows <= kPagedWideJoinRows)
         hipLaunchKernelGGL((paged_join_kernel<D, 512>), dim3((unsigned)rows), dim3(512), 0, st, p);
     else
         hipLaunchKernelGGL((paged_join_kernel<D, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
+}
+
+template <int D>
+void launch_paged(const PagedAttnParams& p, int64_t wgs, int64_t slots, bool uniform, hipStream_t st) {
+    uniform ? launch_paged_attn<D, true>(p, wgs, st) : launch_paged_attn<D, false>(p, wgs, st);
+    launch_paged_join<D>(p, slots, st);
+}
+
+// What both append calls check beside the shape.
+traj_status check_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* q_out,
+                         const void* k_pages, const void* v_pages, const int32_t* page_table, const int32_t* start, const traj_paged_shape* shape) {
+    if (k == nullptr || v == nullptr || k_pages == nullptr || v_pages == nullptr || page_table == nullptr || start == nullptr ||
+        (q == nullptr) != (q_out == nullptr))
+        return TRAJ_E_NULL;
+    const int64_t kv_row = (int64_t)shape->Hkv * shape->D, q_row = (int64_t)shape->Hq * shape->D;
+    if (k_stride < kv_row || v_stride < kv_row || k_stride % 8 != 0 || v_stride % 8 != 0 || k_stride > (1ll << 40) || v_stride > (1ll << 40))
+        return TRAJ_E_SHAPE;
+    if (q != nullptr && (q_stride < q_row || q_stride % 8 != 0 || q_stride > (1ll << 40) || !aligned16(q) || !aligned16(q_out))) return TRAJ_E_SHAPE;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages)) return TRAJ_E_SHAPE;
+    return TRAJ_OK;
+}
+
+// Rotation per position of each pair of head dimensions, in turns (theta 0: none).
+void fill_turns(float rope_theta, int D, double* turns_of) {
+    if (rope_theta == 0.f) return;
+    const double step = std::pow((double)rope_theta, -2.0 / D);
+    double turns = 0.15915494309189533577;  // 1 / 2 pi
+    for (int d = 0; d < D / 2; ++d, turns *= step) turns_of[d] = turns;
+}
+
+// Both attention calls' checks beside the shape, their parameters and their launch.
+struct PagedCall {
+    int64_t wgs, slots;
+    bool uniform;
+};
+
+traj_status paged_attn_call(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table, const int32_t* lens,
+                            const int32_t* n_new, void* out, const traj_paged_shape* shape, float scale, int32_t causal, void* workspace,
+                            size_t workspace_bytes, PagedAttnParams& p, PagedCall& call) {
+    if (q == nullptr || k_pages == nullptr || v_pages == nullptr || page_table == nullptr || lens == nullptr || out == nullptr) return TRAJ_E_NULL;
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return TRAJ_E_SHAPE;
+    const PagedPlan plan = plan_paged(shape);
+    if (workspace != nullptr && (workspace_bytes < plan.workspace || !aligned16(workspace))) return TRAJ_E_WORKSPACE;
+    p.q = static_cast<const uint16_t*>(q);
+    p.cache = paged_cache(shape, k_pages, v_pages, page_table);
+    p.lens = lens;
+    p.n_new = n_new;
+    p.out = static_cast<uint16_t*>(out);
+    p.B = shape->B;
+    p.T = shape->T;
+    p.Hq = shape->Hq;
+    p.Hkv = shape->Hkv;
+    p.group = shape->Hq / shape->Hkv;
+    p.rows = p.T * p.group;
+    p.by_group = fast_div(p.group);
+    p.tile_rows = plan.tile_rows;
+    p.tiles = plan.tiles;
+    p.units = plan.units;
+    p.single = plan.workspace == 0 || workspace == nullptr;
+    p.causal = causal != 0;
+    p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)shape->D)) * 1.4426950408889634f;
+    call.slots = p.single ? p.B : plan.slots;
+    call.wgs = (call.slots * shape->Hkv + 7) / 8 * 8 * plan.tiles;
+    if (call.wgs > kMostWgs || (int64_t)p.B * p.T * p.Hq > INT_MAX) return TRAJ_E_SHAPE;
+    p.part_o = static_cast<float*>(workspace);
+    p.part_ml = p.part_o + (p.single ? 0 : (size_t)plan.slots * p.units * p.tile_rows * shape->D);
+    p.ranges = reinterpret_cast<int2*>(p.part_ml + (p.single ? 0 : (size_t)plan.slots * p.units * p.tile_rows * 2));
+    call.uniform = shape->page_size % 16 == 0 && shape->token_stride >= shape->D;
+    return TRAJ_OK;
+}
+
+// Workgroups from which an 8-bit append gives all heads of a group of rows to one.
+constexpr int64_t kAppend8Wgs = 1024;
+
+// ------------------------------------------------------------------ paged cache in 8 bits
+// What the 8-bit cache asks of a shape beside the bf16 one.
+traj_status check_paged8(const traj_paged_shape* sh, int32_t scale_block) {
+    const traj_status st = check_paged(sh);
+    if (st != TRAJ_OK) return st;
+    for (int64_t s : {sh->page_stride, sh->token_stride, sh->head_stride})
+        if (s % 16 != 0) return TRAJ_E_SHAPE;
+    if (scale_block < 1 || scale_block > kScaleTokens || sh->page_size % scale_block != 0) return TRAJ_E_SHAPE;
+    return TRAJ_OK;
+}
+
+Paged8Cache paged8_cache(const traj_paged_shape* sh, int32_t sb, const void* k, const void* v, const void* ks, const void* vs) {
+    const auto u8 = [](const void* p) { return static_cast<uint8_t*>(const_cast<void*>(p)); };
+    return Paged8Cache{u8(k), u8(v), u8(ks), u8(vs), sb, sh->page_size / sb, sh->Hkv, fast_div(sb)};
+}
+
+template <int D, bool UNIFORM>
+void launch_paged8_attn(const Paged8AttnParams& p, int64_t wgs, hipStream_t st) {
+    constexpr int DEPTH1 = D == 64 || UNIFORM ? 2 : 1, DEPTH2 = D == 64 ? 2 : 1;
+    auto kernel = p.tile_rows == 16   ? paged8_attn_kernel<D, 1, UNIFORM, 1, DEPTH1>
+                  : p.tile_rows == 32 ? paged8_attn_kernel<D, 2, UNIFORM, 1, DEPTH2>
+                  : p.tile_rows == 64 ? paged8_rows_kernel<D, 2, UNIFORM, true>
+                  : p.tiles == 1      ? paged8_rows_kernel<D, 4, UNIFORM, true>
+                                      : paged8_rows_kernel<D, 4, UNIFORM, false>;  // tiles share the keys
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kPagedThreads), 0, st, p);
+}
+
+template <int D>
+void launch_paged8(const Paged8AttnParams& p, int64_t wgs, int64_t slots, bool uniform, hipStream_t st) {
+    uniform ? launch_paged8_attn<D, true>(p, wgs, st) : launch_paged8_attn<D, false>(p, wgs, st);
+    launch_paged_join<D>(p, slots, st);
+}
+
+// ------------------------------------------------------------------ product with 8-bit operands
+struct Gemm8Tiling {
+    int bm, bn, threads;
+    void (*kernel[3])(Gemm8Params);  // [GemmEpilogue: store, accumulate, partial]
+};
+#define TRAJ_G8_TILING(BM, BN, WM, WN, S) \
+    {BM, BN, WM * WN * 64, {gemm8_ring_kernel<BM, BN, WM, WN, S, kEpiStore>, gemm8_ring_kernel<BM, BN, WM, WN, S, kEpiAccumulate>, \
+                            gemm8_ring_kernel<BM, BN, WM, WN, S, kEpiPartial>}}
+const Gemm8Tiling kGemm8Tilings[] = {
+    TRAJ_G8_TILING(64, 128, 2, 2, 8),
+    TRAJ_G8_TILING(128, 128, 2, 2, 6),
+    TRAJ_G8_TILING(256, 256, 2, 4, 4),
+};
+#undef TRAJ_G8_TILING
+
+struct Gemm8Plan {
+    const Gemm8Tiling* tiling;
+    int64_t tiles_m, tiles_n;
+    int splits, k_split;
+    size_t scales, partial, total;  // of the workspace: x in 8 bits, then its scales, then partial products
+    size_t least;                   // without those
+};
+
+int64_t g8_padded(int64_t K) { return (K + kG8Block - 1) / kG8Block * kG8Block; }
+bool gemm8_sizes_ok(int64_t M, int64_t K, int64_t N) { return M >= 1 && M <= INT_MAX - 256 && K >= 8 && N >= 8 && K % 8 == 0 && N % 8 == 0; }
+
+Gemm8Plan plan_gemm8(int64_t M, int64_t K, int64_t N, size_t room) {
+    Gemm8Plan p{};
+    const int64_t KP = g8_padded(K), blocks = KP / kG8Block;
+    p.scales = align256((size_t)M * KP);
+    p.partial = p.scales + align256((size_t)((M + 127) / 128) * 128 * blocks);
+    p.least = p.partial;
+    const auto tiles = [&](const Gemm8Tiling& g) { return ((M + g.bm - 1) / g.bm) * ((N + g.bn - 1) / g.bn); };
+    p.tiling = M <= 64 ? &kGemm8Tilings[0] : tiles(kGemm8Tilings[2]) >= 200 ? &kGemm8Tilings[2] : &kGemm8Tilings[1];
+    p.tiles_m = (M + p.tiling->bm - 1) / p.tiling->bm;
+    p.tiles_n = (N + p.tiling->bn - 1) / p.tiling->bn;
+    int64_t s = std::min<int64_t>(std::min<int64_t>(kGemmCus / std::max<int64_t>(1, tiles(*p.tiling)), blocks / 4), kGemmMaxSplits);
+    const size_t each = (size_t)M * N * sizeof(float);
+    s = std::min<int64_t>(s, room > p.partial ? (int64_t)((room - p.partial) / each) : 0);
+    if (s < 1) s = 1;
+    const int64_t per = (blocks + s - 1) / s;
+    p.splits = (int)((blocks + per - 1) / per);
+    p.k_split = (int)(per * kG8Block);
+    p.total = p.partial + (p.splits > 1 ? p.splits * each : 0);
+    return p;
 }
 
 // ------------------------------------------------------------------ adjusted logits
@@ -988,14 +1141,8 @@ traj_status traj_paged_append(const void* q, int64_t q_stride, const void* k, in
     if (st != TRAJ_OK) return st;
     if (!(rope_theta >= 0.f) || std::isinf(rope_theta)) return TRAJ_E_ARG;
     if (shape->B == 0 || shape->T == 0) return TRAJ_OK;
-    if (k == nullptr || v == nullptr || k_pages == nullptr || v_pages == nullptr || page_table == nullptr || start == nullptr ||
-        (q == nullptr) != (q_out == nullptr))
-        return TRAJ_E_NULL;
-    const int64_t kv_row = (int64_t)shape->Hkv * shape->D, q_row = (int64_t)shape->Hq * shape->D;
-    if (k_stride < kv_row || v_stride < kv_row || k_stride % 8 != 0 || v_stride % 8 != 0 || k_stride > (1ll << 40) || v_stride > (1ll << 40))
-        return TRAJ_E_SHAPE;
-    if (q != nullptr && (q_stride < q_row || q_stride % 8 != 0 || q_stride > (1ll << 40) || !aligned16(q) || !aligned16(q_out))) return TRAJ_E_SHAPE;
-    if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages)) return TRAJ_E_SHAPE;
+    const traj_status sa = check_append(q, q_stride, k, k_stride, v, v_stride, q_out, k_pages, v_pages, page_table, start, shape);
+    if (sa != TRAJ_OK) return sa;
     AppendParams p{};
     p.q = static_cast<const uint16_t*>(q);
     p.k = static_cast<const uint16_t*>(k);
@@ -1016,11 +1163,7 @@ traj_status traj_paged_append(const void* q, int64_t q_stride, const void* k, in
     if (per_token > (1 << 28)) return TRAJ_E_SHAPE;
     p.per_token = (int)per_token;
     p.by_token = fast_div(per_token);
-    if (p.rotate) {
-        const double step = std::pow((double)rope_theta, -2.0 / shape->D);
-        double turns = 0.15915494309189533577;  // 1 / 2 pi
-        for (int d = 0; d < shape->D / 2; ++d, turns *= step) p.turns[d] = turns;
-    }
+    fill_turns(rope_theta, shape->D, p.turns);
     const int tok = (int64_t)shape->B * shape->T < 1024 ? 1 : kAppendTokens;
     const dim3 grid((unsigned)((shape->T + tok - 1) / tok), tok == 1 ? (unsigned)((per_token + kAppendThreads - 1) / kAppendThreads) : 1u,
                     (unsigned)shape->B);
@@ -1044,38 +1187,139 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
     if (st != TRAJ_OK) return st;
     if (!(scale == scale) || std::isinf(scale)) return TRAJ_E_ARG;
     if (shape->B == 0 || shape->T == 0) return TRAJ_OK;
-    if (q == nullptr || k_pages == nullptr || v_pages == nullptr || page_table == nullptr || lens == nullptr || out == nullptr) return TRAJ_E_NULL;
-    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return TRAJ_E_SHAPE;
-    const PagedPlan plan = plan_paged(shape);
-    if (workspace != nullptr && (workspace_bytes < plan.workspace || !aligned16(workspace))) return TRAJ_E_WORKSPACE;
     PagedAttnParams p{};
+    PagedCall call{};
+    const traj_status sa = paged_attn_call(q, k_pages, v_pages, page_table, lens, n_new, out, shape, scale, causal, workspace, workspace_bytes, p, call);
+    if (sa != TRAJ_OK) return sa;
+    hipStream_t s = as_stream(stream);
+    shape->D == 128 ? launch_paged<128>(p, call.wgs, call.slots, call.uniform, s) : launch_paged<64>(p, call.wgs, call.slots, call.uniform, s);
+    return launched();
+}
+
+traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                               void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale, const int32_t* page_table,
+                               const int32_t* start, const int32_t* n_new, const int32_t* pos0, const traj_paged_shape* shape,
+                               int32_t scale_block, float rope_theta, void* stream) {
+    if (shape == nullptr) return TRAJ_E_NULL;
+    const traj_status st = check_paged8(shape, scale_block);
+    if (st != TRAJ_OK) return st;
+    if (!(rope_theta >= 0.f) || std::isinf(rope_theta)) return TRAJ_E_ARG;
+    if (shape->B == 0 || shape->T == 0) return TRAJ_OK;
+    if (k_scale == nullptr || v_scale == nullptr) return TRAJ_E_NULL;
+    const traj_status sa = check_append(q, q_stride, k, k_stride, v, v_stride, q_out, k_pages, v_pages, page_table, start, shape);
+    if (sa != TRAJ_OK) return sa;
+    const int64_t heads = (q != nullptr ? (int64_t)shape->Hq : 0) + 2 * (int64_t)shape->Hkv;
+    Append8Params p{};
     p.q = static_cast<const uint16_t*>(q);
-    p.cache = paged_cache(shape, k_pages, v_pages, page_table);
-    p.lens = lens;
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.q_row = q_stride;
+    p.k_row = k_stride;
+    p.v_row = v_stride;
+    p.q_out = static_cast<uint16_t*>(q_out);
+    p.cache = paged_cache(shape, nullptr, nullptr, page_table);
+    p.c8 = paged8_cache(shape, scale_block, k_pages, v_pages, k_scale, v_scale);
+    p.start = start;
     p.n_new = n_new;
-    p.out = static_cast<uint16_t*>(out);
-    p.B = shape->B;
+    p.pos0 = pos0;
     p.T = shape->T;
     p.Hq = shape->Hq;
     p.Hkv = shape->Hkv;
-    p.group = shape->Hq / shape->Hkv;
-    p.rows = p.T * p.group;
-    p.by_group = fast_div(p.group);
-    p.tile_rows = plan.tile_rows;
-    p.tiles = plan.tiles;
-    p.units = plan.units;
-    p.single = plan.workspace == 0 || workspace == nullptr;
-    p.causal = causal != 0;
-    p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)shape->D)) * 1.4426950408889634f;
-    const int64_t slots = p.single ? p.B : plan.slots;
-    const int64_t wgs = (slots * shape->Hkv + 7) / 8 * 8 * plan.tiles;
-    if (wgs > kMostWgs || (int64_t)p.B * p.T * p.Hq > INT_MAX) return TRAJ_E_SHAPE;
-    p.part_o = static_cast<float*>(workspace);
-    p.part_ml = p.part_o + (p.single ? 0 : (size_t)plan.slots * p.units * p.tile_rows * shape->D);
-    p.ranges = reinterpret_cast<int2*>(p.part_ml + (p.single ? 0 : (size_t)plan.slots * p.units * p.tile_rows * 2));
-    const bool uniform = shape->page_size % 16 == 0 && shape->token_stride >= shape->D;
+    p.rotate = rope_theta > 0.f ? 1 : 0;
+    fill_turns(rope_theta, shape->D, p.turns);
+    const int rows = scale_block <= 16 ? 16 : scale_block <= 32 ? 32 : 64;
+    p.tokens = rows / scale_block * scale_block;
+    const int64_t groups = ((int64_t)shape->T + scale_block - 1 + p.tokens - 1) / p.tokens;
+    // heads are shared out where the groups of rows leave CUs idle
+    const int64_t waves = (heads + 3) / 4, share = std::min(waves, std::max<int64_t>(1, kAppend8Wgs / (groups * shape->B)));
+    const dim3 grid((unsigned)groups, (unsigned)share, (unsigned)shape->B);
+    auto kernel = shape->D == 128 ? (rows == 16   ? paged8_append_kernel<128, 16>
+                                     : rows == 32 ? paged8_append_kernel<128, 32>
+                                                  : paged8_append_kernel<128, 64>)
+                                  : (rows == 16   ? paged8_append_kernel<64, 16>
+                                     : rows == 32 ? paged8_append_kernel<64, 32>
+                                                  : paged8_append_kernel<64, 64>);
+    hipLaunchKernelGGL(kernel, grid, dim3(kAppendThreads), 0, as_stream(stream), p);
+    return launched();
+}
+
+size_t traj_paged_attn_eight_workspace_size(const traj_paged_shape* shape, int32_t scale_block) {
+    if (shape == nullptr || check_paged8(shape, scale_block) != TRAJ_OK) return 0;
+    return plan_paged(shape).workspace;
+}
+
+traj_status traj_paged_attn_eight(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scale, const uint8_t* v_scale,
+                             const int32_t* page_table, const int32_t* lens, const int32_t* n_new, void* out, const traj_paged_shape* shape,
+                             int32_t scale_block, float scale, int32_t causal, void* workspace, size_t workspace_bytes, void* stream) {
+    if (shape == nullptr) return TRAJ_E_NULL;
+    const traj_status st = check_paged8(shape, scale_block);
+    if (st != TRAJ_OK) return st;
+    if (!(scale == scale) || std::isinf(scale)) return TRAJ_E_ARG;
+    if (shape->B == 0 || shape->T == 0) return TRAJ_OK;
+    if (k_scale == nullptr || v_scale == nullptr) return TRAJ_E_NULL;
+    Paged8AttnParams p{};
+    PagedCall call{};
+    const traj_status sa = paged_attn_call(q, k_pages, v_pages, page_table, lens, n_new, out, shape, scale, causal, workspace, workspace_bytes, p, call);
+    if (sa != TRAJ_OK) return sa;
+    p.c8 = paged8_cache(shape, scale_block, k_pages, v_pages, k_scale, v_scale);
     hipStream_t s = as_stream(stream);
-    shape->D == 128 ? launch_paged<128>(p, wgs, slots, uniform, s) : launch_paged<64>(p, wgs, slots, uniform, s);
+    shape->D == 128 ? launch_paged8<128>(p, call.wgs, call.slots, call.uniform, s) : launch_paged8<64>(p, call.wgs, call.slots, call.uniform, s);
+    return launched();
+}
+
+traj_status traj_quantize_eight(const void* w, void* w8, uint8_t* w_scale, int64_t K, int64_t N, void* stream) {
+    if (!gemm8_sizes_ok(1, K, N)) return TRAJ_E_SHAPE;
+    if (K > kG8MaxK || N > kGemmMaxN) return TRAJ_E_UNSUPPORTED;
+    if (w == nullptr || w8 == nullptr || w_scale == nullptr) return TRAJ_E_NULL;
+    if (!aligned16(w) || !aligned16(w8)) return TRAJ_E_SHAPE;
+    const dim3 grid((unsigned)((N + kG8Block - 1) / kG8Block), (unsigned)(g8_padded(K) / kG8Block));
+    hipLaunchKernelGGL(quantize8_kernel, grid, dim3(256), 0, as_stream(stream), static_cast<const uint16_t*>(w), static_cast<uint8_t*>(w8), w_scale,
+                       (int)K, (int)N);
+    return launched();
+}
+
+size_t traj_linear_eight_workspace_size(int64_t M, int64_t K, int64_t N) {
+    if (!gemm8_sizes_ok(M, K, N) || K > kG8MaxK || N > kGemmMaxN) return 0;
+    return plan_gemm8(M, K, N, SIZE_MAX).total;
+}
+
+traj_status traj_linear_eight(const void* x, const void* w8, const uint8_t* w_scale, void* y, int64_t M, int64_t K, int64_t N, int32_t accumulate,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+    if (M < 0 || !gemm8_sizes_ok(std::max<int64_t>(M, 1), K, N)) return TRAJ_E_SHAPE;
+    if (K > kG8MaxK || N > kGemmMaxN) return TRAJ_E_UNSUPPORTED;
+    if (M == 0) return TRAJ_OK;
+    if (x == nullptr || w8 == nullptr || w_scale == nullptr || y == nullptr) return TRAJ_E_NULL;
+    if (!aligned16(x) || !aligned16(w8) || !aligned16(y)) return TRAJ_E_SHAPE;
+    const Gemm8Plan g = plan_gemm8(M, K, N, workspace_bytes);
+    if (workspace == nullptr || workspace_bytes < g.least || !aligned16(workspace)) return TRAJ_E_WORKSPACE;
+    if (g.tiles_m * g.tiles_n > kMostWgs || (M + 15) / 16 > kMostWgs) return TRAJ_E_SHAPE;
+    char* ws = static_cast<char*>(workspace);
+    hipStream_t s = as_stream(stream);
+    const int64_t KP = g8_padded(K);
+    Gemm8Params p{};
+    p.D = static_cast<uint16_t*>(y);
+    p.M = (int)M;
+    p.N = (int)N;
+    p.K = (int)KP;
+    p.tiles_m = (int)g.tiles_m;
+    p.tiles_n = (int)g.tiles_n;
+    p.partial = reinterpret_cast<float*>(ws + g.partial);
+    p.k_split = g.k_split;
+    p.A8 = reinterpret_cast<uint8_t*>(ws);
+    p.a_scale = reinterpret_cast<uint8_t*>(ws + g.scales);
+    p.W8 = static_cast<const uint8_t*>(w8);
+    p.w_scale = w_scale;
+    hipLaunchKernelGGL(quantize8_rows_kernel, dim3((unsigned)((M + 15) / 16), (unsigned)(KP / kG8Block)), dim3(256), 0, s,
+                       static_cast<const uint16_t*>(x), reinterpret_cast<uint8_t*>(ws), reinterpret_cast<uint8_t*>(ws + g.scales), (int)M, (int)K);
+    traj_status rs = launched();
+    if (rs != TRAJ_OK) return rs;
+    const GemmEpilogue epi = accumulate != 0 ? kEpiAccumulate : kEpiStore;
+    hipLaunchKernelGGL(g.tiling->kernel[g.splits > 1 ? kEpiPartial : epi], dim3((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.splits),
+                       dim3(g.tiling->threads), 0, s, p);
+    rs = launched();
+    if (rs != TRAJ_OK || g.splits == 1) return rs;
+    auto reduce = epi == kEpiAccumulate ? gemm_split_reduce_kernel<kEpiAccumulate> : gemm_split_reduce_kernel<kEpiStore>;
+    hipLaunchKernelGGL(reduce, dim3((unsigned)std::min<int64_t>((M * N / 8 + 255) / 256, 4096)), dim3(256), 0, s, p.partial, g.splits, p.D, p.M, p.N);
     return launched();
 }
 
