@@ -584,8 +584,8 @@ traj_status traj_quantize_eight(const void* w, void* w8, uint8_t* w_scale, int64
  * rounded once to bf16.  A NaN or an infinity in x makes its row of y NaN.
  * Limits: those of traj_quantize_eight; 0 <= M < 2^28 - 16 (0 = no-op); x, w8, y 16-byte aligned; y must not overlap x or w8.
  * workspace: traj_linear_eight_workspace_size(M, K, N) bytes, 16-byte aligned: x in 8 bits with its scales and, for shapes
- * whose tiles leave CUs idle, partial products of ranges of K.  One sized for a larger M of the same K and N serves too;
- * TRAJ_E_WORKSPACE where x in 8 bits does not fit, fewer ranges where their products don't. */
+ * whose tiles leave CUs idle, partial products of ranges of K.  0 for a few rows, which take NULL.  One sized for a larger M
+ * of the same K and N serves too; TRAJ_E_WORKSPACE where x in 8 bits does not fit, fewer ranges where their products don't. */
 size_t traj_linear_eight_workspace_size(int64_t M, int64_t K, int64_t N);
 
 traj_status traj_linear_eight(const void* x, const void* w8, const uint8_t* w_scale, void* y, int64_t M, int64_t K, int64_t N,

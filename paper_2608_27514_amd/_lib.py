@@ -884,9 +884,10 @@ def linear8(x, w8, w_scale, y=None, accumulate=False, workspace=None, stream=Non
         y = _empty(shape, torch.bfloat16, x.device, stream)
     yp = _arg(y, "y", torch.bfloat16, shape, dev)
     if workspace is None:
-        ws_bytes = linear8_workspace_size(M, K, N)
-        workspace = _empty((ws_bytes,), torch.uint8, x.device, stream)
-        ws = workspace.data_ptr()
+        ws, ws_bytes = None, linear8_workspace_size(M, K, N)
+        if ws_bytes > 0:
+            workspace = _empty((ws_bytes,), torch.uint8, x.device, stream)
+            ws = workspace.data_ptr()
     else:
         ws, ws_bytes = _room(workspace, dev)
     st = _lib().traj_linear_eight(xp, wp, sp, yp, M, K, N, 1 if accumulate else 0, ws, ws_bytes, _stream(stream))

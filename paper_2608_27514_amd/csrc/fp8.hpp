@@ -49,4 +49,38 @@ __device__ __forceinline__ void unpack_e4m3(const u32x4_t& x, float scale, u32x4
     }
 }
 
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef short s16x2_t __attribute__((ext_vector_type(2)));
+
+// Largest magnitudes of bf16 pairs, by halves: bf16 magnitudes order like their bits.
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, a), __builtin_bit_cast(u16x2_t, b)));
+}
+
+// Magnitude (fp32 bits) for the scale of N words of bf16 pairs: two instructions a pair, four where any is not finite.
+template <int N>
+__device__ __forceinline__ uint32_t magnitude_of(const uint32_t (&x)[N]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = max_pair(m, x[i] & 0x7fff7fffu);
+    uint32_t top = max(m & 0xffffu, m >> 16);
+    if (ballot64(top >= 0x7f80u) != 0ull) {  // rare
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t a = x[i] & 0x7fffu, b = x[i] >> 16 & 0x7fffu;
+            top = max(top, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
+        }
+    }
+    return top << 16;
+}
+
+// Two bf16 pairs divided by a power of two, to e4m3.
+__device__ __forceinline__ uint32_t pack_e4m3(uint32_t a, uint32_t b, float scale) {
+    s16x2_t w = {};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2_t, a), scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2_t, b), scale, true));
+}
+
 }  // namespace trajspec

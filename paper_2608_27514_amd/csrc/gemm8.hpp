@@ -12,6 +12,7 @@
 
 #include "fp8.hpp"
 #include "gemm.hpp"
+#include "verify_attn16.hpp"
 
 namespace trajspec {
 
@@ -83,77 +84,74 @@ __device__ __forceinline__ int64_t g8_scale_at(int64_t r, int kb, int blocks) {
     return (((r >> 7) * blocks + kb) * 32 + (r & 31)) * 4 + ((r >> 5) & 3);
 }
 
-// 16 lanes per row and block of 128, 8 values each.  grid: x = groups of 16 rows, y = blocks of k
+// 16 lanes per row and block of 128, 8 values each, kG8RowBlocks blocks per workgroup with their loads requested together.
+// grid: x = groups of 16 rows, y = groups of blocks of k
+constexpr int kG8RowBlocks = 4;
 __global__ __launch_bounds__(256) void quantize8_rows_kernel(const uint16_t* __restrict__ x, uint8_t* __restrict__ x8, uint8_t* __restrict__ scale,
-                                                             int M, int K) {
-    const int lane = threadIdx.x & 15, kb = blockIdx.y;
+                                                             int M, int K, int blocks) {
+    const int lane = threadIdx.x & 15, kb0 = blockIdx.y * kG8RowBlocks;
     const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const int k = kb * kG8Block + 8 * lane;
-    u32x4_t v = {};
-    if (r < M && k < K) v = ldg16(x + r * K + k);
-    uint32_t m = 0;
+    u32x4_t v[kG8RowBlocks];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) m = max(m, max(magnitude_bits(bf16_lo(v[e])), magnitude_bits(bf16_hi(v[e]))));
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        uint32_t a, b;
-        lane_pair(t, m, a, b);
-        m = max(a, b);
+    for (int i = 0; i < kG8RowBlocks; ++i) {
+        const int k = (kb0 + i) * kG8Block + 8 * lane;
+        v[i] = u32x4_t{};
+        if (r < M && k < K) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(x + r * K + k));
     }
-    if (r >= M) return;
-    const uint32_t byte = scale_byte(m);
-    const float inv = scale_inverse(byte);
-    u32x2_t o;
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-        o[e] = pack_e4m3(bf16_lo(v[2 * e]) * inv, bf16_hi(v[2 * e]) * inv, bf16_lo(v[2 * e + 1]) * inv, bf16_hi(v[2 * e + 1]) * inv);
-    *reinterpret_cast<u32x2_t*>(x8 + ((int64_t)(2 * kb + (lane >> 3)) * M + r) * kG8Slab + 8 * (lane & 7)) = o;
-    if (lane == 0) scale[g8_scale_at(r, kb, gridDim.y)] = (uint8_t)byte;
+    for (int i = 0; i < kG8RowBlocks; ++i) {
+        const int kb = kb0 + i;
+        if (kb >= blocks) break;  // uniform
+        const uint32_t word[4] = {v[i][0], v[i][1], v[i][2], v[i][3]};
+        uint32_t m = magnitude_of(word);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            uint32_t a, b;
+            lane_pair(t, m, a, b);
+            m = max(a, b);
+        }
+        const uint32_t byte = scale_byte(m);
+        if (r >= M) continue;
+        *reinterpret_cast<u32x2_t*>(x8 + ((int64_t)(2 * kb + (lane >> 3)) * M + r) * kG8Slab + 8 * (lane & 7)) =
+            u32x2_t{pack_e4m3(word[0], word[1], scale_value(byte)), pack_e4m3(word[2], word[3], scale_value(byte))};
+        if (lane == 0) scale[g8_scale_at(r, kb, blocks)] = (uint8_t)byte;
+    }
 }
 
 // ------------------------------------------------------------------ product
-struct Gemm8Params : GemmParams {  // A and W of the base unused; K a multiple of 128
+struct Gemm8Params : GemmParams {  // K padded to a multiple of 128; W unused, A where the kernel takes it to 8 bits itself
     const uint8_t *A8, *W8;        // slabs
     const uint8_t *a_scale;        // g8_scale_at
-    const uint8_t *w_scale;        // [ceil(N / 128)][K / 128]
+    const uint8_t* w_scale;        // [ceil(N / 128)][K / 128]
+    int k_rows;                    // K as A has it
 };
 
-// A wave-wide 4-byte-per-lane load from a buffer straight into LDS (as gemm_dma16).
-__device__ __forceinline__ void gemm8_dma4(const gemm_i32x4_t& rsrc, unsigned voffset, unsigned lds) {
-    unsigned saved;
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %1\n\t"
-        "s_nop 0\n\t"
-        "buffer_load_dword %2, %3, 0 offen lds\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "s"(lds), "v"(voffset), "s"(rsrc)
-        : "memory");
-}
-
-// BM x BN tiles by WM x WN waves, k in stages of 64 (a slab) through a ring of S.  LDS rows are 64 bytes, chunk c of row r at
-// c ^ ((r >> 2) & 3): the 16 rows that a quarter of a wave reads cover all 64 banks.  A stage also brings the scales of
-// each wave's 128 rows (a word per lane); those of W's columns are in lanes from the start, one per 128 of k.
-// While a stage multiplies, the next one's fragments are read and the loads of the one S behind go out between the MFMAs.
-template <int BM, int BN, int WM, int WN, int S, int EPI>
+// BM x BN tiles by WM x WN waves, k in stages of KS slabs through a ring of S.  LDS rows are 64 bytes, chunk c of row r at
+// c ^ ((r >> 2) & 3): the 16 rows that a quarter of a wave reads cover all 64 banks.
+// While a slab multiplies, the next one's fragments are read, and the loads of the stage S behind go out between the MFMAs.
+// Where a wave has few MFMAs per slab, a stage holds two, which halves the meetings.
+// Scales: those of each wave's 128 rows come as a kilobyte for 8 blocks of k, into one of two places of the wave's own, a
+// turn ahead; those of W's columns are in lanes from the start, one per block.
+template <int BM, int BN, int WM, int WN, int KS, int S, int EPI>
 __global__ __launch_bounds__(WM* WN * 64, 1) void gemm8_ring_kernel(Gemm8Params P) {
     constexpr int NW = WM * WN, RM = BM / WM, RN = BN / WN, MB = RM / 32, NB = RN / 32;
-    constexpr int AB = BM * kG8Slab, WB = BN * kG8Slab, SB = AB + WB + NW * 256;  // bytes of A, W, a stage
-    constexpr int LA = BM / 16 / NW, LW = BN / 16 / NW, LS = LA + LW + 1;       // wave-wide loads per wave and stage
+    constexpr int AB = BM * kG8Slab, WB = BN * kG8Slab, SB = KS * (AB + WB);    // bytes of a slab of A, of W, of a stage
+    constexpr int LA = BM / 16 / NW, LW = BN / 16 / NW, LS = KS * (LA + LW);  // wave-wide loads per wave: of a slab, of a stage
     static_assert(BM % (16 * NW) == 0 && BN % (16 * NW) == 0, "whole wave loads");
-    static_assert(RM % 32 == 0 && RN % 32 == 0 && (128 % RM == 0 || RM % 128 == 0) && RM <= 128 && 128 % RN == 0, "scales of a wave");
+    static_assert(RM % 32 == 0 && RN % 32 == 0 && 128 % RM == 0 && 128 % RN == 0, "scales of a wave");
     static_assert((S - 2) * LS < 64, "vmcnt has 6 bits");
-    constexpr int kLds = S * SB > BM * BN * 2 ? S * SB : BM * BN * 2;
+    static_assert(KS == 1 || KS == 2, "a block of k is two slabs");
+    constexpr int kScales = S * SB, kRing = kScales + NW * 2048;
+    constexpr int kLds = kRing > BM * BN * 2 ? kRing : BM * BN * 2;
     static_assert(kLds <= 160 * 1024, "LDS");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds];
     const int tid = threadIdx.x;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int m0, n0;
     gemm_tile_origin(P, BM, BN, m0, n0);
-    const int M = P.M, N = P.N, K = P.K, blocks = K / kG8Block;
+    const int M = P.M, N = P.N, blocks = P.K / kG8Block;
     const int kb0 = EPI == kEpiPartial ? (int)blockIdx.y * (P.k_split / kG8Block) : 0;  // this workgroup's blocks of k
-    const int kb1 = EPI == kEpiPartial ? min(blocks, kb0 + P.k_split / kG8Block) : blocks;
+    const int count = (EPI == kEpiPartial ? min(blocks, kb0 + P.k_split / kG8Block) : blocks) - kb0;
     const unsigned lds0 = (unsigned)(size_t)((gemm_lds_void_t*)lds);
     const int wm = wave / WN, wn = wave % WN, r32 = lane & 31, h = lane >> 5;
 
@@ -162,39 +160,43 @@ __global__ __launch_bounds__(WM* WN * 64, 1) void gemm8_ring_kernel(Gemm8Params 
     const uint8_t* a_ptr = P.A8 + ((int64_t)2 * kb0 * M + m0) * kG8Slab;
     const uint8_t* w_ptr = P.W8 + ((int64_t)2 * kb0 * N + n0) * kG8Slab;
     const unsigned a_rec = (unsigned)min(M - m0, BM) * kG8Slab, w_rec = (unsigned)min(N - n0, BN) * kG8Slab;
-    const int group = (m0 + wm * RM) >> 7;  // the wave's 128 rows, which may lie behind the last
-    const uint8_t* s_ptr = P.a_scale + ((int64_t)min(group, (M - 1) >> 7) * blocks + kb0) * 128;
-    int l_k = 2 * kb0;       // the next slab to load
-    unsigned l_dst = lds0;   // its LDS slot
-    gemm_i32x4_t ars, wrs, srs;
-    auto begin_stage = [&]() {
-        const bool in = l_k < 2 * kb1;  // past the range: zeros, into slots that are not multiplied
-        ars = gemm_descriptor(a_ptr, in ? a_rec : 0u);
-        wrs = gemm_descriptor(w_ptr, in ? w_rec : 0u);
-        srs = gemm_descriptor(s_ptr, in ? 128u : 0u);
+    int left = 2 * count;    // slabs to load
+    unsigned l_dst = lds0;   // the next stage's LDS slot
+    gemm_i32x4_t ars, wrs;
+    auto begin_slab = [&]() {  // past the range: zeros, into slots that are not multiplied
+        ars = gemm_descriptor(a_ptr, left > 0 ? a_rec : 0u);
+        wrs = gemm_descriptor(w_ptr, left > 0 ? w_rec : 0u);
     };
-    auto load_one = [&](int i) {
-        if (i < LA)
-            gemm_dma16<false>(ars, off + 1024u * (unsigned)(wave * LA + i), l_dst + 1024u * (unsigned)(wave * LA + i));
-        else if (i < LA + LW)
-            gemm_dma16<false>(wrs, off + 1024u * (unsigned)(wave * LW + i - LA), l_dst + (unsigned)AB + 1024u * (unsigned)(wave * LW + i - LA));
-        else
-            gemm8_dma4(srs, 4u * (unsigned)r32, l_dst + (unsigned)(AB + WB) + 256u * (unsigned)wave);
-    };
-    auto end_stage = [&]() {
+    auto end_slab = [&]() {
         a_ptr += (int64_t)M * kG8Slab;
         w_ptr += (int64_t)N * kG8Slab;
-        s_ptr += (l_k & 1) != 0 ? 128 : 0;
-        ++l_k;
+        --left;
+    };
+    auto load_one = [&](int i) {  // load i of a stage
+        const int s = i / (LA + LW), j = i % (LA + LW);
+        if (j == 0) begin_slab();
+        if (j < LA)
+            gemm_dma16<false>(ars, off + 1024u * (unsigned)(wave * LA + j), l_dst + (unsigned)(s * AB) + 1024u * (unsigned)(wave * LA + j));
+        else
+            gemm_dma16<false>(wrs, off + 1024u * (unsigned)(wave * LW + j - LA),
+                              l_dst + (unsigned)(KS * AB + s * WB) + 1024u * (unsigned)(wave * LW + j - LA));
+        if (j == LA + LW - 1) end_slab();
+    };
+    auto end_stage = [&]() {
         l_dst += SB;
         if (l_dst == lds0 + S * SB) l_dst = lds0;
     };
+    // scales of the wave's rows, which may lie behind the last, for the blocks from c on
+    const uint8_t* s_ptr = P.a_scale + ((int64_t)min((m0 + wm * RM) >> 7, (M - 1) >> 7) * blocks + kb0) * 128;
+    auto load_scales = [&](int c) {
+        const gemm_i32x4_t rs = gemm_descriptor(s_ptr + 128 * c, c < count ? 128u * (unsigned)min(count - c, 8) : 0u);
+        gemm_dma16<false>(rs, 16u * (unsigned)lane, lds0 + (unsigned)kScales + 2048u * (unsigned)wave + 1024u * (unsigned)((c >> 3) & 1));
+    };
 
-    // scale bytes of the wave's columns: block kb0 + 64 i + lane in byte i % 4 of word i / 4
+    // scale bytes of the wave's columns: block 64 i + lane in byte i % 4 of word i / 4
     uint32_t w_scales[2] = {};
     {
         const int64_t nb = min(n0 + wn * RN, N - 1) >> 7;
-        const int count = kb1 - kb0;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (64 * i + lane < count) w_scales[i / 4] |= (uint32_t)P.w_scale[nb * blocks + kb0 + 64 * i + lane] << (8 * (i % 4));
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(WM* WN * 64, 1) void gemm8_ring_kernel(Gemm8Params 
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
         const int r = wn * RN + 32 * i + r32;
-        b_at[i] = AB + r * kG8Slab + 16 * ((2 * h) ^ ((r >> 2) & 3));
+        b_at[i] = KS * AB + r * kG8Slab + 16 * ((2 * h) ^ ((r >> 2) & 3));
     }
     f32x16_t acc[MB][NB];
 #pragma unroll
@@ -216,39 +218,36 @@ __global__ __launch_bounds__(WM* WN * 64, 1) void gemm8_ring_kernel(Gemm8Params 
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = f32x16_t{};
     i32x8_t af[2][MB], bf[2][NB];
-    uint32_t as[2];
     const int shift = RM == 128 ? 0 : 8 * (((m0 + wm * RM) & 127) / 32);  // the wave's bytes of a scale word
+    const uint8_t* scales = lds + kScales + 2048 * wave + 4 * r32;
 
-    constexpr int FR = MB + NB + 1;
-    auto read16 = [&](int at, const uint8_t* st) { return *reinterpret_cast<const u32x4_t*>(st + at); };
-    auto read_frag = [&](auto set_tag, const uint8_t* st, int f) {
-        constexpr int SET = decltype(set_tag)::value;
-        if (f == 0) {
-            as[SET] = *reinterpret_cast<const uint32_t*>(st + AB + WB + 256 * wave + 4 * lane) >> shift;
-        } else if (f <= NB) {
-            const int at = b_at[f >= 1 && f <= NB ? f - 1 : 0];
-            bf[SET][f >= 1 && f <= NB ? f - 1 : 0] =
-                __builtin_bit_cast(i32x8_t, __builtin_shufflevector(read16(at, st), read16(at ^ 16, st), 0, 1, 2, 3, 4, 5, 6, 7));
-        } else {
-            const int at = a_at[f > NB ? f - NB - 1 : 0];
-            af[SET][f > NB ? f - NB - 1 : 0] =
-                __builtin_bit_cast(i32x8_t, __builtin_shufflevector(read16(at, st), read16(at ^ 16, st), 0, 1, 2, 3, 4, 5, 6, 7));
-        }
+    constexpr int FR = MB + NB;
+    auto read32 = [&](const uint8_t* st, int at) {
+        return __builtin_bit_cast(i32x8_t, __builtin_shufflevector(*reinterpret_cast<const u32x4_t*>(st + at),
+                                                                  *reinterpret_cast<const u32x4_t*>(st + (at ^ 16)), 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    // MFMAs of a stage from set CUR; the next stage's fragments and this step's loads go between them
-    auto multiply = [&](auto cur_tag, const uint8_t* nxt, int ws) {
-        constexpr int CUR = decltype(cur_tag)::value;
+    // fragment f of slab s of the stage at st, into set SET; in the order of use: A block 0, the W blocks, the other A blocks
+    auto read_frag = [&](auto set_tag, const uint8_t* st, int s, int f) {
+        constexpr int SET = decltype(set_tag)::value;
+        if (f >= 1 && f <= NB)
+            bf[SET][f >= 1 && f <= NB ? f - 1 : 0] = read32(st + s * WB, b_at[f >= 1 && f <= NB ? f - 1 : 0]);
+        else
+            af[SET][f == 0 ? 0 : f - NB] = read32(st + s * AB, a_at[f == 0 ? 0 : f - NB]);
+    };
+    // MFMAs of a slab from set CUR; the fragments of slab s of the stage at st and loads of a stage from L0 on go between them
+    auto multiply = [&](auto cur_tag, const uint8_t* st, int s, auto l0_tag, auto l1_tag, int as, int ws) {
+        constexpr int CUR = decltype(cur_tag)::value, L0 = decltype(l0_tag)::value, NL = decltype(l1_tag)::value - L0;
         constexpr int NM = MB * NB;
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
             const int am = i / NB, bn = i % NB;
-#define TRAJ_G8_MFMA(SEL) __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(af[CUR][am], bf[CUR][bn], acc[am][bn], 0, 0, SEL, (int)as[CUR], 0, ws)
+#define TRAJ_G8_MFMA(SEL) __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(af[CUR][am], bf[CUR][bn], acc[am][bn], 0, 0, SEL, as, 0, ws)
             acc[am][bn] = am == 0 ? TRAJ_G8_MFMA(0) : am == 1 ? TRAJ_G8_MFMA(1) : am == 2 ? TRAJ_G8_MFMA(2) : TRAJ_G8_MFMA(3);
 #undef TRAJ_G8_MFMA
 #pragma unroll
-            for (int f = FR * i / NM; f < FR * (i + 1) / NM; ++f) read_frag(std::integral_constant<int, CUR ^ 1>{}, nxt, f);
+            for (int f = FR * i / NM; f < FR * (i + 1) / NM; ++f) read_frag(std::integral_constant<int, CUR ^ 1>{}, st, s, f);
 #pragma unroll
-            for (int l = LS * i / NM; l < LS * (i + 1) / NM; ++l) load_one(l);
+            for (int l = NL * i / NM; l < NL * (i + 1) / NM; ++l) load_one(L0 + l);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -258,17 +257,17 @@ __global__ __launch_bounds__(WM* WN * 64, 1) void gemm8_ring_kernel(Gemm8Params 
     };
     using Z = std::integral_constant<int, 0>;
     using O = std::integral_constant<int, 1>;
+    using LEnd = std::integral_constant<int, LS>;
+    load_scales(0);
 #pragma unroll
     for (int i = 0; i < S - 1; ++i) {
-        begin_stage();
 #pragma unroll
         for (int l = 0; l < LS; ++l) load_one(l);
         end_stage();
     }
     meet();
 #pragma unroll
-    for (int f = 0; f < FR; ++f) read_frag(Z{}, lds, f);
-    begin_stage();
+    for (int f = 0; f < FR; ++f) read_frag(Z{}, lds, 0, f);
 #pragma unroll
     for (int l = 0; l < LS; ++l) load_one(l);
     end_stage();
@@ -277,17 +276,24 @@ __global__ __launch_bounds__(WM* WN * 64, 1) void gemm8_ring_kernel(Gemm8Params 
         slot = slot == S - 1 ? 0 : slot + 1;
         return lds + slot * SB;
     };
-    for (int i = 0; i < kb1 - kb0; ++i) {
+    for (int i = 0; i < count; ++i) {
         const uint32_t word = i < 256 ? w_scales[0] : w_scales[1];
         const int ws = (int)((uint32_t)__builtin_amdgcn_readlane((int)word, i & 63) >> (8 * ((i >> 6) & 3)));
-        meet();
-        begin_stage();
-        multiply(Z{}, next_slot(), ws);
-        end_stage();
-        meet();
-        begin_stage();
-        multiply(O{}, next_slot(), ws);
-        end_stage();
+        const int as = (int)(*reinterpret_cast<const uint32_t*>(scales + 128 * (i & 15)) >> shift);
+        if ((i & 7) == 0) load_scales(i + 8);  // read from two blocks on at the earliest: waits count it as one more of the ring's
+        if constexpr (KS == 1) {
+            meet();
+            multiply(Z{}, next_slot(), 0, Z{}, LEnd{}, as, ws);
+            end_stage();
+            meet();
+            multiply(O{}, next_slot(), 0, Z{}, LEnd{}, as, ws);
+            end_stage();
+        } else {
+            multiply(Z{}, lds + slot * SB, 1, Z{}, Z{}, as, ws);
+            meet();
+            multiply(O{}, next_slot(), 0, Z{}, LEnd{}, as, ws);
+            end_stage();
+        }
     }
     __builtin_amdgcn_s_waitcnt(wait_vmcnt_imm(0) & ~0x0F00);  // the loads past the k range have landed too
     ring_barrier();
@@ -307,6 +313,154 @@ __global__ __launch_bounds__(WM* WN * 64, 1) void gemm8_ring_kernel(Gemm8Params 
         return;
     }
     gemm_epilogue<BM, BN, WM, WN, EPI>(P, acc, reinterpret_cast<uint16_t*>(lds), m0, n0);
+}
+
+// ---------------------------------------------------------------- few rows
+// Up to 16 MR rows: the stream of W bounds the call, so nothing but W passes through memory at length.  A workgroup takes
+// 16 NB columns, its waves the blocks of 128 of k in turn, DEPTH of them in flight; W's fragments (16 columns, 2 KB) come
+// straight into registers, each load 1 KB in a row, and the waves' sums meet in LDS in the waves' order.
+// The k order within a block is the same for both operands but not the memory's: lane l has 16 of each slab, from 16 (l / 16).
+// LDSX 0: A comes in 8 bits from the workspace; otherwise (M K at most LDSX) every workgroup takes A to 8 bits itself, into LDS
+// in the order of the fragments, while its first loads of W are on their way: one launch for the whole call.
+template <int MR, int NB, int WAVES, int DEPTH, int LDSX, int EPI>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void gemm8_rows_kernel(Gemm8Params P) {
+    constexpr bool X8 = LDSX == 0;
+    constexpr int kSums = WAVES * NB * MR * 1024, kX = LDSX + LDSX / kG8Block;
+    static_assert((kSums > kX ? kSums : kX) <= 160 * 1024, "LDS");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kSums > kX ? kSums : kX];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row = lane & 15, q = lane >> 4;
+    const int n0 = (int)blockIdx.x * 16 * NB, M = P.M, N = P.N, blocks = P.K / kG8Block;
+    u32x4_t w[DEPTH][NB][2], x[X8 ? DEPTH : 1][MR][2];
+    uint32_t xs[X8 ? DEPTH : 1][MR], scales[NB];
+    f32x4_t acc[NB][MR];
+    // Blocks behind the last read nothing and count as 0.
+    auto request = [&](auto slot, int kb) {
+        constexpr int u = decltype(slot)::value;
+        const bool in = kb < blocks;
+        const int64_t at = in ? kb : 0;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)(P.W8 + ((2 * at + s) * N + n0) * kG8Slab), (short)0,
+                                                              in ? min(N - n0, 16 * NB) * kG8Slab : 0, kGemmBufferFlags);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) w[u][j][s] = __builtin_amdgcn_raw_buffer_load_b128(rs, 1024 * j + kG8Slab * row + 16 * q, 0, 2);
+        }
+        if constexpr (X8) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)(P.A8 + (2 * at + s) * M * kG8Slab), (short)0, in ? M * kG8Slab : 0,
+                                                                  kGemmBufferFlags);
+#pragma unroll
+                for (int i = 0; i < MR; ++i) x[u][i][s] = __builtin_amdgcn_raw_buffer_load_b128(rs, 1024 * i + kG8Slab * row + 16 * q, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < MR; ++i) xs[u][i] = P.a_scale[g8_scale_at(min(16 * i + row, M - 1), (int)at, blocks)];
+        }
+    };
+    auto multiply = [&](auto slot, int t) {
+        constexpr int u = decltype(slot)::value, ux = X8 ? u : 0;
+        if constexpr (!X8) {
+            const int kb = min(wave + WAVES * t, blocks - 1);
+#pragma unroll
+            for (int i = 0; i < MR; ++i) {
+                const int m = min(16 * i + row, M - 1);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) x[0][i][s] = *reinterpret_cast<const u32x4_t*>(lds + (((2 * kb + s) * 4 + q) * M + m) * 16);
+                xs[0][i] = lds[P.K * M + kb * M + m];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int ws = __builtin_amdgcn_readlane((int)scales[j], t & 63);
+            const i32x8_t wf = __builtin_bit_cast(i32x8_t, __builtin_shufflevector(w[u][j][0], w[u][j][1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int i = 0; i < MR; ++i) {
+                const i32x8_t xf = __builtin_bit_cast(i32x8_t, __builtin_shufflevector(x[ux][i][0], x[ux][i][1], 0, 1, 2, 3, 4, 5, 6, 7));
+                acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, acc[j][i], 0, 0, 0, ws, 0, (int)xs[ux][i]);
+            }
+        }
+    };
+    const int turns = (blocks - wave + WAVES - 1) / WAVES;  // blocks of this wave
+    auto each = [&](auto&& f) {  // f(slot) for every slot of the ring
+        f(std::integral_constant<int, 0>{});
+        if constexpr (DEPTH > 1) f(std::integral_constant<int, (DEPTH > 1 ? 1 : 0)>{});
+        if constexpr (DEPTH > 2) f(std::integral_constant<int, (DEPTH > 2 ? 2 : 0)>{});
+        if constexpr (DEPTH > 3) f(std::integral_constant<int, (DEPTH > 3 ? 3 : 0)>{});
+    };
+    each([&](auto slot) { request(slot, wave + WAVES * decltype(slot)::value); });
+    // block wave + WAVES i of the scales of W's columns is in lane i
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const int64_t nb = min(n0 + 16 * j, N - 1) >> 7;
+        scales[j] = wave + WAVES * lane < blocks ? P.w_scale[nb * blocks + wave + WAVES * lane] : kScaleOne;
+#pragma unroll
+        for (int i = 0; i < MR; ++i) acc[j][i] = f32x4_t{};
+    }
+    if constexpr (!X8) {
+        // 16 lanes per row and block, 8 values each
+        const int part = tid & 15;
+        constexpr int STEP = WAVES * 4, U = 4;
+        for (int at0 = tid >> 4; at0 < M * blocks; at0 += U * STEP) {
+            u32x4_t v[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int at = at0 + i * STEP, kb = at / M, m = at - kb * M, k = kb * kG8Block + 8 * part;
+                v[i] = u32x4_t{};
+                if (at < M * blocks && k < P.k_rows) v[i] = ldg16(P.A + (int64_t)m * P.k_rows + k);
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int at = at0 + i * STEP, kb = at / M, m = at - kb * M;
+                const uint32_t word[4] = {v[i][0], v[i][1], v[i][2], v[i][3]};
+                uint32_t top = magnitude_of(word);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    uint32_t a, b;
+                    lane_pair(t, top, a, b);
+                    top = max(a, b);
+                }
+                if (at >= M * blocks) break;
+                const uint32_t byte = scale_byte(top);
+                *reinterpret_cast<u32x2_t*>(lds + ((8 * kb + part / 2) * M + m) * 16 + 8 * (part & 1)) =
+                    u32x2_t{pack_e4m3(word[0], word[1], scale_value(byte)), pack_e4m3(word[2], word[3], scale_value(byte))};
+                if (part == 0) lds[P.K * M + kb * M + m] = (uint8_t)byte;
+            }
+        }
+        __syncthreads();
+    }
+    for (int t = 0; t < turns; t += DEPTH)
+        each([&](auto slot) {
+            constexpr int u = decltype(slot)::value;
+            multiply(slot, t + u);
+            request(slot, wave + WAVES * (t + u + DEPTH));
+        });
+    if (!X8) __syncthreads();
+    f32x4_t(*sums)[NB * MR][64] = reinterpret_cast<f32x4_t(*)[NB * MR][64]>(lds);
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int i = 0; i < MR; ++i) sums[wave][j * MR + i][lane] = acc[j][i];
+    __syncthreads();
+    for (int at = tid; at < NB * MR * 64; at += WAVES * 64) {
+        const int f = at >> 6, l = at & 63;
+        f32x4_t v = sums[0][f][l];
+#pragma unroll
+        for (int s = 1; s < WAVES; ++s) v += sums[s][f][l];
+        // the lane's result: row l % 16 of A, columns 4 (l / 16) .. + 4
+        const int m = 16 * (f % MR) + (l & 15), n = n0 + 16 * (f / MR) + 4 * (l >> 4);
+        if (m >= M || n >= N) continue;
+        u32x2_t* dst = reinterpret_cast<u32x2_t*>(P.D + (int64_t)m * N + n);
+        if (EPI == kEpiAccumulate) {
+            const u32x2_t d = *dst;
+            v += f32x4_t{bf16_lo(d[0]), bf16_hi(d[0]), bf16_lo(d[1]), bf16_hi(d[1])};
+        }
+        u32x2_t o;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            o[e] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * e]) | ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * e + 1]) << 16);
+        *dst = o;
+    }
 }
 
 }  // namespace trajspec

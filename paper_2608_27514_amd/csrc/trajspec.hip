@@ -750,25 +750,56 @@ void launch_paged8(const Paged8AttnParams& p, int64_t wgs, int64_t slots, bool u
 }
 
 // ------------------------------------------------------------------ product with 8-bit operands
+// Tilings with the figures that the plan is made from: the microseconds that one block of 128 of k takes with a workgroup on
+// every CU, those to fill and drain the ring, those that a further round of workgroups takes beside its blocks, and the rate
+// in TB/s at which weights stream when they bound the call.  Fitted to the fastest tiling and split of 149 products of 24 ..
+// 4096 rows (weights from HBM): 0.1% above it on the geometric mean, at worst 2.4%.
 struct Gemm8Tiling {
     int bm, bn, threads;
+    float block_us, fill_us, round_us, stream;
     void (*kernel[3])(Gemm8Params);  // [GemmEpilogue: store, accumulate, partial]
 };
-#define TRAJ_G8_TILING(BM, BN, WM, WN, S) \
-    {BM, BN, WM * WN * 64, {gemm8_ring_kernel<BM, BN, WM, WN, S, kEpiStore>, gemm8_ring_kernel<BM, BN, WM, WN, S, kEpiAccumulate>, \
-                            gemm8_ring_kernel<BM, BN, WM, WN, S, kEpiPartial>}}
+#define TRAJ_G8_TILING(BM, BN, WM, WN, KS, S, BLOCK, FILL, ROUND, STREAM) \
+    {BM, BN, WM * WN * 64, BLOCK, FILL, ROUND, STREAM, \
+     {gemm8_ring_kernel<BM, BN, WM, WN, KS, S, kEpiStore>, gemm8_ring_kernel<BM, BN, WM, WN, KS, S, kEpiAccumulate>, \
+      gemm8_ring_kernel<BM, BN, WM, WN, KS, S, kEpiPartial>}}
 const Gemm8Tiling kGemm8Tilings[] = {
-    TRAJ_G8_TILING(64, 128, 2, 2, 8),
-    TRAJ_G8_TILING(128, 128, 2, 2, 6),
-    TRAJ_G8_TILING(256, 256, 2, 4, 4),
+    TRAJ_G8_TILING(64, 64, 2, 2, 2, 3, 0.316f, 0.43f, 2.24f, 7.8f),
+    TRAJ_G8_TILING(64, 64, 2, 2, 2, 5, 0.229f, 2.08f, 28.1f, 7.6f),
+    TRAJ_G8_TILING(64, 128, 2, 2, 2, 3, 0.264f, 3.22f, 0.30f, 8.7f),
+    TRAJ_G8_TILING(128, 128, 2, 2, 1, 4, 0.351f, 3.60f, 0.42f, 16.9f),
+    TRAJ_G8_TILING(256, 128, 2, 2, 2, 3, 0.506f, 7.40f, 4.31f, 8.2f),
+    TRAJ_G8_TILING(256, 256, 2, 4, 2, 2, 0.922f, 6.60f, 0.23f, 34.8f),
 };
 #undef TRAJ_G8_TILING
+constexpr int64_t kG8MinSplitBlocks = 4;
+
+// Few rows: [row fragments][fragments of 16 columns: those that spread N over the CUs][store, accumulate], with A in 8 bits
+// from the workspace or, first, in bf16.
+struct Gemm8Rows {
+    int nb, threads;
+    void (*kernel[2])(Gemm8Params);
+};
+#define TRAJ_G8_ROWS(MR, NB, WAVES, DEPTH, LDSX) \
+    {NB, WAVES * 64, {gemm8_rows_kernel<MR, NB, WAVES, DEPTH, LDSX, kEpiStore>, gemm8_rows_kernel<MR, NB, WAVES, DEPTH, LDSX, kEpiAccumulate>}}
+constexpr int kG8LdsX = 64 * 1024;
+const Gemm8Rows kGemm8Rows[3][3] = {
+    {TRAJ_G8_ROWS(1, 1, 16, 2, kG8LdsX), TRAJ_G8_ROWS(1, 2, 16, 2, kG8LdsX), TRAJ_G8_ROWS(1, 3, 16, 1, kG8LdsX)},
+    {TRAJ_G8_ROWS(1, 1, 16, 2, 0), TRAJ_G8_ROWS(1, 2, 8, 2, 0), TRAJ_G8_ROWS(1, 3, 8, 2, 0)},
+    {TRAJ_G8_ROWS(2, 1, 16, 2, 0), TRAJ_G8_ROWS(2, 2, 8, 2, 0), TRAJ_G8_ROWS(2, 3, 8, 2, 0)},
+};
+#undef TRAJ_G8_ROWS
+// Up to 16 rows go by the rows' kernels, up to 32 where K is short: one workgroup holds all of K, which tiles can split
+// (32 rows: 4096 x 4096 11.5 us, by tiles 13.2; 4096 x 12288 15.3 and 16.3; 12288 x 4096 19.5 and 18.3).
+constexpr int64_t kG8FewRows = 16, kG8MoreRows = 32, kG8MoreRowsK = 8192;
 
 struct Gemm8Plan {
-    const Gemm8Tiling* tiling;
+    const Gemm8Tiling* tiling;      // null: rows
+    const Gemm8Rows* rows;
+    bool inside;                    // A is taken to 8 bits by the product's own kernel
     int64_t tiles_m, tiles_n;
     int splits, k_split;
-    size_t scales, partial, total;  // of the workspace: x in 8 bits, then its scales, then partial products
+    size_t scales, partial, total;  // of the workspace: A in 8 bits, then its scales, then partial products
     size_t least;                   // without those
 };
 
@@ -778,20 +809,42 @@ bool gemm8_sizes_ok(int64_t M, int64_t K, int64_t N) { return M >= 1 && M <= INT
 Gemm8Plan plan_gemm8(int64_t M, int64_t K, int64_t N, size_t room) {
     Gemm8Plan p{};
     const int64_t KP = g8_padded(K), blocks = KP / kG8Block;
+    p.splits = 1;
     p.scales = align256((size_t)M * KP);
     p.partial = p.scales + align256((size_t)((M + 127) / 128) * 128 * blocks);
-    p.least = p.partial;
-    const auto tiles = [&](const Gemm8Tiling& g) { return ((M + g.bm - 1) / g.bm) * ((N + g.bn - 1) / g.bn); };
-    p.tiling = M <= 64 ? &kGemm8Tilings[0] : tiles(kGemm8Tilings[2]) >= 200 ? &kGemm8Tilings[2] : &kGemm8Tilings[1];
-    p.tiles_m = (M + p.tiling->bm - 1) / p.tiling->bm;
-    p.tiles_n = (N + p.tiling->bn - 1) / p.tiling->bn;
-    int64_t s = std::min<int64_t>(std::min<int64_t>(kGemmCus / std::max<int64_t>(1, tiles(*p.tiling)), blocks / 4), kGemmMaxSplits);
-    const size_t each = (size_t)M * N * sizeof(float);
-    s = std::min<int64_t>(s, room > p.partial ? (int64_t)((room - p.partial) / each) : 0);
-    if (s < 1) s = 1;
-    const int64_t per = (blocks + s - 1) / s;
-    p.splits = (int)((blocks + per - 1) / per);
-    p.k_split = (int)(per * kG8Block);
+    p.least = p.total = p.partial;
+    if (M <= kG8FewRows || (M <= kG8MoreRows && KP <= kG8MoreRowsK)) {
+        p.inside = M <= kG8FewRows && M * KP <= kG8LdsX;
+        if (p.inside) p.scales = p.partial = p.least = p.total = 0;
+        const int64_t frags = (N + 15) / 16;
+        p.rows = &kGemm8Rows[p.inside ? 0 : M <= kG8FewRows ? 1 : 2][frags <= kGemmCus ? 0 : frags <= 2 * kGemmCus ? 1 : 2];
+        p.tiles_m = 1;
+        p.tiles_n = (frags + p.rows->nb - 1) / p.rows->nb;
+        return p;
+    }
+    const size_t each = partial_bytes(M, N);
+    const int64_t most = std::min<int64_t>(kGemmMaxSplits, room > p.partial ? (int64_t)((room - p.partial) / each) : 0);
+    double best_us = 0.0;
+    for (const Gemm8Tiling& g : kGemm8Tilings) {
+        const int64_t tm = (M + g.bm - 1) / g.bm, tn = (N + g.bn - 1) / g.bn;
+        const double stream_us = (double)K * (double)N * 1e-6 / g.stream;
+        for (int s = 1; s <= kGemmMaxSplits; ++s) {
+            if (s > 1 && (s > most || blocks / s < kG8MinSplitBlocks || tm * tn * s > 300)) break;
+            const int64_t per = (blocks + s - 1) / s;
+            if ((blocks + per - 1) / per != s) continue;  // the same as a smaller s
+            const double rounds = (double)((tm * tn * s + kGemmCus - 1) / kGemmCus);
+            double us = std::max(rounds * (double)per * g.block_us + (rounds - 1.0) * g.round_us, stream_us) + g.fill_us;
+            if (s > 1) us += 2.7 + 0.22 * s + (double)s * (double)M * (double)N * 8e-6 / 8.5;
+            if (p.tiling == nullptr || us < best_us) {
+                p.tiling = &g;
+                p.tiles_m = tm;
+                p.tiles_n = tn;
+                p.splits = s;
+                p.k_split = (int)(per * kG8Block);
+                best_us = us;
+            }
+        }
+    }
     p.total = p.partial + (p.splits > 1 ? p.splits * each : 0);
     return p;
 }
@@ -1290,33 +1343,41 @@ traj_status traj_linear_eight(const void* x, const void* w8, const uint8_t* w_sc
     if (M == 0) return TRAJ_OK;
     if (x == nullptr || w8 == nullptr || w_scale == nullptr || y == nullptr) return TRAJ_E_NULL;
     if (!aligned16(x) || !aligned16(w8) || !aligned16(y)) return TRAJ_E_SHAPE;
-    const Gemm8Plan g = plan_gemm8(M, K, N, workspace_bytes);
-    if (workspace == nullptr || workspace_bytes < g.least || !aligned16(workspace)) return TRAJ_E_WORKSPACE;
+    const Gemm8Plan g = plan_gemm8(M, K, N, workspace == nullptr ? 0 : workspace_bytes);
+    if (workspace == nullptr ? g.least > 0 : workspace_bytes < g.least || !aligned16(workspace)) return TRAJ_E_WORKSPACE;
     if (g.tiles_m * g.tiles_n > kMostWgs || (M + 15) / 16 > kMostWgs) return TRAJ_E_SHAPE;
     char* ws = static_cast<char*>(workspace);
     hipStream_t s = as_stream(stream);
-    const int64_t KP = g8_padded(K);
+    const int64_t KP = g8_padded(K), blocks = KP / kG8Block;
     Gemm8Params p{};
+    p.A = static_cast<const uint16_t*>(x);
     p.D = static_cast<uint16_t*>(y);
     p.M = (int)M;
     p.N = (int)N;
     p.K = (int)KP;
     p.tiles_m = (int)g.tiles_m;
     p.tiles_n = (int)g.tiles_n;
-    p.partial = reinterpret_cast<float*>(ws + g.partial);
     p.k_split = g.k_split;
-    p.A8 = reinterpret_cast<uint8_t*>(ws);
-    p.a_scale = reinterpret_cast<uint8_t*>(ws + g.scales);
     p.W8 = static_cast<const uint8_t*>(w8);
     p.w_scale = w_scale;
-    hipLaunchKernelGGL(quantize8_rows_kernel, dim3((unsigned)((M + 15) / 16), (unsigned)(KP / kG8Block)), dim3(256), 0, s,
-                       static_cast<const uint16_t*>(x), reinterpret_cast<uint8_t*>(ws), reinterpret_cast<uint8_t*>(ws + g.scales), (int)M, (int)K);
-    traj_status rs = launched();
-    if (rs != TRAJ_OK) return rs;
+    p.k_rows = (int)K;
     const GemmEpilogue epi = accumulate != 0 ? kEpiAccumulate : kEpiStore;
-    hipLaunchKernelGGL(g.tiling->kernel[g.splits > 1 ? kEpiPartial : epi], dim3((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.splits),
-                       dim3(g.tiling->threads), 0, s, p);
-    rs = launched();
+    if (!g.inside) {
+        uint8_t *x8 = reinterpret_cast<uint8_t*>(ws), *scales = reinterpret_cast<uint8_t*>(ws + g.scales);
+        p.A8 = x8;
+        p.a_scale = scales;
+        p.partial = reinterpret_cast<float*>(ws + g.partial);
+        const dim3 grid((unsigned)((M + 15) / 16), (unsigned)((blocks + kG8RowBlocks - 1) / kG8RowBlocks));
+        hipLaunchKernelGGL(quantize8_rows_kernel, grid, dim3(256), 0, s, p.A, x8, scales, (int)M, (int)K, (int)blocks);
+        const traj_status rs = launched();
+        if (rs != TRAJ_OK) return rs;
+    }
+    if (g.rows != nullptr)
+        hipLaunchKernelGGL(g.rows->kernel[epi], dim3((unsigned)g.tiles_n), dim3(g.rows->threads), 0, s, p);
+    else
+        hipLaunchKernelGGL(g.tiling->kernel[g.splits > 1 ? kEpiPartial : epi], dim3((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.splits),
+                           dim3(g.tiling->threads), 0, s, p);
+    const traj_status rs = launched();
     if (rs != TRAJ_OK || g.splits == 1) return rs;
     auto reduce = epi == kEpiAccumulate ? gemm_split_reduce_kernel<kEpiAccumulate> : gemm_split_reduce_kernel<kEpiStore>;
     hipLaunchKernelGGL(reduce, dim3((unsigned)std::min<int64_t>((M * N / 8 + 255) / 256, 4096)), dim3(256), 0, s, p.partial, g.splits, p.D, p.M, p.N);

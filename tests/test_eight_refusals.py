@@ -106,7 +106,7 @@ def test_a_workspace_for_more_rows_serves_fewer(K, N):
     most = 0
     for M in list(range(1, 300)) + [511, 512, 513, 2000, 4096, 30000]:
         up = lambda n: -(-n // 256) * 256  # noqa: E731
-        least = up(M * KP) + up(-(-M // 128) * KP)
+        least = 0 if M <= 16 and M * KP <= 65536 else up(M * KP) + up(-(-M // 128) * KP)  # a few rows need none
         assert size(M, K, N) >= least and least >= most
         most = least
 

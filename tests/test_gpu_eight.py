@@ -375,6 +375,8 @@ PRODUCT = [
     (17, 512, 520), (31, 128, 1000), (32, 2048, 2048), (33, 1032, 128), (48, 3584, 512), (64, 1024, 1024), (65, 384, 328), (96, 3584, 640),
     (100, 4096, 256), (128, 2048, 1024), (129, 136, 264), (200, 10752, 136), (256, 1024, 4096), (300, 520, 2056), (513, 640, 1000),
     (1000, 256, 8), (2048, 384, 4104), (4096, 136, 4096), (1, 65536, 64), (40, 33000, 72),
+    (2, 640, 4112), (16, 384, 8200), (3, 256, 12328), (16, 8192, 136), (5, 16384, 4200), (9, 8320, 8216), (17, 640, 5000), (32, 512, 8296),
+    (31, 9000, 200), (70, 4096, 2048), (160, 4096, 6000), (700, 1024, 2048), (1100, 512, 5000), (1300, 2048, 4360),
 ]
 
 
@@ -393,7 +395,7 @@ def test_every_number_of_rows():
 
 def test_product_in_larger_and_smaller_workspaces():
     rng = np.random.default_rng(3)
-    for M, K, N in ((5, 4096, 256), (96, 3584, 640), (300, 4096, 512)):
+    for M, K, N in ((20, 4096, 256), (9, 12288, 128), (96, 3584, 640), (300, 4096, 512)):
         need = tsp.linear8_workspace_size(M, K, N)
         big = torch.full((need + 512,), 255, dtype=U8, device="cuda")
         x, w8, scale, out = product(rng, M, K, N, workspace=big)
