@@ -201,15 +201,15 @@ __device__ __forceinline__ int paged_new(const PagedAttnParams& P, int b, bool r
     return n;
 }
 
-// Keys per workgroup, a multiple of GRANULE.  Every wave computes the same from the same lengths (whole numbers, quotients
-// by powers of two).
-template <int GRANULE>
+// Keys per workgroup, in at least FILL workgroups where they suffice.  Every wave computes the same from the same lengths
+// (whole numbers, quotients by powers of two).
+template <int FILL>
 __device__ __forceinline__ int paged_chunk(int64_t total, int units, int capacity) {
-    const double work = (double)total * (double)units / GRANULE;
-    double per = fmax(work / kPagedMostWgs, fmin(work / kPagedFillWgs, (double)(kPagedChunk / GRANULE)));
-    per = fmin(per, (double)(capacity / GRANULE + 1));
+    const double work = (double)total * (double)units / kPagedGranule;
+    double per = fmax(work / kPagedMostWgs, fmin(work / FILL, (double)(kPagedChunk / kPagedGranule)));
+    per = fmin(per, (double)(capacity / kPagedGranule + 1));
     const int granules = (int)ceil(per);
-    return GRANULE * (granules < 1 ? 1 : granules);
+    return kPagedGranule * (granules < 1 ? 1 : granules);
 }
 
 // Workgroup i runs on XCD i % 8.  The row tiles of one (slot, kv head) follow each other on one XCD, whose L2
@@ -230,7 +230,7 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedAttnParams& P) {
 
 // The range that the workgroup's slot stands for; false where the batch has fewer.  All lanes of the wave take part.
 // Lengths out of range are reported once per sequence where each workgroup looks at its own alone, else by workgroup 0.
-template <int GRANULE = kPagedGranule>
+template <int FILL = kPagedFillWgs>
 __device__ __forceinline__ bool paged_range(const PagedAttnParams& P, const PagedPlace& w, PagedRange& r) {
     const int lane = threadIdx.x & 63, slot = w.slot;
     if (P.single) {
@@ -248,7 +248,7 @@ __device__ __forceinline__ bool paged_range(const PagedAttnParams& P, const Page
         lane_pair64(t, total, x, y);
         total = x + y;
     }
-    const int chunk = __builtin_amdgcn_readfirstlane(paged_chunk<GRANULE>((int64_t)total, P.units, P.cache.capacity));
+    const int chunk = __builtin_amdgcn_readfirstlane(paged_chunk<FILL>((int64_t)total, P.units, P.cache.capacity));
     int base = 0;
     for (int i0 = 0; i0 < P.B; i0 += 64) {
         const int i = i0 + lane;
@@ -357,10 +357,11 @@ struct PagedLds {
     static constexpr int kKRow = D + 8, kVRow = D + 16, kMergeRow = D + 4;
 };
 
-// A wave's query rows: 16 NR of them, row 16 f + lane % 16 in fragment f.
-template <int D, int NR>
+// A wave's query rows: 16 NR of them, row 16 f + lane % 16 in fragment f.  PAIRED: the scores' products take the head dims in
+// the order of 8-bit rows that are loaded 16 values to a lane.
+template <int D, int NR, bool PAIRED = false>
 struct PagedRows {
-    bf16x8_t qf[NR][D / 32];     // head dims 32 ks + 8 (lane / 16) ..
+    bf16x8_t qf[NR][D / 32];     // head dims 32 ks + 8 (lane / 16) ..; PAIRED: 64 (ks / 2) + 16 (lane / 16) + 8 (ks % 2) ..
     int limit[NR];               // keys that the row sees
     f32x4_t o[NR][D / 16];       // O^T: head dims 16 db + 4 (lane / 16) ..
     float m[NR], neg_mc[NR], lsum[NR];  // the reference is the maximum itself: the largest weight is 1 and exact in bf16
@@ -374,7 +375,8 @@ struct PagedRows {
             limit[f] = P.causal ? len - n_new + t + 1 : len;
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks)
-                qf[f][ks] = __builtin_bit_cast(bf16x8_t, ldg16(P.q + (((int64_t)b * P.T + t) * P.Hq + h) * D + 32 * ks + 8 * (lane >> 4)));
+                qf[f][ks] = __builtin_bit_cast(bf16x8_t, ldg16(P.q + (((int64_t)b * P.T + t) * P.Hq + h) * D +
+                                                               (PAIRED ? 64 * (ks / 2) + 16 * (lane >> 4) + 8 * (ks % 2) : 32 * ks + 8 * (lane >> 4))));
             m[f] = kNegInf;
             neg_mc[f] = 0.f;
             lsum[f] = 0.f;

@@ -195,9 +195,29 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
 }
 
 // ------------------------------------------------------------------ attention
+// Up to 16 rows chunks make twice the bf16 cache's workgroups: two or three fit a CU, and half the bytes take half as long
+// (4 x 16384 keys x 8 heads 25.2 -> 22.4 us, 2 x 16384 x 16 heads of 64 24.3 -> 20.6; 768 24.0 and 21.2).  More rows leave
+// more partial results behind each (32 rows: 15.5 us, 17.8 with 512; blocks of 32 tokens 29.9 and 32.3).
+constexpr int kPaged8FillWgs = 512;
+constexpr int kPaged8FillRows = 16;
+
 struct Paged8AttnParams : PagedAttnParams {
     Paged8Cache c8;
 };
+
+// paged_place, but where a head's row of a token is half a line two heads follow each other on an XCD, whose L2 then has the
+// other half (16384 and 10323 keys of 16 heads of 64, [page, token, head] pools: 22.8 us with the heads on XCDs of their own).
+template <int D>
+__device__ __forceinline__ PagedPlace paged8_place(const PagedAttnParams& P) {
+    if (D == 128 || P.Hkv % 2 != 0) return paged_place(P);
+    PagedPlace w;
+    const int turn = blockIdx.x / 8 / P.tiles, pair = turn / 2 * 8 + blockIdx.x % 8;  // of two heads
+    w.row_tile = blockIdx.x / 8 - turn * P.tiles;
+    w.slot = pair / (P.Hkv / 2);
+    w.g = 2 * (pair - w.slot * (P.Hkv / 2)) + (turn & 1);
+    w.unit = w.g * P.tiles + w.row_tile;
+    return w;
+}
 
 // Where 16 BLK keys lie, as PagedTile, and their scales: lane l has those of key l % (16 BLK).
 template <bool UNIFORM, int BLK>
@@ -242,6 +262,11 @@ __device__ __forceinline__ Paged8Tile<UNIFORM, BLK> paged8_tile(const Paged8Attn
     return t;
 }
 
+// What a lane multiplies its key's values by: 1 for an invisible one, whose scale may be anything.
+__device__ __forceinline__ uint32_t paged8_scale(uint32_t byte, uint64_t vis, int key) {
+    return ((vis >> key) & 1ull) != 0ull ? byte : kScaleOne;
+}
+
 // A tile's rows of K or V: a wave-wide load takes 1024 / D rows.  UNIFORM: buffers of the visible rows, so that rows
 // behind them read as 0.
 template <int D, bool UNIFORM, int BLK, bool ONCE>
@@ -261,132 +286,121 @@ __device__ __forceinline__ void paged8_load(u32x4_t (&x)[BLK * D / 64], const ui
     }
 }
 
-// Loaded rows to LDS as bf16, times their scales (lane l of `scale` has key l's).  Rows that are not in vis count as 0:
-// neither their values nor their scales need to be anything.
-template <int D, int BLK, int ROW>
+// Loaded rows to LDS as bf16, times their scales (lane l of `scale` has key l's, that of an invisible one being 1).  Rows that
+// are not in vis may hold anything and count as 0; those of a buffer (UNIFORM) read as 0 anyway.
+template <int D, bool UNIFORM, int BLK, int ROW>
 __device__ __forceinline__ void paged8_put(uint16_t* to, const u32x4_t (&x)[BLK * D / 64], uint64_t vis, uint32_t scale) {
     constexpr int RPI = 1024 / D;
     const int lane = threadIdx.x & 63, vrow = lane / (D / 16), vchunk = lane % (D / 16);
 #pragma unroll
     for (int i = 0; i < BLK * D / 64; ++i) {
         const int row = i * RPI + vrow;
-        const bool seen = ((vis >> row) & 1ull) != 0ull;
-        const uint32_t byte = (uint32_t)__shfl((int)scale, row);
-        u32x4_t lo, hi;
-        unpack_e4m3(seen ? x[i] : u32x4_t{}, scale_value(seen ? byte : kScaleOne), lo, hi);
+        u32x4_t v = x[i], lo, hi;
+        if (!UNIFORM) v = ((vis >> row) & 1ull) != 0ull ? v : u32x4_t{};
+        unpack_e4m3(v, scale_value((uint32_t)__shfl((int)scale, row)), lo, hi);
         uint16_t* p = to + row * ROW + 16 * vchunk;
         *reinterpret_cast<u32x4_t*>(p) = lo;
         *reinterpret_cast<u32x4_t*>(p + 8) = hi;
     }
 }
 
-// Up to 32 rows: the waves take the range's tiles of 32 NK keys in turn, DEPTH tiles in flight each.
-template <int D, int NR, bool UNIFORM, int NK, int DEPTH>
+// Up to 32 rows: the waves take the range's 32-key tiles in turn, the next one in flight.  K passes through LDS as it was
+// loaded, in whole lines where the matrix core wants 16 values of each of 16 rows, and becomes bf16 on the way to the matrix
+// core; V becomes bf16 before LDS, whose transposing reads take 16-bit values, while the scores are multiplied.
+//   MI355X, one token a sequence, K from memory in the operand's order (no LDS) / as bf16 through LDS / as here: 32
+//   sequences of up to 8192 keys x 32 heads of 128 222 / 213 / 210 us, 65536 keys x 8 heads 30.5 / 34.7 / 31.1, 4 x 16384
+//   24.0 / 28.8 / 25.6; with two or three tiles in flight no faster (210.9, 33.3, 27.4), as 12 waves a CU hold enough loads.
+template <int D, int NR, bool UNIFORM>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged8_attn_kernel(Paged8AttnParams P) {
     using L = PagedLds<D>;
-    constexpr int ROWS = 16 * NR, KEYS = 32 * NK, BLK = 2 * NK, NVL = BLK * D / 64, ROUND = kPagedWaves * KEYS;
-    constexpr int kTileBytes = KEYS * L::kVRow * 2, kMergeBytes = ROWS * L::kMergeRow * 4;
+    constexpr int ROWS = 16 * NR, BLK = 2, NVL = BLK * D / 64, RPI = 1024 / D;
+    constexpr int kTileBytes = kPagedTile * L::kVRow * 2, kMergeBytes = ROWS * L::kMergeRow * 4;
     constexpr int kTiles = kPagedWaves * kTileBytes, kMerge = kPagedWaves * kMergeBytes;
-    constexpr uint64_t kAll = KEYS == 64 ? ~0ull : (1ull << (KEYS & 63)) - 1ull;
+    constexpr int kRow8 = D + 16;  // LDS bytes per row of K: the 16 rows of a fragment read start 4 banks apart
     __shared__ __align__(16) char lds[kTiles > kMerge ? kTiles : kMerge];
     __shared__ float sh_m[kPagedWaves * ROWS], sh_l[kPagedWaves * ROWS];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const PagedPlace w = paged_place(P);
+    const PagedPlace w = paged8_place<D>(P);
     PagedRange r;
-    if (!paged_range<ROUND>(P, w, r)) return;
+    if (!paged_range<ROWS <= kPaged8FillRows ? kPaged8FillWgs : kPagedFillWgs>(P, w, r)) return;
     const int len = r.len;
     const int begin = r.split * r.chunk, end = len - begin > r.chunk ? begin + r.chunk : len;
     const int n_new = paged_new(P, r.b, w.unit == 0 && r.split == 0 && threadIdx.x == 0);
     const int min_limit = P.causal ? len - n_new + 1 : len;  // of a row that is not padding
 
     uint16_t* tile = reinterpret_cast<uint16_t*>(lds + wave * kTileBytes);  // K's and then V's
+    uint8_t* kwrite = reinterpret_cast<uint8_t*>(tile) + lane / (D / 16) * kRow8 + 16 * (lane % (D / 16));
+    const uint8_t* kread = reinterpret_cast<const uint8_t*>(tile) + (lane & 15) * kRow8 + 16 * (lane >> 4);
     const PagedCache& C = P.cache;
     const int ts = (int)C.token_stride;
     const int32_t* row = C.table + r.b * C.table_stride;
     const float c = P.scale_log2;
-    const int first = begin + wave * KEYS;
-    u32x4_t kr[DEPTH][NVL], vr[DEPTH][NVL];
-    uint64_t vis[DEPTH];
-    uint32_t ks[DEPTH], vs[DEPTH];
+    const int first = begin + wave * kPagedTile;
+    u32x4_t kr[NVL], vr[NVL];
+    uint32_t vis = 0, ks = 0, vs = 0;
     bool bad = false;
-    using Tile = Paged8Tile<UNIFORM, BLK>;
-    using Pages = PagedPages<UNIFORM, BLK>;
-    PagedRows<D, NR> st;
-    Pages pages;  // of the tile after those in flight
-    // The tile at key0, held in ring slot u; with `more` also the loads of the tile DEPTH rounds behind it.
-    auto step = [&](auto slot, int key0, bool more) {
-        constexpr int u = decltype(slot)::value;
-        paged8_put<D, BLK, L::kKRow>(tile, kr[u], vis[u], ks[u]);
-        f32x4_t s[NR][2 * NK];
-        st.template scores<NK>(tile, s);
-        Tile next;
-        if (more) {
-            next = paged8_tile<UNIFORM, BLK>(P, pages, w.g, key0 + DEPTH * ROUND, first, end, bad);
-            pages = paged_pages<UNIFORM, BLK>(C, row, key0 + (DEPTH + 1) * ROUND, first, end);
-            paged8_load<D, UNIFORM, BLK, true>(kr[u], P.c8.k, next, ts);
+    PagedRows<D, NR, true> st;
+    PagedPages<UNIFORM, BLK> pages;  // of the tile to load next
+    auto fetch = [&](int key0) { pages = paged_pages<UNIFORM, BLK>(C, row, key0, first, end); };
+    auto load = [&](int key0) {
+        const Paged8Tile<UNIFORM, BLK> t = paged8_tile<UNIFORM, BLK>(P, pages, w.g, key0, first, end, bad);
+        paged8_load<D, UNIFORM, BLK, true>(kr, P.c8.k, t, ts);
+        paged8_load<D, UNIFORM, BLK, true>(vr, P.c8.v, t, ts);
+        vis = (uint32_t)t.vis;
+        ks = t.ks;
+        vs = t.vs;
+    };
+    // The tile at key0; with `more` also the loads of the next one.
+    auto step = [&](int key0, bool more) {
+#pragma unroll
+        for (int i = 0; i < NVL; ++i) *reinterpret_cast<u32x4_t*>(kwrite + i * RPI * kRow8) = kr[i];
+        u32x4_t k[BLK][D / 64];
+#pragma unroll
+        for (int j = 0; j < BLK; ++j)
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) k[j][i] = *reinterpret_cast<const u32x4_t*>(kread + 16 * j * kRow8 + 64 * i);
+        // The scale of the row that the lane has of each block (an invisible row's score is replaced, so its scale may be
+        // anything).  Lanes have a block's by rows of 16, which are exchanged in pairs.
+        uint32_t scale[BLK];
+        lane_pair(4, ks, scale[0], scale[1]);
+        f32x4_t s[NR][BLK];
+#pragma unroll
+        for (int j = 0; j < BLK; ++j) {
+#pragma unroll
+            for (int f = 0; f < NR; ++f) s[f][j] = f32x4_t{};
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) {
+                u32x4_t half[2];
+                unpack_e4m3(k[j][i], scale_value(scale[j]), half[0], half[1]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int f = 0; f < NR; ++f)
+                        s[f][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, half[e]), st.qf[f][2 * i + e], s[f][j], 0, 0, 0);
+            }
         }
-        if (vis[u] != kAll || key0 + KEYS > min_limit) st.template mask<NK>(s, vis[u], key0);  // rare: a sequence's last tile
-        bf16x8_t pf[2][NR][NK];
-        st.template weights<NK>(s, c, pf);
-        paged8_put<D, BLK, L::kVRow>(tile, vr[u], vis[u], vs[u]);
+        const uint32_t seen = vis;
+        paged8_put<D, UNIFORM, BLK, L::kVRow>(tile, vr, seen, paged8_scale(vs, seen, lane & 31));
         if (more) {
-            paged8_load<D, UNIFORM, BLK, true>(vr[u], P.c8.v, next, ts);
-            vis[u] = next.vis;
-            ks[u] = next.ks;
-            vs[u] = next.vs;
+            load(key0 + kPagedGranule);
+            fetch(key0 + 2 * kPagedGranule);
         }
+        if (seen != ~0u || key0 + kPagedTile > min_limit) st.template mask<1>(s, seen, key0);  // rare: a sequence's last tile
+        bf16x8_t pf[2][NR][1];
+        st.template weights<1>(s, c, pf);
         __builtin_amdgcn_sched_barrier(0);  // the next tile's products stay behind this one's: registers
-        st.template values<NK>(tile, pf);
+        st.template values<1>(tile, pf);
         __builtin_amdgcn_sched_barrier(0);
     };
-
-    auto fetch = [&](int u) { return paged_pages<UNIFORM, BLK>(C, row, first + u * ROUND, first, end); };
-    Pages p0{}, p1{};
-    if (first < end) {
-        p0 = fetch(0);
-        p1 = fetch(DEPTH - 1);
-        pages = fetch(DEPTH);
-    }
+    if (first < end) fetch(first);
     st.init(P, r.b, w.g, len, n_new, w.row_tile * ROWS);
-    int left = first < end ? (end - first + ROUND - 1) / ROUND : 0;  // tiles of this wave
-    if (left > 0) {
-        using Slot0 = std::integral_constant<int, 0>;
-        using Slot1 = std::integral_constant<int, DEPTH - 1>;
-        auto request = [&](auto slot, const Pages& p) {
-            constexpr int u = decltype(slot)::value;
-            const Tile t = paged8_tile<UNIFORM, BLK>(P, p, w.g, first + u * ROUND, first, end, bad);
-            vis[u] = t.vis;
-            ks[u] = t.ks;
-            vs[u] = t.vs;
-            paged8_load<D, UNIFORM, BLK, true>(kr[u], P.c8.k, t, ts);
-            paged8_load<D, UNIFORM, BLK, true>(vr[u], P.c8.v, t, ts);
-        };
+    if (first < end) {
+        load(first);
+        fetch(first + kPagedGranule);
         int key0 = first;
-        // No load under a condition ahead of the loop: the compiler's waits count the loads that every path issued.
-        if constexpr (DEPTH == 1) {
-            request(Slot0{}, p0);
-            for (; left > 1; --left, key0 += ROUND) step(Slot0{}, key0, true);
-            step(Slot0{}, key0, false);
-        } else if (left == 1) {
-            request(Slot0{}, p0);
-            step(Slot0{}, key0, false);
-        } else {
-            request(Slot0{}, p0);
-            request(Slot1{}, p1);
-            for (; left > 3; left -= 2, key0 += 2 * ROUND) {
-                step(Slot0{}, key0, true);
-                step(Slot1{}, key0 + ROUND, true);
-            }
-            if (left > 2) {
-                step(Slot0{}, key0, true);
-                step(Slot1{}, key0 + ROUND, false);
-                step(Slot0{}, key0 + 2 * ROUND, false);
-            } else {
-                step(Slot0{}, key0, false);
-                step(Slot1{}, key0 + ROUND, false);
-            }
-        }
+        for (; end - key0 > kPagedGranule; key0 += kPagedGranule) step(key0, true);
+        step(key0, false);
         if (ballot64(bad) != 0ull && lane == 0) flag_device_status(kDevBadPage);
     }
 
@@ -412,7 +426,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged8_rows_kernel(Paged8Att
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kg = wave / RW, rw = wave % RW;
-    const PagedPlace w = paged_place(P);
+    const PagedPlace w = paged8_place<D>(P);
     PagedRange r;
     if (!paged_range(P, w, r)) return;
     const int len = r.len;
@@ -444,8 +458,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged8_rows_kernel(Paged8Att
     };
     auto put = [&](int n) {
         uint16_t* k = stage + (n & 1) * kStage;
-        paged8_put<D, 1, L::kKRow>(k + 16 * rw * L::kKRow, kr, vis, ks);
-        paged8_put<D, 1, L::kVRow>(k + STAGE * L::kKRow + 16 * rw * L::kVRow, vr, vis, vs);
+        paged8_put<D, UNIFORM, 1, L::kKRow>(k + 16 * rw * L::kKRow, kr, vis, paged8_scale(ks, vis, lane & 15));
+        paged8_put<D, UNIFORM, 1, L::kVRow>(k + STAGE * L::kKRow + 16 * rw * L::kVRow, vr, vis, paged8_scale(vs, vis, lane & 15));
         if (lane == 0) sh_vis[kg][n & 1][rw] = (uint32_t)vis;
     };
     PagedRows<D, NR> st;

@@ -599,7 +599,7 @@ struct PagedPlan {
     size_t workspace;  // 0: no sequence can be split
 };
 
-PagedPlan plan_paged(const traj_paged_shape* sh) {
+PagedPlan plan_paged(const traj_paged_shape* sh, bool eight = false) {
     PagedPlan p{};
     if (sh->B == 0 || sh->T == 0) return p;
     const int rows = sh->T * (sh->Hq / sh->Hkv);
@@ -609,9 +609,10 @@ PagedPlan plan_paged(const traj_paged_shape* sh) {
     p.units = units > INT_MAX ? INT_MAX : (int)units;
     const int64_t cap = (int64_t)sh->max_pages * sh->page_size;
     // what paged_chunk() comes to at most: chunks of total * units / kPagedMostWgs keys or more, and of kPagedChunk or
-    // more once there are kPagedFillWgs of them
+    // more once there are kPagedFillWgs (8 bits and few rows: kPaged8FillWgs) of them
     const auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
-    const int64_t most = std::max(up(kPagedFillWgs, units), std::min(up(kPagedMostWgs, units), sh->B * up(cap, kPagedChunk)));
+    const int64_t fill = eight && p.tile_rows <= kPaged8FillRows ? kPaged8FillWgs : kPagedFillWgs;
+    const int64_t most = std::max(up(fill, units), std::min(up(kPagedMostWgs, units), sh->B * up(cap, kPagedChunk)));
     p.slots = std::min<int64_t>(most + sh->B, sh->B * up(cap, kPagedGranule));
     const bool whole = cap <= kPagedWhole || sh->B > kPagedSplitBatch || (int64_t)sh->B * sh->T * sh->Hq >= kPagedSplitRows;
     p.workspace = whole ? 0 : (size_t)p.slots * (size_t)units * p.tile_rows * (sh->D + 2) * sizeof(float) + (size_t)sh->B * sizeof(int2);
@@ -680,10 +681,10 @@ struct PagedCall {
 
 traj_status paged_attn_call(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table, const int32_t* lens,
                             const int32_t* n_new, void* out, const traj_paged_shape* shape, float scale, int32_t causal, void* workspace,
-                            size_t workspace_bytes, PagedAttnParams& p, PagedCall& call) {
+                            size_t workspace_bytes, bool eight, PagedAttnParams& p, PagedCall& call) {
     if (q == nullptr || k_pages == nullptr || v_pages == nullptr || page_table == nullptr || lens == nullptr || out == nullptr) return TRAJ_E_NULL;
     if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return TRAJ_E_SHAPE;
-    const PagedPlan plan = plan_paged(shape);
+    const PagedPlan plan = plan_paged(shape, eight);
     if (workspace != nullptr && (workspace_bytes < plan.workspace || !aligned16(workspace))) return TRAJ_E_WORKSPACE;
     p.q = static_cast<const uint16_t*>(q);
     p.cache = paged_cache(shape, k_pages, v_pages, page_table);
@@ -704,7 +705,8 @@ traj_status paged_attn_call(const void* q, const void* k_pages, const void* v_pa
     p.causal = causal != 0;
     p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)shape->D)) * 1.4426950408889634f;
     call.slots = p.single ? p.B : plan.slots;
-    call.wgs = (call.slots * shape->Hkv + 7) / 8 * 8 * plan.tiles;
+    const int together = eight && shape->D == 64 && shape->Hkv % 2 == 0 ? 2 : 1;  // heads that follow each other on an XCD
+    call.wgs = (call.slots * (shape->Hkv / together) + 7) / 8 * 8 * together * plan.tiles;
     if (call.wgs > kMostWgs || (int64_t)p.B * p.T * p.Hq > INT_MAX) return TRAJ_E_SHAPE;
     p.part_o = static_cast<float*>(workspace);
     p.part_ml = p.part_o + (p.single ? 0 : (size_t)plan.slots * p.units * p.tile_rows * shape->D);
@@ -734,9 +736,8 @@ Paged8Cache paged8_cache(const traj_paged_shape* sh, int32_t sb, const void* k, 
 
 template <int D, bool UNIFORM>
 void launch_paged8_attn(const Paged8AttnParams& p, int64_t wgs, hipStream_t st) {
-    constexpr int DEPTH1 = D == 64 || UNIFORM ? 2 : 1, DEPTH2 = D == 64 ? 2 : 1;
-    auto kernel = p.tile_rows == 16   ? paged8_attn_kernel<D, 1, UNIFORM, 1, DEPTH1>
-                  : p.tile_rows == 32 ? paged8_attn_kernel<D, 2, UNIFORM, 1, DEPTH2>
+    auto kernel = p.tile_rows == 16   ? paged8_attn_kernel<D, 1, UNIFORM>
+                  : p.tile_rows == 32 ? paged8_attn_kernel<D, 2, UNIFORM>
                   : p.tile_rows == 64 ? paged8_rows_kernel<D, 2, UNIFORM, true>
                   : p.tiles == 1      ? paged8_rows_kernel<D, 4, UNIFORM, true>
                                       : paged8_rows_kernel<D, 4, UNIFORM, false>;  // tiles share the keys
@@ -1242,7 +1243,7 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
     if (shape->B == 0 || shape->T == 0) return TRAJ_OK;
     PagedAttnParams p{};
     PagedCall call{};
-    const traj_status sa = paged_attn_call(q, k_pages, v_pages, page_table, lens, n_new, out, shape, scale, causal, workspace, workspace_bytes, p, call);
+    const traj_status sa = paged_attn_call(q, k_pages, v_pages, page_table, lens, n_new, out, shape, scale, causal, workspace, workspace_bytes, false, p, call);
     if (sa != TRAJ_OK) return sa;
     hipStream_t s = as_stream(stream);
     shape->D == 128 ? launch_paged<128>(p, call.wgs, call.slots, call.uniform, s) : launch_paged<64>(p, call.wgs, call.slots, call.uniform, s);
@@ -1298,7 +1299,7 @@ traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void*
 
 size_t traj_paged_attn_eight_workspace_size(const traj_paged_shape* shape, int32_t scale_block) {
     if (shape == nullptr || check_paged8(shape, scale_block) != TRAJ_OK) return 0;
-    return plan_paged(shape).workspace;
+    return plan_paged(shape, true).workspace;
 }
 
 traj_status traj_paged_attn_eight(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scale, const uint8_t* v_scale,
@@ -1312,7 +1313,7 @@ traj_status traj_paged_attn_eight(const void* q, const void* k_pages, const void
     if (k_scale == nullptr || v_scale == nullptr) return TRAJ_E_NULL;
     Paged8AttnParams p{};
     PagedCall call{};
-    const traj_status sa = paged_attn_call(q, k_pages, v_pages, page_table, lens, n_new, out, shape, scale, causal, workspace, workspace_bytes, p, call);
+    const traj_status sa = paged_attn_call(q, k_pages, v_pages, page_table, lens, n_new, out, shape, scale, causal, workspace, workspace_bytes, true, p, call);
     if (sa != TRAJ_OK) return sa;
     p.c8 = paged8_cache(shape, scale_block, k_pages, v_pages, k_scale, v_scale);
     hipStream_t s = as_stream(stream);
