@@ -51,6 +51,7 @@ __device__ __forceinline__ void unpack_e4m3(const u32x4_t& x, float scale, u32x4
 
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x2_t __attribute__((ext_vector_type(2)));
 
 // Largest magnitudes of bf16 pairs, by halves: bf16 magnitudes order like their bits.

@@ -32,20 +32,23 @@ struct Append8Params {
     double turns[kAppendMaxHalf];         // rotation per position of pair d in turns: theta^(-2d/D) / 2 pi
 };
 
-// A workgroup takes `tokens` cache rows (whole scale blocks, at most ROWS) of a sequence: page numbers, angles' sines and
-// cosines go to LDS once, then each wave takes a head of q, K or V at a time.  A lane holds 8 values of a row's first half
-// and the matching 8 of its second, a wave ROWS rows; a block's largest magnitude is found by lane exchanges and an LDS
-// maximum per wave.  Rows that the first block held before are rounded again if the block's scale grows (rare: read only
-// then).  Bound by the copy: (4 Hq + 6 Hkv) D bytes per token.
-// grid: x = groups of rows from the block that holds the first token, y shares the heads out, z = sequence.
+// A workgroup takes `tokens` cache rows (whole scale blocks) of a sequence, of which at most ROWS are the call's: their places
+// and angles' sines and cosines go to LDS once, then each wave takes a head of q, K or V at a time, the next one's loads under
+// way.  A lane holds 8 values of a row's first half and the matching 8 of its second, a wave all rows; a block's largest
+// magnitude is found by lane exchanges and an LDS maximum per wave.  Rows that the first block held before are rounded
+// again if the block's scale grows (rare: read only then).  Bound by the copy: (4 Hq + 6 Hkv) D bytes per token.
+// grid: x = groups of cache rows from the block that holds the first token, y shares the heads out, z = sequence.
 template <int D, int ROWS>
 __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Params P) {
     constexpr int HALF = D / 2, LPR = D / 16, RPS = 64 / LPR, STEPS = ROWS / RPS, WAVES = kAppendThreads / 64;
-    __shared__ float cs[ROWS][HALF], sn[ROWS][HALF];
+    // Registers: long blocks keep their rows as loaded and rotate them twice, and request no head ahead.
+    constexpr bool AHEAD = STEPS <= 4;
+    static_assert(STEPS * RPS == ROWS && kAppendThreads % HALF == 0, "whole steps");
+    __shared__ __align__(16) float cs[ROWS][HALF], sn[ROWS][HALF];
     __shared__ int64_t sh_row[ROWS];    // the row's place in the pools; -1: none
     __shared__ int64_t sh_scale[ROWS];  // of the row's block, head 0
-    __shared__ uint32_t sh_max[WAVES][ROWS];
-    const int b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ uint32_t sh_max[WAVES][kScaleTokens];
+    const int b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int start = P.start[b];
     int n = P.n_new != nullptr ? P.n_new[b] : P.T;
     const bool report = blockIdx.x == 0 && blockIdx.y == 0 && tid == 0;
@@ -57,10 +60,32 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
     if ((start < 0 || (int64_t)start + n > P.cache.capacity) && report) flag_device_status(kDevBadLength);
     int lead = start % P.c8.sb;  // rows of the first block before the call's tokens
     if (lead < 0) lead += P.c8.sb;
-    const int t0 = (int)blockIdx.x * P.tokens - lead;  // of the workgroup's first row, as a token of the call
+    const int t0 = max((int)blockIdx.x * P.tokens - lead, 0);  // the workgroup's first token of the call
     if (t0 >= n) return;
-    const int rows = min(P.tokens, n - t0);
-    const int first = t0 < 0 ? -t0 : 0;  // the first row that is the call's
+    lead = blockIdx.x == 0 ? lead : 0;
+    const int rows = min(P.tokens - lead, n - t0);
+    const int qh = P.q != nullptr ? P.Hq : 0, units = qh + 2 * P.Hkv;
+    const int row0 = lane / LPR, d0 = 8 * (lane % LPR);
+    const int64_t token0 = (int64_t)b * P.T + t0;
+    u32x4_t lo[STEPS], hi[STEPS];
+    auto fetch = [&](int unit) {
+        const bool query = unit < qh, key = unit < qh + P.Hkv;
+        const int head = query ? unit : unit - qh - (key ? 0 : P.Hkv);
+        const uint16_t* src = (query ? P.q : key ? P.k : P.v) + head * D + d0;
+        const int64_t src_row = query ? P.q_row : key ? P.k_row : P.v_row;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const int r = s * RPS + row0;
+            lo[s] = hi[s] = u32x4_t{};
+            if (r < rows) {
+                const uint16_t* p = src + (token0 + r) * src_row;
+                lo[s] = ldg16(p);
+                hi[s] = ldg16(p + HALF);
+            }
+        }
+    };
+    const int unit0 = (int)blockIdx.y * WAVES + wave;
+    if (AHEAD && unit0 < units) fetch(unit0);
     if (tid < rows) {
         const int64_t at = (int64_t)start + t0 + tid;
         int64_t row = -1, scale = 0;
@@ -70,7 +95,7 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
             if (page >= 0 && page < P.cache.num_pages) {
                 row = page * P.cache.page_stride + in * P.cache.token_stride;
                 scale = ((int64_t)page * P.c8.blocks + P.c8.by_block.div(in)) * P.Hkv;
-            } else if (blockIdx.y == 0 && tid >= first) {
+            } else if (blockIdx.y == 0) {
                 flag_device_status(kDevBadPage);
             }
         }
@@ -79,62 +104,59 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
     }
     if (P.rotate) {
         const int64_t pos0 = (int64_t)(P.pos0 != nullptr ? P.pos0[b] : start) + t0;
-        for (int i = first * HALF + tid; i < rows * HALF; i += kAppendThreads) {
-            const int r = i / HALF, d = i % HALF;
-            const double turn = (double)(pos0 + r) * P.turns[d];
+        const int d = tid % HALF;
+        const double per = P.turns[d];
+        for (int r = tid / HALF; r < rows; r += kAppendThreads / HALF) {
+            const double turn = (double)(pos0 + r) * per;
             sincospif(2.0f * (float)(turn - floor(turn)), &sn[r][d], &cs[r][d]);
         }
     }
     __syncthreads();
-    const int qh = P.q != nullptr ? P.Hq : 0;
-    const int d0 = 8 * (lane % LPR);
-    const int64_t token0 = (int64_t)b * P.T + t0;
-    for (int unit = (int)blockIdx.y * WAVES + wave; unit < qh + 2 * P.Hkv; unit += (int)gridDim.y * WAVES) {
+    for (int unit = unit0; unit < units; unit += (int)gridDim.y * WAVES) {
+        if (!AHEAD) fetch(unit);
         const bool query = unit < qh, key = unit < qh + P.Hkv;
         const int head = query ? unit : unit - qh - (key ? 0 : P.Hkv);
-        const uint16_t* src = (query ? P.q : key ? P.k : P.v) + head * D + d0;
-        const int64_t src_row = query ? P.q_row : key ? P.k_row : P.v_row;
-        uint8_t* scales = (key ? P.c8.k_scale : P.c8.v_scale) + head;
-        u32x4_t lo[STEPS], hi[STEPS];
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int r = s * RPS + lane / LPR;
-            const bool mine = r >= first && r < rows;
-            lo[s] = hi[s] = u32x4_t{};
-            if (mine) {
-                const uint16_t* p = src + (token0 + r) * src_row;
-                lo[s] = ldg16(p);
-                hi[s] = ldg16(p + HALF);
-            }
-        }
         // the first block's scale where it holds rows from before
-        const bool kept = !query && first > 0 && sh_row[0] >= 0;
+        uint8_t* scales = (key ? P.c8.k_scale : P.c8.v_scale) + head;
+        const bool kept = !query && lead > 0 && sh_row[0] >= 0;
         const uint32_t old = kept ? min(max((uint32_t)scales[sh_scale[0]], kScaleLowest), kScaleHighest) : 0u;
-        float x[STEPS][16];
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int r = s * RPS + lane / LPR;
+        auto rotated = [&](int s, float(&v)[16]) {  // the lane's values of step s
+            const int r = s * RPS + row0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float a = e % 2 == 0 ? bf16_lo(lo[s][e / 2]) : bf16_hi(lo[s][e / 2]);
-                const float c = e % 2 == 0 ? bf16_lo(hi[s][e / 2]) : bf16_hi(hi[s][e / 2]);
-                x[s][e] = a;
-                x[s][8 + e] = c;
-                if (P.rotate && key) {
-                    const float co = cs[r][d0 + e], si = sn[r][d0 + e];
-                    x[s][e] = a * co - c * si;
-                    x[s][8 + e] = c * co + a * si;
+                v[e] = e % 2 == 0 ? bf16_lo(lo[s][e / 2]) : bf16_hi(lo[s][e / 2]);
+                v[8 + e] = e % 2 == 0 ? bf16_lo(hi[s][e / 2]) : bf16_hi(hi[s][e / 2]);
+            }
+            if (P.rotate && key) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float a = v[e], c = v[8 + e], co = cs[r][d0 + e], si = sn[r][d0 + e];
+                    v[e] = a * co - c * si;
+                    v[8 + e] = c * co + a * si;
                 }
             }
+        };
+        float x[AHEAD ? STEPS : 1][16];
+#pragma unroll
+        for (int s = 0; s < (AHEAD ? STEPS : 0); ++s) {
+            if (s * RPS >= rows) break;  // uniform
+            rotated(s, x[AHEAD ? s : 0]);
         }
+        const int next = unit + (int)gridDim.y * WAVES;
+        if (AHEAD && next < units) fetch(next);
         if (query) {
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
-                const int r = s * RPS + lane / LPR;
-                if (r < first || r >= rows) continue;
+                const int r = s * RPS + row0;
+                if (r >= rows) continue;
+                float(&v)[16] = x[AHEAD ? s : 0];
+                if (!AHEAD) rotated(s, v);
                 u32x4_t o[2];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e / 4][e % 4] = (uint32_t)f2bf(x[s][2 * e]) | ((uint32_t)f2bf(x[s][2 * e + 1]) << 16);
+                for (int e = 0; e < 8; ++e) {
+                    const f32x2_t pair = {v[2 * e], v[2 * e + 1]};
+                    o[e / 4][e % 4] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pair, bf16x2_t));
+                }
                 uint16_t* dst = P.q_out + ((token0 + r) * P.Hq + head) * D + d0;
                 *reinterpret_cast<u32x4_t*>(dst) = o[0];
                 *reinterpret_cast<u32x4_t*>(dst + HALF) = o[1];
@@ -142,42 +164,49 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
             continue;
         }
         uint32_t* most = sh_max[wave];
-        if (lane < ROWS) most[lane] = 0u;
+        most[lane] = 0u;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            const int r = s * RPS + lane / LPR;
+            if (s * RPS >= rows) break;
+            const int r = s * RPS + row0;
+            float(&v)[16] = x[AHEAD ? s : 0];
+            if (!AHEAD) rotated(s, v);
             uint32_t m = 0u;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) m = max(m, magnitude_bits(x[s][e]));
+            for (int e = 0; e < 16; ++e) m = max(m, magnitude_bits(v[e]));
 #pragma unroll
             for (int t = 0; t < (LPR == 8 ? 3 : 2); ++t) m = max(m, (uint32_t)__shfl_xor((int)m, 1 << t));
-            if (lane % LPR == 0 && r >= first && r < rows) atomicMax(&most[P.c8.by_block.div(r)], m);
+            if (lane % LPR == 0 && r < rows) atomicMax(&most[P.c8.by_block.div(lead + r)], m);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         uint8_t* pool = (key ? P.c8.k : P.c8.v) + head * P.cache.head_stride + d0;
+        const uint32_t first_byte = max(scale_byte(most[0]), old);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            const int r = s * RPS + lane / LPR;
+            const int r = s * RPS + row0;
             if (r >= rows || sh_row[r] < 0) continue;
-            const int block = P.c8.by_block.div(r);
-            uint32_t byte = scale_byte(most[block]);
-            if (block == 0) byte = max(byte, old);
-            uint8_t* dst = pool + sh_row[r];
-            if (r >= first) {
-                const float inv = scale_inverse(byte);
-                u32x2_t a, c;
+            const int block = P.c8.by_block.div(lead + r);
+            const uint32_t byte = block == 0 ? first_byte : scale_byte(most[block]);
+            const float inv = scale_inverse(byte);
+            float(&v)[16] = x[AHEAD ? s : 0];
+            if (!AHEAD) rotated(s, v);
+            u32x2_t a, c;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    a[e] = pack_e4m3(x[s][4 * e] * inv, x[s][4 * e + 1] * inv, x[s][4 * e + 2] * inv, x[s][4 * e + 3] * inv);
-                    c[e] = pack_e4m3(x[s][8 + 4 * e] * inv, x[s][9 + 4 * e] * inv, x[s][10 + 4 * e] * inv, x[s][11 + 4 * e] * inv);
-                }
-                *reinterpret_cast<u32x2_t*>(dst) = a;
-                *reinterpret_cast<u32x2_t*>(dst + HALF) = c;
-                if (lane % LPR == 0 && r == max(first, block * P.c8.sb)) scales[sh_scale[r]] = (uint8_t)byte;
-            } else if (byte > old) {
-                // 2^(old - byte): exact but for what falls into the subnormals, or below them
-                const float down = byte - old < kScaleOne ? scale_value(kScaleOne - (byte - old)) : 0.f;
+            for (int e = 0; e < 2; ++e) {
+                a[e] = pack_e4m3(v[4 * e] * inv, v[4 * e + 1] * inv, v[4 * e + 2] * inv, v[4 * e + 3] * inv);
+                c[e] = pack_e4m3(v[8 + 4 * e] * inv, v[9 + 4 * e] * inv, v[10 + 4 * e] * inv, v[11 + 4 * e] * inv);
+            }
+            uint8_t* dst = pool + sh_row[r];
+            *reinterpret_cast<u32x2_t*>(dst) = a;
+            *reinterpret_cast<u32x2_t*>(dst + HALF) = c;
+            if (lane % LPR == 0 && r == max(0, block * P.c8.sb - lead)) scales[sh_scale[r]] = (uint8_t)byte;
+        }
+        if (kept && first_byte > old) {
+            // 2^(old - byte): exact but for what falls into the subnormals, or below them
+            const float down = first_byte - old < kScaleOne ? scale_value(kScaleOne - (first_byte - old)) : 0.f;
+            for (int r = row0; r < lead; r += RPS) {
+                uint8_t* dst = pool + sh_row[0] - (int64_t)(lead - r) * P.cache.token_stride;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     u32x2_t a = *reinterpret_cast<const u32x2_t*>(dst + h * HALF);

@@ -716,7 +716,7 @@ traj_status paged_attn_call(const void* q, const void* k_pages, const void* v_pa
 }
 
 // Workgroups from which an 8-bit append gives all heads of a group of rows to one.
-constexpr int64_t kAppend8Wgs = 1024;
+constexpr int64_t kAppend8Wgs = 2048;
 
 // ------------------------------------------------------------------ paged cache in 8 bits
 // What the 8-bit cache asks of a shape beside the bf16 one.
@@ -1281,17 +1281,19 @@ traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void*
     p.Hkv = shape->Hkv;
     p.rotate = rope_theta > 0.f ? 1 : 0;
     fill_turns(rope_theta, shape->D, p.turns);
-    const int rows = scale_block <= 16 ? 16 : scale_block <= 32 ? 32 : 64;
-    p.tokens = rows / scale_block * scale_block;
+    const int whole = scale_block <= 16 ? 16 : scale_block <= 32 ? 32 : 64;
+    p.tokens = whole / scale_block * scale_block;
+    const int most = std::min(shape->T, p.tokens);  // of the call's rows in a group
     const int64_t groups = ((int64_t)shape->T + scale_block - 1 + p.tokens - 1) / p.tokens;
     // heads are shared out where the groups of rows leave CUs idle
     const int64_t waves = (heads + 3) / 4, share = std::min(waves, std::max<int64_t>(1, kAppend8Wgs / (groups * shape->B)));
     const dim3 grid((unsigned)groups, (unsigned)share, (unsigned)shape->B);
-    auto kernel = shape->D == 128 ? (rows == 16   ? paged8_append_kernel<128, 16>
-                                     : rows == 32 ? paged8_append_kernel<128, 32>
+    auto kernel = shape->D == 128 ? (most <= 8    ? paged8_append_kernel<128, 8>
+                                     : most <= 16 ? paged8_append_kernel<128, 16>
+                                     : most <= 32 ? paged8_append_kernel<128, 32>
                                                   : paged8_append_kernel<128, 64>)
-                                  : (rows == 16   ? paged8_append_kernel<64, 16>
-                                     : rows == 32 ? paged8_append_kernel<64, 32>
+                                  : (most <= 16   ? paged8_append_kernel<64, 16>
+                                     : most <= 32 ? paged8_append_kernel<64, 32>
                                                   : paged8_append_kernel<64, 64>);
     hipLaunchKernelGGL(kernel, grid, dim3(kAppendThreads), 0, as_stream(stream), p);
     return launched();
