@@ -417,6 +417,20 @@ struct PagedRows {
             }
     }
 
+    // The running reference of fragment f to mx where that is larger.
+    __device__ __forceinline__ void raise(int f, float mx, float c) {
+        const bool up = mx > m[f];
+        if (ballot64(up) != 0ull) {  // rare after the first tiles
+            const float m_new = up ? mx : m[f];
+            const float alpha = up ? fast_exp2((m[f] - m_new) * c) : 1.0f;  // 0 at the first reference
+            lsum[f] *= alpha;
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db) o[f][db] *= alpha;
+            m[f] = m_new;
+            neg_mc[f] = m_new == kNegInf ? 0.f : -m_new * c;
+        }
+    }
+
     // Weights of the keys against the running reference, in the operand order of values().  What rounding to bf16 leaves
     // goes into a second operand, so that the product has the weights to 16 bits.
     template <int NK>
@@ -426,17 +440,7 @@ struct PagedRows {
             float mx = s[f][0][0];
 #pragma unroll
             for (int v = 1; v < 8 * NK; ++v) mx = __builtin_elementwise_maximum(mx, s[f][v >> 2][v & 3]);
-            mx = quad_max(mx);
-            const bool up = mx > m[f];
-            if (ballot64(up) != 0ull) {  // rare after the first tiles
-                const float m_new = up ? mx : m[f];
-                const float alpha = up ? fast_exp2((m[f] - m_new) * c) : 1.0f;  // 0 at the first reference
-                lsum[f] *= alpha;
-#pragma unroll
-                for (int db = 0; db < D / 16; ++db) o[f][db] *= alpha;
-                m[f] = m_new;
-                neg_mc[f] = m_new == kNegInf ? 0.f : -m_new * c;
-            }
+            raise(f, quad_max(mx), c);
 #pragma unroll
             for (int v = 0; v < 8 * NK; ++v) {
                 const float p = fast_exp2(__builtin_fmaf(s[f][v >> 2][v & 3], c, neg_mc[f]));

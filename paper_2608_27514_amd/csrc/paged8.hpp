@@ -333,6 +333,36 @@ __device__ __forceinline__ void paged8_put(uint16_t* to, const u32x4_t (&x)[BLK 
     }
 }
 
+// PagedRows::weights with the first operand cut to 16 bits rather than rounded, a pair in one instruction: the second one takes
+// what is left, so that the product has the weights to 2^-16.
+template <int D, int NR, int NK, bool PAIRED>
+__device__ __forceinline__ void paged8_weights(PagedRows<D, NR, PAIRED>& st, const f32x4_t (&s)[NR][2 * NK], float c, bf16x8_t (&pf)[2][NR][NK]) {
+#pragma unroll
+    for (int f = 0; f < NR; ++f) {
+        float mx = s[f][0][0];
+#pragma unroll
+        for (int v = 1; v < 8 * NK; ++v) mx = __builtin_elementwise_maximum(mx, s[f][v >> 2][v & 3]);
+        st.raise(f, quad_max(mx), c);
+        u32x4_t first[NK], rest[NK];
+#pragma unroll
+        for (int v = 0; v < 8 * NK; v += 2) {
+            const float a = fast_exp2(__builtin_fmaf(s[f][v >> 2][v & 3], c, st.neg_mc[f]));
+            const float b = fast_exp2(__builtin_fmaf(s[f][v >> 2][(v & 3) + 1], c, st.neg_mc[f]));
+            st.lsum[f] += a;
+            st.lsum[f] += b;
+            const uint32_t ua = __builtin_bit_cast(uint32_t, a), ub = __builtin_bit_cast(uint32_t, b);
+            first[v / 8][v % 8 / 2] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
+            const bf16x2_t left = {(__bf16)(a - __builtin_bit_cast(float, ua & 0xffff0000u)), (__bf16)(b - __builtin_bit_cast(float, ub & 0xffff0000u))};
+            rest[v / 8][v % 8 / 2] = __builtin_bit_cast(uint32_t, left);
+        }
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            pf[0][f][i] = __builtin_bit_cast(bf16x8_t, first[i]);
+            pf[1][f][i] = __builtin_bit_cast(bf16x8_t, rest[i]);
+        }
+    }
+}
+
 // Up to 32 rows: the waves take the range's 32-key tiles in turn, the next one in flight.  K passes through LDS as it was
 // loaded, in whole lines where the matrix core wants 16 values of each of 16 rows, and becomes bf16 on the way to the matrix
 // core; V becomes bf16 before LDS, whose transposing reads take 16-bit values, while the scores are multiplied.
@@ -417,7 +447,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged8_attn_kernel(Paged8Att
         }
         if (seen != ~0u || key0 + kPagedTile > min_limit) st.template mask<1>(s, seen, key0);  // rare: a sequence's last tile
         bf16x8_t pf[2][NR][1];
-        st.template weights<1>(s, c, pf);
+        paged8_weights<D, NR, 1>(st, s, c, pf);
         __builtin_amdgcn_sched_barrier(0);  // the next tile's products stay behind this one's: registers
         st.template values<1>(tile, pf);
         __builtin_amdgcn_sched_barrier(0);
@@ -440,17 +470,24 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged8_attn_kernel(Paged8Att
     paged_store<D, ROWS, kPagedWaves>(P, r, w, n_new, buf, sh_m, sh_l);
 }
 
-// More rows: RW waves of 32 rows each share the stages of 16 RW keys that they load into LDS together; 4 / RW such groups
-// of waves take the range's stages in turn.  While a stage is multiplied the next one lies in registers on its way to the
-// other buffer.
+// More rows: RW waves of 32 rows each share the stages of 16 RW keys that they load into LDS together, as bf16 (the stage is
+// read once per 32 rows, taken from 8 bits once); 4 / RW such groups of waves take the range's stages in turn.  While a stage
+// is multiplied the next one lies in registers on its way to the other buffer.
+// A long call is bound by the products and the vector instructions beside them (4 x 512 tokens, 32 over 8 heads, 4096 keys:
+// 251 us = 0.82 PFLOP/s with both parts of the weights); a short one by the latency of one wave a SIMD: 2.2 us a stage (scores
+// 0.45, weights 0.7, values 0.5, LDS 0.4) and 4 us before the first.  The states go to memory from the registers, 64 bytes of
+// a row at once, in 1.5 us; in whole rows, through LDS, 4 us.
+//   MI355X: 8 blocks of 32 tokens, 28 over 4 heads, up to 2048 keys 28.1 us (30.1 through LDS and with rounded weights); a
+//   block over 4096 keys, 32 over 8 heads, 17.8 (19.1).  Workgroups of eight waves, two ranges of keys each: 28.0 and 19.3,
+//   8 x 4096 keys 43.0 for 46.4, but 64 rows of 256 keys 13.3 for 12.3 and of 4096 51.7 .. 64 for 54.
 template <int D, int RW, bool UNIFORM, bool ONCE>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged8_rows_kernel(Paged8AttnParams P) {
     using L = PagedLds<D>;
     constexpr int NR = 2, KW = kPagedWaves / RW, ROWS = 32 * RW, STAGE = 16 * RW, NK = STAGE / 32, NVL = D / 64;
     constexpr int kStage = STAGE * (L::kKRow + L::kVRow);  // elements
-    constexpr int kStages = KW * 2 * kStage * 2, kMerge = KW * ROWS * L::kMergeRow * 4;
+    constexpr int kStages = KW * 2 * kStage * 2, kMerge = (KW - 1) * ROWS * L::kMergeRow * 4;
     __shared__ __align__(16) char lds[kStages > kMerge ? kStages : kMerge];
-    __shared__ float sh_m[KW * ROWS], sh_l[KW * ROWS];
+    __shared__ float sh_m[KW > 1 ? (KW - 1) * ROWS : 1], sh_l[KW > 1 ? (KW - 1) * ROWS : 1];
     __shared__ uint32_t sh_vis[KW][2][RW];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -500,35 +537,72 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged8_rows_kernel(Paged8Att
         request(1);  // past the end: the range's first row, not visible
         __syncthreads();
         for (int n = 0; n < rounds; ++n) {
-            if (n + 1 < rounds) {
-                put(n + 1);
-                request(n + 2);
-            }
             const uint16_t* k = stage + (n & 1) * kStage;
             uint32_t seen[NK];
 #pragma unroll
             for (int i = 0; i < NK; ++i)
                 seen[i] = __builtin_amdgcn_readfirstlane(sh_vis[kg][n & 1][2 * i] | sh_vis[kg][n & 1][2 * i + 1] << 16);
+            put(n + 1);
+            request(n + 2);
+            f32x4_t s[NR][2 * NK];
+            st.template scores<NK>(k, s);
             const uint64_t all = NK == 1 ? seen[0] : seen[0] | (uint64_t)seen[NK - 1] << 32;
-            if (all != 0ull) {
-                f32x4_t s[NR][2 * NK];
-                st.template scores<NK>(k, s);
-                const int key0 = stage_key(n);
-                if (all != (NK == 1 ? 0xffffffffull : ~0ull) || key0 + STAGE > min_limit) st.template mask<NK>(s, all, key0);
-                bf16x8_t pf[2][NR][NK];
-                st.template weights<NK>(s, c, pf);
-                st.template values<NK>(k + STAGE * L::kKRow, pf);
-            }
+            const int key0 = stage_key(n);
+            if (all != (NK == 1 ? 0xffffffffull : ~0ull) || key0 + STAGE > min_limit) st.template mask<NK>(s, all, key0);
+            bf16x8_t pf[2][NR][NK];
+            paged8_weights<D, NR, NK>(st, s, c, pf);
+            st.template values<NK>(k + STAGE * L::kKRow, pf);
             __syncthreads();
         }
         if (ballot64(bad) != 0ull && lane == 0) flag_device_status(kDevBadPage);
     }
 
+    // the first group takes in what the others leave, in their order, and writes the result or its part of one
     float* buf = reinterpret_cast<float*>(lds);
-    const int set = kg * ROWS + 32 * rw;
-    st.leave(buf + set * L::kMergeRow, sh_m + set, sh_l + set);
-    __syncthreads();
-    paged_store<D, ROWS, KW>(P, r, w, n_new, buf, sh_m, sh_l);
+    if (KW > 1) {
+        const int set = (kg - 1) * ROWS + 32 * rw;
+        if (kg > 0) st.leave(buf + set * L::kMergeRow, sh_m + set, sh_l + set);
+        __syncthreads();
+        if (kg > 0) return;
+    }
+    if (!P.single && w.unit == 0 && r.split == 0 && threadIdx.x == 0) P.ranges[r.b] = make_int2(r.n, r.slot0);
+    const int l16 = lane & 15, q4 = lane >> 4;
+#pragma unroll
+    for (int f = 0; f < NR; ++f) {
+        const int rr = 32 * rw + 16 * f + l16, qrow = w.row_tile * ROWS + rr;
+        float M = st.m[f], l = quad_sum(st.lsum[f]);
+#pragma unroll
+        for (int e = 0; e < KW - 1; ++e) {
+            const float m = sh_m[e * ROWS + rr], top = fmaxf(M, m), base = top == kNegInf ? 0.f : top;
+            const float a = fast_exp2((M - base) * c), b = fast_exp2((m - base) * c);  // 0 for a state without keys
+            l = a * l + b * sh_l[e * ROWS + rr];
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db)
+                st.o[f][db] = a * st.o[f][db] + b * *reinterpret_cast<const f32x4_t*>(buf + (e * ROWS + rr) * L::kMergeRow + 16 * db + 4 * q4);
+            M = top;
+        }
+        const int t = P.by_group.div(qrow), h = w.g * P.group + qrow - t * P.group;
+        const bool pad = t >= n_new;  // whose query may hold anything
+        if (qrow >= P.rows) continue;
+        if (r.n == 1) {
+            const float inv = l > 0.f && !pad ? 1.0f / l : 0.f;  // a row that sees nothing: 0
+            uint16_t* out = P.out + (((int64_t)r.b * P.T + t) * P.Hq + h) * D + 4 * q4;
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db) {
+                const f32x4_t o = pad ? f32x4_t{} : st.o[f][db];
+                u32x2_t x;
+                x[0] = (uint32_t)f2bf(o[0] * inv) | ((uint32_t)f2bf(o[1] * inv) << 16);
+                x[1] = (uint32_t)f2bf(o[2] * inv) | ((uint32_t)f2bf(o[3] * inv) << 16);
+                *reinterpret_cast<u32x2_t*>(out + 16 * db) = x;
+            }
+        } else {
+            const int64_t at = ((int64_t)w.slot * P.units + w.unit) * ROWS + rr;
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db)
+                *reinterpret_cast<f32x4_t*>(P.part_o + at * D + 16 * db + 4 * q4) = pad ? f32x4_t{} : st.o[f][db];
+            if (q4 == 0) *reinterpret_cast<float2*>(P.part_ml + 2 * at) = pad ? make_float2(kNegInf, 0.f) : make_float2(M, l);
+        }
+    }
 }
 
 }  // namespace trajspec
