@@ -1455,6 +1455,14 @@ void traj_test_gemm_plan(int64_t M, int64_t K, int64_t N, int32_t swiglu, int32_
     plan[2] = g.splits;
 }
 
+// The same for a product with 8-bit weights, as the kernel that multiplies (tilings, then those of few rows) and k ranges.
+void traj_test_gemm_eight_plan(int64_t M, int64_t K, int64_t N, int32_t plan[2]) {
+    const Gemm8Plan g = plan_gemm8(M, K, N, SIZE_MAX);
+    constexpr int tilings = sizeof(kGemm8Tilings) / sizeof(kGemm8Tilings[0]);
+    plan[0] = (int32_t)(g.rows != nullptr ? tilings + (g.rows - &kGemm8Rows[0][0]) : g.tiling - kGemm8Tilings);
+    plan[1] = g.splits;
+}
+
 const char* traj_status_string(int32_t status) {
     switch (status) {
         case TRAJ_OK: return "ok";

@@ -8,6 +8,7 @@ import torch
 
 import paper_2608_27514_amd as tsp
 from paper_2608_27514_amd import _lib
+from test_gpu_eight import PRODUCT
 from test_paged_refusals import BAD_SHAPES, FAKE, NULL, ODD, SHAPE, UNSUPPORTED, WORKSPACE, ARG, shape
 
 pytestmark = pytest.mark.skipif(not os.path.exists(_lib.LIB_PATH), reason="libtrajspec.so not built")
@@ -109,6 +110,23 @@ def test_a_workspace_for_more_rows_serves_fewer(K, N):
         least = 0 if M <= 16 and M * KP <= 65536 else up(M * KP) + up(-(-M // 128) * KP)  # a few rows need none
         assert size(M, K, N) >= least and least >= most
         most = least
+
+
+def product_plan(M, K, N):
+    """(kernel, k ranges) that a product runs with: 6 tilings, then 3 x 3 kernels of few rows."""
+    out = (ctypes.c_int32 * 2)()
+    fn = _lib.load().traj_test_gemm_eight_plan
+    fn.restype, fn.argtypes = None, [ctypes.c_int64] * 3 + [ctypes.POINTER(ctypes.c_int32)]
+    fn(M, K, N, out)
+    return tuple(out)
+
+
+def test_the_tested_products_reach_every_kernel():
+    plans = {product_plan(*c) for c in PRODUCT}
+    assert {kernel for kernel, _ in plans} == set(range(15))
+    assert {kernel for kernel, splits in plans if splits > 1} == set(range(6))
+    # a product of the benchmark's layer with many tokens, and few rows of its widest matrix
+    assert product_plan(4096, 4096, 12288) == (5, 1) and product_plan(8, 4096, 12288)[0] == 8
 
 
 def test_the_binding_refuses_host_tensors_and_other_types():

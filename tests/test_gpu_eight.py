@@ -3,7 +3,7 @@
 A rounding to e4m3 is off by at most half a step: 2^-4 of the value, or 2^-10 of the scale among the subnormals.  Values and
 weights are bf16 and taken to 8 bits directly, so they match bit for bit.  Keys are rotated in fp32 first, whose products with a
 sine and a cosine are off by e = 2^-20 (|a| + |b|): |err| <= 2^-4 (|y| + e) + 2^-10 scale + e.
-Attention: keys and values enter exactly; fp32 scores (128 products each), weights to 16 bits and sums over some thousand
+Attention: keys and values enter exactly; fp32 scores (128 products each), weights to 2^-16 and sums over some thousand
 keys move the result by less than 2^-10 sum w |v|, its own rounding to bf16 by 2^-8 |out|.
 Product: operands enter exactly, the matrix core adds 8 products at a time, each cut to 2^-13 of the
 largest (8 2^-13 = 2^-10 of the sum of magnitudes), and those sums in fp32; the result is rounded to
@@ -221,13 +221,19 @@ ATTEND = [
     (1, 17, 1, 128, 16, 1, [100, 260]),                  # 17 rows: a second fragment of one row
     (3, 14, 2, 128, 24, 8, [500, 2, 3, 0, 129]),          # causal: rows before the sequence's start see nothing
     (5, 4, 4, 64, 5, 5, [777, 4, 131]),
-    (32, 4, 1, 128, 1, 1, [200, 33]),                     # four row tiles
+    (32, 4, 1, 128, 1, 1, [200, 33]),
     (64, 2, 2, 64, 736, 46, [736, 64, 65, 100]),
     (33, 1, 1, 128, 48, 24, [400]),
     (2, 8, 2, 64, 100, 50, [4000, 1]),                    # one long sequence: split over many workgroups
     (1, 8, 8, 128, 64, 64, [5000, 40, 2222]),
     (4, 8, 1, 128, 48, 3, [3000]),
     (4, 8, 1, 64, 80, 20, [2900, 100]),
+    (32, 8, 2, 128, 16, 16, [1500, 300]),                 # 128 rows, split
+    (16, 8, 2, 128, 20, 4, [900, 90]),
+    (40, 8, 2, 128, 12, 6, [513, 31, 0]),                 # two row tiles that share the keys, the second of 32 rows
+    (48, 12, 4, 64, 32, 32, [700, 0, 64]),                # heads in pairs
+    (3, 9, 3, 64, 16, 16, [600, 257]),                    # and an odd number of them
+    (1, 6, 3, 64, 48, 16, [1, 2000]),
 ]
 
 
@@ -254,6 +260,9 @@ def test_attention_lengths_around_every_tile():
     lens = list(range(0, 530))
     attend(rng, len(lens), 1, 2, 1, 64, 16, 8, lens, False)
     attend(rng, len(lens), 1, 1, 1, 128, 12, 4, lens, False)
+    lens = list(range(0, 270))
+    attend(rng, len(lens), 9, 4, 1, 64, 16, 16, lens, True)
+    attend(rng, len(lens), 30, 3, 1, 128, 10, 5, lens, True)
 
 
 def test_attention_unsplit_and_in_a_larger_workspace_agree():
@@ -377,6 +386,8 @@ PRODUCT = [
     (1000, 256, 8), (2048, 384, 4104), (4096, 136, 4096), (1, 65536, 64), (40, 33000, 72),
     (2, 640, 4112), (16, 384, 8200), (3, 256, 12328), (16, 8192, 136), (5, 16384, 4200), (9, 8320, 8216), (17, 640, 5000), (32, 512, 8296),
     (31, 9000, 200), (70, 4096, 2048), (160, 4096, 6000), (700, 1024, 2048), (1100, 512, 5000), (1300, 2048, 4360),
+    (67, 2384, 2360), (66, 4664, 2736), (66, 4968, 2848), (96, 5264, 8416), (449, 2184, 8320), (129, 11472, 5456),
+    (3055, 136, 8464), (2340, 680, 5656), (131, 14232, 8232),
 ]
 
 
