@@ -128,6 +128,24 @@ def test_append_parity(B, T, Hq, Hkv, D, ps, sb, start, n_new, pos0, theta):
     check_append(got, out, (ref, size), pools, exact, qkv, theta)
 
 
+@pytest.mark.parametrize("D,ps,sb", [(128, 16, 16), (64, 24, 8), (128, 64, 64), (64, 48, 24), (128, 32, 1), (128, 60, 5), (64, 64, 32)])
+def test_append_from_every_offset(D, ps, sb):
+    """A sequence for each place of a page to begin at, calls shorter and longer than a group of rows."""
+    rng = np.random.default_rng(D + ps + sb)
+    for T in (1, 7, 16, 17, 33, 70):
+        columns = -(-(ps + T) // ps)
+        table, pages = make_table(rng, ps, columns)
+        before = make_pools(rng, pages, ps, sb, 1, D)
+        k, v = (bf16_round(rng.standard_normal((ps, T, 1, D)) * 2.0 ** rng.integers(-3, 4, (ps, T, 1, 1))) for _ in range(2))
+        start, n_new = np.arange(ps, dtype=np.int32), rng.integers(0, T + 1, ps).astype(np.int32)
+        _, pools, _ = eight.paged_append8(k, k, v, before, table, start, n_new, theta=0)
+        got = on_gpu(before)
+        tsp.paged_append8(bf(k), bf(v), *got, i32(table), i32(start), n_new=i32(n_new), rope_theta=0.0)
+        assert tsp.device_status() == 0
+        for x, want in zip(got, pools):
+            assert np.array_equal(f64(x) if x.dtype == E4 else bytes_of(x), want)
+
+
 def test_append_token_by_token_and_again():
     """Single tokens into blocks whose scales grow, and a denoising step that writes its rows a second time."""
     rng = np.random.default_rng(1)
