@@ -107,8 +107,15 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
         const int d = tid % HALF;
         const double per = P.turns[d];
         for (int r = tid / HALF; r < rows; r += kAppendThreads / HALF) {
-            const double turn = (double)(pos0 + r) * per;
-            sincospif(2.0f * (float)(turn - floor(turn)), &sn[r][d], &cs[r][d]);
+            double turn = (double)(pos0 + r) * per;
+            turn -= rint(turn);
+            // 32 bits hold it to 2^-25, 0.2 millionths of a radian, which would show where a key lies next to the middle
+            // between two codes: what they leave is added to the angle to first order
+            const float near = (float)turn, rest = (float)(turn - near) * 6.2831853f;
+            float s, c;
+            sincospif(2.0f * near, &s, &c);
+            sn[r][d] = s + c * rest;
+            cs[r][d] = c - s * rest;
         }
     }
     __syncthreads();
