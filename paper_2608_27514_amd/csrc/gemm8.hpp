@@ -4,6 +4,7 @@
 //   quantize8_kernel       W to 8 bits, once
 //   quantize8_rows_kernel  A to 8 bits, into the workspace
 //   gemm8_ring_kernel      the product
+//   gemm8_rows_kernel      the product of few rows, A taken to 8 bits on the way where it is small
 //
 // Operands lie in slabs of 64 of k: [k / 64][row][k % 64], rows being rows of A and columns of W, and K padded with zeros
 // to a multiple of 128.  So what a workgroup needs of a slab is contiguous, whole lines however few of k a stage holds, and
@@ -24,7 +25,8 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
 // ------------------------------------------------------------------ W
 // A workgroup per 128 x 128 block: 4 x 8 values (4 of k, 8 columns) per thread and turn, whose bytes go through LDS, so that
-// both sides move whole lines.  Bound by the copy.
+// both sides move whole lines.  Bound by the copy: 4096 x 12288 (151 MB) 27 us in a row of calls = 5.6 TB/s, where a copy of
+// as much moves 5.2; 1000 x 712 4.7 us, its latencies.
 // grid: x = blocks of columns, y = blocks of k
 constexpr int kQ8Row = 132;  // LDS bytes per column: the 32 words that half a wave writes lie in banks of their own
 __global__ __launch_bounds__(256) void quantize8_kernel(const uint16_t* __restrict__ w, uint8_t* __restrict__ w8, uint8_t* __restrict__ scale,
@@ -85,6 +87,7 @@ __device__ __forceinline__ int64_t g8_scale_at(int64_t r, int kb, int blocks) {
 }
 
 // 16 lanes per row and block of 128, 8 values each, kG8RowBlocks blocks per workgroup with their loads requested together.
+// Bound by the copy: 4096 x 4096 11 us (50 MB, 9.8 at the copy's rate); 96 x 3584 3.2, a launch.
 // grid: x = groups of 16 rows, y = groups of blocks of k
 constexpr int kG8RowBlocks = 4;
 __global__ __launch_bounds__(256) void quantize8_rows_kernel(const uint16_t* __restrict__ x, uint8_t* __restrict__ x8, uint8_t* __restrict__ scale,
@@ -130,6 +133,11 @@ struct Gemm8Params : GemmParams {  // K padded to a multiple of 128; W unused, A
 // c ^ ((r >> 2) & 3): the 16 rows that a quarter of a wave reads cover all 64 banks.
 // While a slab multiplies, the next one's fragments are read, and the loads of the stage S behind go out between the MFMAs.
 // Where a wave has few MFMAs per slab, a stage holds two, which halves the meetings.
+// What bounds it is the way from the L2 to LDS and the meetings, not the matrix core and not HBM: 4096 x 4096 x 12288 takes
+// 160 us = 2.57 PFLOP/s (8192 x 8192 x 8192 2.78), 105 with the loads left out, and neither deeper rings nor other cache
+// policies change it (with A's 8 bits 180 us; four stages of one slab 186, tiles of 256 x 128 205).  Fewer rows run through their k at some
+// 0.32 us per 128, again at any depth: 96 x 3584 x 4608 14.8 us with a ring of 5 and 15.3 with one of 9, 14.1 in tiles
+// of 32 x 64, which take 19.2 for 17.2 at 64 x 4096 x 12288.
 // Scales: those of each wave's 128 rows come as a kilobyte for 8 blocks of k, into one of two places of the wave's own, a
 // turn ahead; those of W's columns are in lanes from the start, one per block.
 template <int BM, int BN, int WM, int WN, int KS, int S, int EPI>
@@ -322,6 +330,8 @@ __global__ __launch_bounds__(WM* WN * 64, 1) void gemm8_ring_kernel(Gemm8Params 
 // The k order within a block is the same for both operands but not the memory's: lane l has 16 of each slab, from 16 (l / 16).
 // LDSX 0: A comes in 8 bits from the workspace; otherwise (M K at most LDSX) every workgroup takes A to 8 bits itself, into LDS
 // in the order of the fragments, while its first loads of W are on their way: one launch for the whole call.
+//   MI355X: 1 x 4096 x 12288 (50 MB of W) 10.0 us, where the read takes 8.1; with A taken to 8 bits first and
+//   through the ring kernel 15.5.
 template <int MR, int NB, int WAVES, int DEPTH, int LDSX, int EPI>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void gemm8_rows_kernel(Gemm8Params P) {
     constexpr bool X8 = LDSX == 0;

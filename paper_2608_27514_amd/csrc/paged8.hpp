@@ -36,7 +36,11 @@ struct Append8Params {
 // and angles' sines and cosines go to LDS once, then each wave takes a head of q, K or V at a time, the next one's loads under
 // way.  A lane holds 8 values of a row's first half and the matching 8 of its second, a wave all rows; a block's largest
 // magnitude is found by lane exchanges and an LDS maximum per wave.  Rows that the first block held before are rounded
-// again if the block's scale grows (rare: read only then).  Bound by the copy: (4 Hq + 6 Hkv) D bytes per token.
+// again if the block's scale grows (rare: read only then).  Bound by the copy, (4 Hq + 6 Hkv) D bytes per token, and in
+// small calls by a chain of loads, angles, rows and stores.
+//   MI355X: 4 x 4096 tokens, 28 over 4 heads of 128 62.1 us (289 MB, 55.9 at the copy's rate), blocks of 64 tokens 52.7 (8192
+//   tokens, 32 over 8 heads, copy 36.2; with the rotated values kept and a head ahead 256 registers and 70.9); one token 4.7,
+//   16 blocks of up to 32 tokens of 32 heads 7.7, 64 sequences' tokens 5.2.
 // grid: x = groups of cache rows from the block that holds the first token, y shares the heads out, z = sequence.
 template <int D, int ROWS>
 __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Params P) {

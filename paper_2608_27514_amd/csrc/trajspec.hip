@@ -715,7 +715,9 @@ traj_status paged_attn_call(const void* q, const void* k_pages, const void* v_pa
     return TRAJ_OK;
 }
 
-// Workgroups from which an 8-bit append gives all heads of a group of rows to one.
+// Workgroups from which an 8-bit append gives all heads of a group of rows to one.  With 256, 2048 and 16384: 16 blocks of 32
+// tokens of 32 heads 12.1, 7.7 and 7.7 us; 4 x 4096 tokens, 28 over 4 heads, 64.5, 62.8 and 69.2; 2 x 4096 in blocks of 64,
+// 32 over 8 heads, 81.6, 52.4 and 53.1.
 constexpr int64_t kAppend8Wgs = 2048;
 
 // ------------------------------------------------------------------ paged cache in 8 bits
