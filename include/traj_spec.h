@@ -554,10 +554,10 @@ traj_status traj_confidence_topk_adjusted(const void* logits, int32_t k, float* 
  * scale, so they have to be written again before they are attended to.  q_out (bf16), tokens without a place and the
  * status bits as traj_paged_append.  No two sequences of a call may write the same block. */
 traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
-                               int64_t v_stride, void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale,
-                               uint8_t* v_scale, const int32_t* page_table, const int32_t* start, const int32_t* n_new,
-                               const int32_t* pos0, const traj_paged_shape* shape, int32_t scale_block, float rope_theta,
-                               void* stream);
+                                    int64_t v_stride, void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale,
+                                    uint8_t* v_scale, const int32_t* page_table, const int32_t* start, const int32_t* n_new,
+                                    const int32_t* pos0, const traj_paged_shape* shape, int32_t scale_block, float rope_theta,
+                                    void* stream);
 
 /* Everything but the cache's elements as traj_paged_attn; keys and values enter the products exactly (e4m3 times a power
  * of two is a bf16 value).  Scales of blocks without a visible key may hold anything.
@@ -565,9 +565,9 @@ traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void*
 size_t traj_paged_attn_eight_workspace_size(const traj_paged_shape* shape, int32_t scale_block);
 
 traj_status traj_paged_attn_eight(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
-                             const uint8_t* v_scale, const int32_t* page_table, const int32_t* lens,
-                             const int32_t* n_new, void* out, const traj_paged_shape* shape, int32_t scale_block,
-                             float scale, int32_t causal, void* workspace, size_t workspace_bytes, void* stream);
+                                  const uint8_t* v_scale, const int32_t* page_table, const int32_t* lens,
+                                  const int32_t* n_new, void* out, const traj_paged_shape* shape, int32_t scale_block,
+                                  float scale, int32_t causal, void* workspace, size_t workspace_bytes, void* stream);
 
 /* A weight matrix w [K, N] (bf16, row-major, as traj_linear's) to 8 bits with a scale per block of 128 x 128, once, for
  * traj_linear_eight.  With KP = K rounded up to a multiple of 128:
@@ -580,8 +580,7 @@ traj_status traj_quantize_eight(const void* w, void* w8, uint8_t* w_scale, int64
 /* traj_linear with weights in 8 bits: y[M,N] = q(x)[M,K] @ w[K,N] (+ y with accumulate != 0), w the values that w8 and
  * w_scale (as traj_quantize_eight writes them) stand for, q(x) the bf16 x with each row's blocks of 128 of k taken to 8 bits.  The
  * matrix core's 8-bit products accumulate in fp32 (groups of 8 of them to 13 bits: within 2^-10 of the sum of their magnitudes,
- * some 2^-15 as a rule), each result is
- * rounded once to bf16.  A NaN or an infinity in x makes its row of y NaN.
+ * some 2^-15 as a rule), each result is rounded once to bf16.  A NaN or an infinity in x makes its row of y NaN.
  * Limits: those of traj_quantize_eight; 0 <= M < 2^28 - 16 (0 = no-op); x, w8, y 16-byte aligned; y must not overlap x or w8.
  * workspace: traj_linear_eight_workspace_size(M, K, N) bytes, 16-byte aligned: x in 8 bits with its scales and, for shapes
  * whose tiles leave CUs idle, partial products of ranges of K.  0 for a few rows, which take NULL.  One sized for a larger M
@@ -589,7 +588,7 @@ traj_status traj_quantize_eight(const void* w, void* w8, uint8_t* w_scale, int64
 size_t traj_linear_eight_workspace_size(int64_t M, int64_t K, int64_t N);
 
 traj_status traj_linear_eight(const void* x, const void* w8, const uint8_t* w_scale, void* y, int64_t M, int64_t K, int64_t N,
-                         int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+                              int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------
  * Utilities

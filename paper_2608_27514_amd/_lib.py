@@ -788,9 +788,9 @@ def paged_append8(k, v, k_pages, v_pages, k_scale, v_scale, page_table, start, q
     kp, ks, vp, vs, qp, qs, qop, q_out = _append_rows(k, v, q, q_out, n_new, dev, stream)
     i32, per_seq = torch.int32, (B,)
     st = _lib().traj_paged_append_eight(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), ksp, vsp, page_table.data_ptr(),
-                                   _arg(start, "start", i32, per_seq, dev),
-                                   None if n_new is None else _arg(n_new, "n_new", i32, per_seq, dev),
-                                   None if pos0 is None else _arg(pos0, "pos0", i32, per_seq, dev), ref, sb, rope_theta, _stream(stream))
+                                        _arg(start, "start", i32, per_seq, dev),
+                                        None if n_new is None else _arg(n_new, "n_new", i32, per_seq, dev),
+                                        None if pos0 is None else _arg(pos0, "pos0", i32, per_seq, dev), ref, sb, rope_theta, _stream(stream))
     if st != TRAJ_OK:
         _check(st, "traj_paged_append_eight")
     return q_out
@@ -830,8 +830,8 @@ def paged_attn8(q, k_pages, v_pages, k_scale, v_scale, page_table, lens, out=Non
     else:
         ws, ws_bytes = _room(workspace, dev)
     st = _lib().traj_paged_attn_eight(qp, k_pages.data_ptr(), v_pages.data_ptr(), ksp, vsp, page_table.data_ptr(),
-                                 _arg(lens, "lens", torch.int32, (B,), dev), None if n_new is None else _arg(n_new, "n_new", torch.int32, (B,), dev),
-                                 _arg(out, "out", bf16, shape, dev), ref, sb, scale, 1 if causal else 0, ws, ws_bytes, _stream(stream))
+                                      _arg(lens, "lens", torch.int32, (B,), dev), None if n_new is None else _arg(n_new, "n_new", torch.int32, (B,), dev),
+                                      _arg(out, "out", bf16, shape, dev), ref, sb, scale, 1 if causal else 0, ws, ws_bytes, _stream(stream))
     if st != TRAJ_OK:
         _check(st, "traj_paged_attn_eight")
     return out

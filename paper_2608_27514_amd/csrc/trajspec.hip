@@ -1253,9 +1253,9 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
 }
 
 traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
-                               void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale, const int32_t* page_table,
-                               const int32_t* start, const int32_t* n_new, const int32_t* pos0, const traj_paged_shape* shape,
-                               int32_t scale_block, float rope_theta, void* stream) {
+                                    void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale, const int32_t* page_table,
+                                    const int32_t* start, const int32_t* n_new, const int32_t* pos0, const traj_paged_shape* shape,
+                                    int32_t scale_block, float rope_theta, void* stream) {
     if (shape == nullptr) return TRAJ_E_NULL;
     const traj_status st = check_paged8(shape, scale_block);
     if (st != TRAJ_OK) return st;
@@ -1307,8 +1307,8 @@ size_t traj_paged_attn_eight_workspace_size(const traj_paged_shape* shape, int32
 }
 
 traj_status traj_paged_attn_eight(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scale, const uint8_t* v_scale,
-                             const int32_t* page_table, const int32_t* lens, const int32_t* n_new, void* out, const traj_paged_shape* shape,
-                             int32_t scale_block, float scale, int32_t causal, void* workspace, size_t workspace_bytes, void* stream) {
+                                  const int32_t* page_table, const int32_t* lens, const int32_t* n_new, void* out, const traj_paged_shape* shape,
+                                  int32_t scale_block, float scale, int32_t causal, void* workspace, size_t workspace_bytes, void* stream) {
     if (shape == nullptr) return TRAJ_E_NULL;
     const traj_status st = check_paged8(shape, scale_block);
     if (st != TRAJ_OK) return st;
@@ -1342,7 +1342,7 @@ size_t traj_linear_eight_workspace_size(int64_t M, int64_t K, int64_t N) {
 }
 
 traj_status traj_linear_eight(const void* x, const void* w8, const uint8_t* w_scale, void* y, int64_t M, int64_t K, int64_t N, int32_t accumulate,
-                         void* workspace, size_t workspace_bytes, void* stream) {
+                              void* workspace, size_t workspace_bytes, void* stream) {
     if (M < 0 || !gemm8_sizes_ok(std::max<int64_t>(M, 1), K, N)) return TRAJ_E_SHAPE;
     if (K > kG8MaxK || N > kGemmMaxN) return TRAJ_E_UNSUPPORTED;
     if (M == 0) return TRAJ_OK;
