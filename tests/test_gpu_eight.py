@@ -272,6 +272,19 @@ def test_attention_layouts_scales_and_many_sequences():
     attend(rng, 3, 7, 4, 2, 128, 16, 16, [27, 300, 9], True, n_new=[7, 0, 3])
 
 
+@pytest.mark.parametrize("T", [2, 6, 10, 20, 40])
+def test_attention_padding_may_hold_anything(T):
+    """Queries behind n_new are NaN: their rows are 0 and no other row changes; rows that see nothing are 0 too."""
+    rng = np.random.default_rng(T)
+    n_new = [T, T // 2, 0, 1]
+    for ps, sb, lens in ((16, 8, [40, 200, 33, 0]), (20, 20, [900, 30, 70, 5])):  # whole, split
+        (q, *t), out = attend(rng, 4, T, 8, 2, 128, ps, sb, lens, True, n_new=n_new)
+        for b, n in enumerate(n_new):
+            assert not out[b, n:].any()
+            q[b, n:] = float("nan")
+        assert torch.equal(tsp.paged_attn8(q, *t, causal=True, n_new=i32(n_new)), out)
+
+
 def test_attention_lengths_around_every_tile():
     """A sequence of every length up to two rounds of tiles, whole and within a batch that is split."""
     rng = np.random.default_rng(9)
