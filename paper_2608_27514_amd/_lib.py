@@ -678,14 +678,15 @@ def _token_rows(t, name, shape, dev):
     return t.data_ptr(), row
 
 
-def _append_rows(k, v, q, q_out, n_new, dev, stream):
-    """Checks the new tokens' rows of an append call; returns their addresses and strides, and q_out (allocated when None)."""
-    shape = k.shape
+def _append_rows(B, T, Hq, Hkv, D, k, v, q, q_out, n_new, dev, stream):
+    """Checks the new tokens' rows of an append call; returns their addresses and strides, and q_out (allocated when None).
+    Shapes are plain tuples: putting one together from pieces of torch.Size costs some 0.8 us, 5% of a call."""
+    shape = (B, T, Hkv, D)
     kp, ks = _token_rows(k, "k", shape, dev)
     vp, vs = _token_rows(v, "v", shape, dev)
     qp, qs, qop = None, 0, None
     if q is not None:
-        shape = shape[:2] + q.shape[2:3] + shape[3:]
+        shape = (B, T, Hq, D)
         qp, qs = _token_rows(q, "q", shape, dev)
         if q_out is None:
             if n_new is None:
@@ -714,7 +715,7 @@ def paged_append(k, v, k_pages, v_pages, page_table, start, q=None, q_out=None, 
     sh, ref = _paged_struct(*_paged_sizes(B, T, Hq, k_pages, v_pages, page_table, dev))
     if sh.Hkv != Hkv or sh.D != D:
         raise ValueError(f"k has {Hkv} heads of {D}, the pages {sh.Hkv} of {sh.D}")
-    kp, ks, vp, vs, qp, qs, qop, q_out = _append_rows(k, v, q, q_out, n_new, dev, stream)
+    kp, ks, vp, vs, qp, qs, qop, q_out = _append_rows(B, T, Hq, Hkv, D, k, v, q, q_out, n_new, dev, stream)
     i32, per_seq = torch.int32, (B,)
     st = _lib().traj_paged_append(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
                                   _arg(start, "start", i32, per_seq, dev),
@@ -785,7 +786,7 @@ def paged_append8(k, v, k_pages, v_pages, k_scale, v_scale, page_table, start, q
     ksp, vsp, sb = _scale_block(k_pages.shape, k_scale, v_scale, dev)
     if sh.Hkv != Hkv or sh.D != D:
         raise ValueError(f"k has {Hkv} heads of {D}, the pages {sh.Hkv} of {sh.D}")
-    kp, ks, vp, vs, qp, qs, qop, q_out = _append_rows(k, v, q, q_out, n_new, dev, stream)
+    kp, ks, vp, vs, qp, qs, qop, q_out = _append_rows(B, T, Hq, Hkv, D, k, v, q, q_out, n_new, dev, stream)
     i32, per_seq = torch.int32, (B,)
     st = _lib().traj_paged_append_eight(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), ksp, vsp, page_table.data_ptr(),
                                         _arg(start, "start", i32, per_seq, dev),
