@@ -28,7 +28,7 @@
  *                               lengths: new tokens' keys rotated and written, and attention of the
  *                               new tokens over it.
  *   8. traj_confidence_topk_adjusted -- call 2 under each request's penalties, biases and grammar.
- *   9. traj_paged_append_eight, traj_paged_attn_eight -- call 7 over a cache held in 8 bits; traj_quantize_eight, traj_linear_eight --
+ *   9. traj_paged_append_eight(_within), traj_paged_attn_eight -- call 7 over a cache held in 8 bits; traj_quantize_eight, traj_linear_eight --
  *                               the projection GEMM with 8-bit weights and activations.
  *
  * Conventions shared by every entry point
@@ -551,13 +551,24 @@ traj_status traj_confidence_topk_adjusted(const void* logits, int32_t k, float* 
  * this call.  Where a call begins inside a block (start[b] % scale_block != 0) the block's rows before start[b] keep their
  * values: its scale is the larger of the old one (a byte outside [27, 247] counts as the nearest) and what the new rows need,
  * and where it grows those rows are rounded again.  Rows of a block behind the call's last token keep their bits under the block's new
- * scale, so they have to be written again before they are attended to.  q_out (bf16), tokens without a place and the
+ * scale, so they have to be written again before they are attended to: a call in front of tokens that stay needs
+ * traj_paged_append_eight_within or blocks that end where it ends.  q_out (bf16), tokens without a place and the
  * status bits as traj_paged_append.  No two sequences of a call may write the same block. */
 traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                     int64_t v_stride, void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale,
                                     uint8_t* v_scale, const int32_t* page_table, const int32_t* start, const int32_t* n_new,
                                     const int32_t* pos0, const traj_paged_shape* shape, int32_t scale_block, float rope_theta,
                                     void* stream);
+
+/* The same for a call inside a sequence (a block that is denoised in front of a cached suffix): with lens [B] (device) the
+ * sequences' tokens, the rows of the call's last block from start[b] + n_new[b] up to lens[b] keep their values as those before
+ * start[b] do.  A length that ends at or before the call's last token keeps nothing; one outside [0, max_pages * page_size] is
+ * clamped (TRAJ_DEV_BAD_LENGTH).  lens NULL: traj_paged_append_eight. */
+traj_status traj_paged_append_eight_within(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                           int64_t v_stride, void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale,
+                                           uint8_t* v_scale, const int32_t* page_table, const int32_t* start,
+                                           const int32_t* n_new, const int32_t* pos0, const int32_t* lens,
+                                           const traj_paged_shape* shape, int32_t scale_block, float rope_theta, void* stream);
 
 /* Everything but the cache's elements as traj_paged_attn; keys and values enter the products exactly (e4m3 times a power
  * of two is a bf16 value).  Scales of blocks without a visible key may hold anything.

@@ -57,8 +57,9 @@ def linear8(x, values, byte):
     return q @ w, np.abs(q) @ np.abs(w)
 
 
-def paged_append8(q, k, v, pools, page_table, start, n_new=None, pos0=None, theta=500000.0, q_out=None):
+def paged_append8(q, k, v, pools, page_table, start, n_new=None, pos0=None, theta=500000.0, q_out=None, lens=None):
     """pools: (k values, v values [pages, page_size, Hkv, D], k bytes, v bytes [pages, blocks, Hkv]), scaled e4m3 values.
+    Rows of a block before the call's keep their values, with lens also those behind them up to lens[b].
     Returns (q_out, pools, exact): exact are the keys' and values' pools before rounding, NaN where nothing was written."""
     B, T = k.shape[:2]
     pools = [p.copy() for p in pools]
@@ -85,10 +86,16 @@ def paged_append8(q, k, v, pools, page_table, start, n_new=None, pos0=None, thet
                 x = rows[i][lo - first:hi - first]
                 byte = scale_byte(magnitude(x).max((0, 2)))
                 old = np.clip(pools[2 + i][page, s % ps // sb], LOWEST, HIGHEST)
-                if lo > s:
+                kept = [before] if lo > s else []
+                if lens is not None:
+                    end = min(max(int(lens[b]), 0), page_table.shape[1] * ps, s + sb)  # of what the block holds
+                    if end > hi:
+                        kept.append(slice(at.stop, at.stop + end - hi))
+                if kept:
                     byte = np.maximum(byte, old)
-                    pools[i][page, before] = np.where((byte > old)[:, None], e4m3(pools[i][page, before] * scale_value(old - byte + 127)[:, None]),
-                                                      pools[i][page, before])
+                for rows_kept in kept:
+                    x8 = pools[i][page, rows_kept]
+                    pools[i][page, rows_kept] = np.where((byte > old)[:, None], e4m3(x8 * scale_value(old - byte + 127)[:, None]), x8)
                 pools[2 + i][page, s % ps // sb] = byte
                 pools[i][page, at] = e4m3(x / scale_value(byte)[:, None])
                 exact[i][page, at] = x

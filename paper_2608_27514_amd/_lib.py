@@ -138,6 +138,8 @@ EXPORTS = {
                                                        ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "traj_paged_append_eight": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p] * 9 +
                            [ctypes.POINTER(PagedShape), ctypes.c_int32, ctypes.c_float, ctypes.c_void_p]),
+    "traj_paged_append_eight_within": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_int64] * 3 + [ctypes.c_void_p] * 10 +
+                                       [ctypes.POINTER(PagedShape), ctypes.c_int32, ctypes.c_float, ctypes.c_void_p]),
     "traj_paged_attn_eight_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(PagedShape), ctypes.c_int32]),
     "traj_paged_attn_eight": (ctypes.c_int32, [ctypes.c_void_p] * 9 + [ctypes.POINTER(PagedShape), ctypes.c_int32, ctypes.c_float,
                                                                   ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t,
@@ -774,11 +776,13 @@ def _scale_block(pages, k_scale, v_scale, dev):
 
 
 def paged_append8(k, v, k_pages, v_pages, k_scale, v_scale, page_table, start, q=None, q_out=None, n_new=None, pos0=None,
-                  rope_theta=500000.0, stream=None):
+                  rope_theta=500000.0, stream=None, lens=None):
     """:func:`paged_append` to a cache in 8 bits: k_pages / v_pages [pages, page_size, Hkv, D] float8_e4m3fn, and k_scale /
     v_scale [pages, blocks, Hkv] float8_e8m0fnu, a scale for each block of page_size / blocks tokens (at most 64) and head.
     A block's scale is the smallest power of two that brings its rows to 448 at most.  Rows of a block before start[b] keep
-    their values (rounded again where the scale grows), rows behind the call's last token do not."""
+    their values (rounded again where the scale grows).  So do rows behind the call's last token up to lens[b], the
+    sequence's tokens, where lens (int32 [B]) is given: a block denoised in front of a cached suffix needs it.  Other rows behind the
+    call's keep their bits under the new scale, so their values are lost."""
     B, T, Hkv, D = k.shape
     Hq = q.shape[2] if q is not None else Hkv
     dev = _current()
@@ -788,10 +792,12 @@ def paged_append8(k, v, k_pages, v_pages, k_scale, v_scale, page_table, start, q
         raise ValueError(f"k has {Hkv} heads of {D}, the pages {sh.Hkv} of {sh.D}")
     kp, ks, vp, vs, qp, qs, qop, q_out = _append_rows(B, T, Hq, Hkv, D, k, v, q, q_out, n_new, dev, stream)
     i32, per_seq = torch.int32, (B,)
-    st = _lib().traj_paged_append_eight(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), ksp, vsp, page_table.data_ptr(),
-                                        _arg(start, "start", i32, per_seq, dev),
-                                        None if n_new is None else _arg(n_new, "n_new", i32, per_seq, dev),
-                                        None if pos0 is None else _arg(pos0, "pos0", i32, per_seq, dev), ref, sb, rope_theta, _stream(stream))
+    st = _lib().traj_paged_append_eight_within(qp, qs, kp, ks, vp, vs, qop, k_pages.data_ptr(), v_pages.data_ptr(), ksp, vsp,
+                                               page_table.data_ptr(), _arg(start, "start", i32, per_seq, dev),
+                                               None if n_new is None else _arg(n_new, "n_new", i32, per_seq, dev),
+                                               None if pos0 is None else _arg(pos0, "pos0", i32, per_seq, dev),
+                                               None if lens is None else _arg(lens, "lens", i32, per_seq, dev), ref, sb, rope_theta,
+                                               _stream(stream))
     if st != TRAJ_OK:
         _check(st, "traj_paged_append_eight")
     return q_out

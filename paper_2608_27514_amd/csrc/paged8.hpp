@@ -30,19 +30,21 @@ struct Append8Params {
     int T, Hq, Hkv, rotate;
     int tokens;                           // cache rows of a workgroup: whole blocks
     double turns[kAppendMaxHalf];         // rotation per position of pair d in turns: theta^(-2d/D) / 2 pi
+    const int32_t* lens;                  // [B]; WITHIN: the sequences' tokens, those behind the call's among them
 };
 
 // A workgroup takes `tokens` cache rows (whole scale blocks) of a sequence, of which at most ROWS are the call's: their places
 // and angles' sines and cosines go to LDS once, then each wave takes a head of q, K or V at a time, the next one's loads under
 // way.  A lane holds 8 values of a row's first half and the matching 8 of its second, a wave all rows; a block's largest
 // magnitude is found by lane exchanges and an LDS maximum per wave.  Rows that the first block held before are rounded
-// again if the block's scale grows (rare: read only then).  Bound by the copy, (4 Hq + 6 Hkv) D bytes per token, and in
+// again if the block's scale grows (rare: read only then).  WITHIN: so are the rows that its last block holds behind the
+// call's (a kernel of its own, so that other calls pay nothing for it: one token 5.1 us for 4.6, 4 x 4096 62.9 for 62.4).  Bound by the copy, (4 Hq + 6 Hkv) D bytes per token, and in
 // small calls by a chain of loads, angles, rows and stores.
 //   MI355X: 4 x 4096 tokens, 28 over 4 heads of 128 62.1 us (289 MB, 55.9 at the copy's rate), blocks of 64 tokens 52.7 (8192
 //   tokens, 32 over 8 heads, copy 36.2; with the rotated values kept and a head ahead 256 registers and 70.9); one token 4.7,
 //   16 blocks of up to 32 tokens of 32 heads 7.7, 64 sequences' tokens 5.2.
 // grid: x = groups of cache rows from the block that holds the first token, y shares the heads out, z = sequence.
-template <int D, int ROWS>
+template <int D, int ROWS, bool WITHIN>
 __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Params P) {
     constexpr int HALF = D / 2, LPR = D / 16, RPS = 64 / LPR, STEPS = ROWS / RPS, WAVES = kAppendThreads / 64;
     // Registers: long blocks keep their rows as loaded and rotate them twice, and request no head ahead.
@@ -68,6 +70,17 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
     if (t0 >= n) return;
     lead = blockIdx.x == 0 ? lead : 0;
     const int rows = min(P.tokens - lead, n - t0);
+    int behind = 0;  // rows behind the call's last token that its block holds
+    const int last = WITHIN ? P.c8.by_block.div(lead + rows - 1) : 0;  // that block, where this is the last workgroup
+    if constexpr (WITHIN) {
+        int len = P.lens[b];
+        if (len < 0 || len > P.cache.capacity) {
+            if (report) flag_device_status(kDevBadLength);
+            len = len < 0 ? 0 : P.cache.capacity;
+        }
+        const int64_t more = (int64_t)len - ((int64_t)start + n);
+        if (t0 + rows == n && more > 0) behind = (int)min(more, (int64_t)((last + 1) * P.c8.sb - (lead + rows)));
+    }
     const int qh = P.q != nullptr ? P.Hq : 0, units = qh + 2 * P.Hkv;
     const int row0 = lane / LPR, d0 = 8 * (lane % LPR);
     const int64_t token0 = (int64_t)b * P.T + t0;
@@ -127,10 +140,13 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
         if (!AHEAD) fetch(unit);
         const bool query = unit < qh, key = unit < qh + P.Hkv;
         const int head = query ? unit : unit - qh - (key ? 0 : P.Hkv);
-        // the first block's scale where it holds rows from before
+        // the scales of the first and the last block where they hold rows that stay
         uint8_t* scales = (key ? P.c8.k_scale : P.c8.v_scale) + head;
+        auto scale_of = [&](int r) { return min(max((uint32_t)scales[sh_scale[r]], kScaleLowest), kScaleHighest); };
         const bool kept = !query && lead > 0 && sh_row[0] >= 0;
-        const uint32_t old = kept ? min(max((uint32_t)scales[sh_scale[0]], kScaleLowest), kScaleHighest) : 0u;
+        const uint32_t old = kept ? scale_of(0) : 0u;
+        const bool kept_behind = WITHIN && !query && behind > 0 && sh_row[rows - 1] >= 0;
+        const uint32_t old_behind = kept_behind ? scale_of(rows - 1) : 0u;
         auto rotated = [&](int s, float(&v)[16]) {  // the lane's values of step s
             const int r = s * RPS + row0;
 #pragma unroll
@@ -192,13 +208,15 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         uint8_t* pool = (key ? P.c8.k : P.c8.v) + head * P.cache.head_stride + d0;
-        const uint32_t first_byte = max(scale_byte(most[0]), old);
+        // the two are the same block where the call lies in one
+        const uint32_t first_byte = max(scale_byte(most[0]), WITHIN && last == 0 ? max(old, old_behind) : old);
+        const uint32_t last_byte = last == 0 ? first_byte : max(scale_byte(most[last]), old_behind);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             const int r = s * RPS + row0;
             if (r >= rows || sh_row[r] < 0) continue;
             const int block = P.c8.by_block.div(lead + r);
-            const uint32_t byte = block == 0 ? first_byte : scale_byte(most[block]);
+            const uint32_t byte = block == 0 ? first_byte : WITHIN && block == last ? last_byte : scale_byte(most[block]);
             const float inv = scale_inverse(byte);
             float(&v)[16] = x[AHEAD ? s : 0];
             if (!AHEAD) rotated(s, v);
@@ -213,11 +231,11 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
             *reinterpret_cast<u32x2_t*>(dst + HALF) = c;
             if (lane % LPR == 0 && r == max(0, block * P.c8.sb - lead)) scales[sh_scale[r]] = (uint8_t)byte;
         }
-        if (kept && first_byte > old) {
-            // 2^(old - byte): exact but for what falls into the subnormals, or below them
-            const float down = first_byte - old < kScaleOne ? scale_value(kScaleOne - (first_byte - old)) : 0.f;
-            for (int r = row0; r < lead; r += RPS) {
-                uint8_t* dst = pool + sh_row[0] - (int64_t)(lead - r) * P.cache.token_stride;
+        // rows that stay, those before `end`: by 2^(was - byte), exact but for what falls into the subnormals, or below them
+        auto move = [&](uint8_t* end, int count, uint32_t was, uint32_t byte) {
+            const float down = byte - was < kScaleOne ? scale_value(kScaleOne - (byte - was)) : 0.f;
+            for (int r = row0; r < count; r += RPS) {
+                uint8_t* dst = end - (int64_t)(count - r) * P.cache.token_stride;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     u32x2_t a = *reinterpret_cast<const u32x2_t*>(dst + h * HALF);
@@ -229,7 +247,10 @@ __global__ __launch_bounds__(kAppendThreads) void paged8_append_kernel(Append8Pa
                     *reinterpret_cast<u32x2_t*>(dst + h * HALF) = a;
                 }
             }
-        }
+        };
+        if (kept && first_byte > old) move(pool + sh_row[0], lead, old, first_byte);
+        if (kept_behind && last_byte > old_behind)
+            move(pool + sh_row[rows - 1] + (behind + 1) * P.cache.token_stride, behind, old_behind, last_byte);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }

@@ -736,6 +736,19 @@ Paged8Cache paged8_cache(const traj_paged_shape* sh, int32_t sb, const void* k, 
     return Paged8Cache{u8(k), u8(v), u8(ks), u8(vs), sb, sh->page_size / sb, sh->Hkv, fast_div(sb)};
 }
 
+// The append's kernel for `most` rows of the call in a group.
+template <bool WITHIN>
+void (*append8_kernel(int D, int most))(Append8Params) {
+    if (D == 128)
+        return most <= 8    ? paged8_append_kernel<128, 8, WITHIN>
+               : most <= 16 ? paged8_append_kernel<128, 16, WITHIN>
+               : most <= 32 ? paged8_append_kernel<128, 32, WITHIN>
+                            : paged8_append_kernel<128, 64, WITHIN>;
+    return most <= 16   ? paged8_append_kernel<64, 16, WITHIN>
+           : most <= 32 ? paged8_append_kernel<64, 32, WITHIN>
+                        : paged8_append_kernel<64, 64, WITHIN>;
+}
+
 template <int D, bool UNIFORM>
 void launch_paged8_attn(const Paged8AttnParams& p, int64_t wgs, hipStream_t st) {
     auto kernel = p.tile_rows == 16   ? paged8_attn_kernel<D, 1, UNIFORM>
@@ -1252,10 +1265,11 @@ traj_status traj_paged_attn(const void* q, const void* k_pages, const void* v_pa
     return launched();
 }
 
-traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
-                                    void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale, const int32_t* page_table,
-                                    const int32_t* start, const int32_t* n_new, const int32_t* pos0, const traj_paged_shape* shape,
-                                    int32_t scale_block, float rope_theta, void* stream) {
+traj_status traj_paged_append_eight_within(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                           void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale,
+                                           const int32_t* page_table, const int32_t* start, const int32_t* n_new, const int32_t* pos0,
+                                           const int32_t* lens, const traj_paged_shape* shape, int32_t scale_block, float rope_theta,
+                                           void* stream) {
     if (shape == nullptr) return TRAJ_E_NULL;
     const traj_status st = check_paged8(shape, scale_block);
     if (st != TRAJ_OK) return st;
@@ -1278,6 +1292,7 @@ traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void*
     p.start = start;
     p.n_new = n_new;
     p.pos0 = pos0;
+    p.lens = lens;
     p.T = shape->T;
     p.Hq = shape->Hq;
     p.Hkv = shape->Hkv;
@@ -1290,15 +1305,17 @@ traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void*
     // heads are shared out where the groups of rows leave CUs idle
     const int64_t waves = (heads + 3) / 4, share = std::min(waves, std::max<int64_t>(1, kAppend8Wgs / (groups * shape->B)));
     const dim3 grid((unsigned)groups, (unsigned)share, (unsigned)shape->B);
-    auto kernel = shape->D == 128 ? (most <= 8    ? paged8_append_kernel<128, 8>
-                                     : most <= 16 ? paged8_append_kernel<128, 16>
-                                     : most <= 32 ? paged8_append_kernel<128, 32>
-                                                  : paged8_append_kernel<128, 64>)
-                                  : (most <= 16   ? paged8_append_kernel<64, 16>
-                                     : most <= 32 ? paged8_append_kernel<64, 32>
-                                                  : paged8_append_kernel<64, 64>);
+    auto kernel = lens != nullptr ? append8_kernel<true>(shape->D, most) : append8_kernel<false>(shape->D, most);
     hipLaunchKernelGGL(kernel, grid, dim3(kAppendThreads), 0, as_stream(stream), p);
     return launched();
+}
+
+traj_status traj_paged_append_eight(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                    void* q_out, void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale, const int32_t* page_table,
+                                    const int32_t* start, const int32_t* n_new, const int32_t* pos0, const traj_paged_shape* shape,
+                                    int32_t scale_block, float rope_theta, void* stream) {
+    return traj_paged_append_eight_within(q, q_stride, k, k_stride, v, v_stride, q_out, k_pages, v_pages, k_scale, v_scale, page_table, start,
+                                          n_new, pos0, nullptr, shape, scale_block, rope_theta, stream);
 }
 
 size_t traj_paged_attn_eight_workspace_size(const traj_paged_shape* shape, int32_t scale_block) {
