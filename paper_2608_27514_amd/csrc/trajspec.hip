@@ -1482,6 +1482,15 @@ void traj_test_gemm_eight_plan(int64_t M, int64_t K, int64_t N, int32_t plan[2])
     plan[1] = g.splits;
 }
 
+// With a workspace of `room` bytes: the kernel, its k ranges, blocks of 128 of k in the longest of them.
+void traj_test_gemm_eight_ranges(int64_t M, int64_t K, int64_t N, size_t room, int32_t plan[3]) {
+    const Gemm8Plan g = plan_gemm8(M, K, N, room);
+    constexpr int tilings = sizeof(kGemm8Tilings) / sizeof(kGemm8Tilings[0]);
+    plan[0] = (int32_t)(g.rows != nullptr ? tilings + (g.rows - &kGemm8Rows[0][0]) : g.tiling - kGemm8Tilings);
+    plan[1] = g.splits;
+    plan[2] = (int32_t)(g.splits > 1 ? g.k_split / kG8Block : g8_padded(K) / kG8Block);
+}
+
 const char* traj_status_string(int32_t status) {
     switch (status) {
         case TRAJ_OK: return "ok";
