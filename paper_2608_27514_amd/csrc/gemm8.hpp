@@ -133,10 +133,11 @@ struct Gemm8Params : GemmParams {  // K padded to a multiple of 128; W unused, A
 // c ^ ((r >> 2) & 3): the 16 rows that a quarter of a wave reads cover all 64 banks.
 // While a slab multiplies, the next one's fragments are read, and the loads of the stage S behind go out between the MFMAs.
 // Where a wave has few MFMAs per slab, a stage holds two, which halves the meetings.
-// What bounds it is the way from the L2 to LDS and the meetings, not the matrix core and not HBM: 4096 x 4096 x 12288 takes
-// 160 us = 2.57 PFLOP/s (8192 x 8192 x 8192 2.78), 105 with the loads left out, and neither deeper rings nor other cache
-// policies change it (with A's 8 bits 180 us; four stages of one slab 186, tiles of 256 x 128 205).  Fewer rows run through their k at some
-// 0.32 us per 128, again at any depth: 96 x 3584 x 4608 14.8 us with a ring of 5 and 15.3 with one of 9, 14.1 in tiles
+// What bounds it is the way from the L2 to LDS and the meetings, not the matrix core and not HBM: 4096 x 4096 x 12288, normal
+// values, takes 164 us by itself = 2.5 PFLOP/s (8192 x 8192 x 8192 403 = 2.73), 117 with the loads left out (266), and 174 .. 181
+// (446) behind quantize8_rows_kernel, whose 11 us (40) are in it.  With that kernel, rings of four stages of one slab 177 (476)
+// and tiles of 256 x 128 205 (503); other cache policies change nothing.  Fewer rows run through their k at some
+// 0.32 us per 128 at any depth of the ring: 96 x 3584 x 4608 14.8 us with a ring of 5 and 15.3 with one of 9, 14.1 in tiles
 // of 32 x 64, which take 19.2 for 17.2 at 64 x 4096 x 12288.
 // Scales: those of each wave's 128 rows come as a kilobyte for 8 blocks of k, into one of two places of the wave's own, a
 // turn ahead; those of W's columns are in lanes from the start, one per block.
@@ -330,7 +331,7 @@ __global__ __launch_bounds__(WM* WN * 64, 1) void gemm8_ring_kernel(Gemm8Params 
 // The k order within a block is the same for both operands but not the memory's: lane l has 16 of each slab, from 16 (l / 16).
 // LDSX 0: A comes in 8 bits from the workspace; otherwise (M K at most LDSX) every workgroup takes A to 8 bits itself, into LDS
 // in the order of the fragments, while its first loads of W are on their way: one launch for the whole call.
-//   MI355X: 1 x 4096 x 12288 (50 MB of W) 10.0 us, where the read takes 8.1; with A taken to 8 bits first and
+//   MI355X: 1 x 4096 x 12288 (50 MB of W) 10.0 .. 10.7 us, where the read takes 8.1; with A taken to 8 bits first and
 //   through the ring kernel 15.5.
 template <int MR, int NB, int WAVES, int DEPTH, int LDSX, int EPI>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void gemm8_rows_kernel(Gemm8Params P) {

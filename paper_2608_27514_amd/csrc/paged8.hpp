@@ -38,8 +38,9 @@ struct Append8Params {
 // way.  A lane holds 8 values of a row's first half and the matching 8 of its second, a wave all rows; a block's largest
 // magnitude is found by lane exchanges and an LDS maximum per wave.  Rows that the first block held before are rounded
 // again if the block's scale grows (rare: read only then).  WITHIN: so are the rows that its last block holds behind the
-// call's (a kernel of its own, so that other calls pay nothing for it: one token 5.1 us for 4.6, 4 x 4096 62.9 for 62.4).  Bound by the copy, (4 Hq + 6 Hkv) D bytes per token, and in
-// small calls by a chain of loads, angles, rows and stores.
+// call's (a kernel of its own, so that other calls pay nothing for it: one token 5.1 us for 4.6, 4 x 4096 62.9 for 62.4).
+// Bound by the copy, (4 Hq + 6 Hkv) D bytes per token, and in small calls by a chain of loads, angles, rows and stores, where
+// every workgroup that shares a group of rows computes all its angles and waits for them, also one of V heads alone.
 //   MI355X: 4 x 4096 tokens, 28 over 4 heads of 128 62.1 us (289 MB, 55.9 at the copy's rate), blocks of 64 tokens 52.7 (8192
 //   tokens, 32 over 8 heads, copy 36.2; with the rotated values kept and a head ahead 256 registers and 70.9); one token 4.7,
 //   16 blocks of up to 32 tokens of 32 heads 7.7, 64 sequences' tokens 5.2.
@@ -506,12 +507,15 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged8_attn_kernel(Paged8Att
 // read once per 32 rows, taken from 8 bits once); 4 / RW such groups of waves take the range's stages in turn.  While a stage
 // is multiplied the next one lies in registers on its way to the other buffer.
 // A long call is bound by the products and the vector instructions beside them (4 x 512 tokens, 32 over 8 heads, 4096 keys:
-// 251 us = 0.82 PFLOP/s with both parts of the weights); a short one by the latency of one wave a SIMD: 2.2 us a stage (scores
-// 0.45, weights 0.7, values 0.5, LDS 0.4) and 4 us before the first.  The states go to memory from the registers, 64 bytes of
-// a row at once, in 1.5 us; in whole rows, through LDS, 4 us.
+// 251 us = 0.82 PFLOP/s with both parts of the weights); a short one by the latency of one wave a SIMD: 2.2 us a stage (2.5
+// the first) and 4.2 before it (the range from the lengths 1.3, queries 1.5, the first stage's loads 1.4).  With a stamp
+// behind every part, which costs a fifth more, a stage is scores 0.45, weights 0.8, values 0.75, to LDS 0.35, next loads 0.25,
+// what is visible 0.2.  The states go to memory from the registers, 64 bytes of a row at once, in 1.9 us; in whole rows,
+// through LDS, 4 us.
 //   MI355X: 8 blocks of 32 tokens, 28 over 4 heads, up to 2048 keys 28.1 us (30.1 through LDS and with rounded weights); a
 //   block over 4096 keys, 32 over 8 heads, 17.8 (19.1).  Workgroups of eight waves, two ranges of keys each: 28.0 and 19.3,
-//   8 x 4096 keys 43.0 for 46.4, but 64 rows of 256 keys 13.3 for 12.3 and of 4096 51.7 .. 64 for 54.
+//   8 x 4096 keys 43.0 for 46.4, but 64 rows of 256 keys 13.3 for 12.3 and of 4096 51.7 .. 64 for 54.  Pages of bf16 take
+//   as long (27.4, 19.0, 46.5) and the long call 233: here the 8 bits save memory, not time.
 template <int D, int RW, bool UNIFORM, bool ONCE>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged8_rows_kernel(Paged8AttnParams P) {
     using L = PagedLds<D>;

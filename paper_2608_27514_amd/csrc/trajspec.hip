@@ -766,10 +766,11 @@ void launch_paged8(const Paged8AttnParams& p, int64_t wgs, int64_t slots, bool u
 }
 
 // ------------------------------------------------------------------ product with 8-bit operands
-// Tilings with the figures that the plan is made from: the microseconds that one block of 128 of k takes with a workgroup on
-// every CU, those to fill and drain the ring, those that a further round of workgroups takes beside its blocks, and the rate
-// in TB/s at which weights stream when they bound the call.  Fitted to the fastest tiling and split of 149 products of 24 ..
-// 4096 rows (weights from HBM): 0.1% above it on the geometric mean, at worst 2.4%.
+// Tilings with the coefficients that the plan ranks them by: per block of 128 of k and round of workgroups, per call, per
+// further round, and of K N for weights that bound the call.  They are those of a fit to the fastest tiling and split of 149 products
+// of 24 .. 4096 rows with up to 4096 x 24576 weights (its choice 0.1% above the fastest on the geometric mean, at worst 2.4%), not
+// times and rates of their own: 28.1 and 34.8 stand where few of those products had a say.  Wider matrices are outside of
+// the fit, 33 rows of 4096 x 126464 96 us where the read of the weights takes 84.
 struct Gemm8Tiling {
     int bm, bn, threads;
     float block_us, fill_us, round_us, stream;
@@ -806,7 +807,7 @@ const Gemm8Rows kGemm8Rows[3][3] = {
 };
 #undef TRAJ_G8_ROWS
 // Up to 16 rows go by the rows' kernels, up to 32 where K is short: one workgroup holds all of K, which tiles can split
-// (32 rows: 4096 x 4096 11.5 us, by tiles 13.2; 4096 x 12288 15.3 and 16.3; 12288 x 4096 19.5 and 18.3).
+// (32 rows: 4096 x 4096 11.5 us, by the fastest tiles 13.0; 4096 x 12288 15.4 and 16.4; 12288 x 4096 19.8 and 18.3).
 constexpr int64_t kG8FewRows = 16, kG8MoreRows = 32, kG8MoreRowsK = 8192;
 
 struct Gemm8Plan {
