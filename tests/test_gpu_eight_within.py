@@ -144,3 +144,19 @@ def test_the_binding_refuses():
     for bad in (n.long(), n[:1], n.cpu()):
         with pytest.raises((TypeError, ValueError)):
             tsp.paged_append8(x, x, kp, kp.clone(), scale, scale.clone(), table, n, lens=bad)
+
+
+def test_calls_that_begin_before_the_cache_or_end_at_its_end():
+    """Tokens without a place lie in blocks of their own; the last block of the table may be the call's last, or full."""
+    rng = np.random.default_rng(5)
+    H, D, ps, sb, T = 2, 64, 16, 8, 6
+    table, pages = make_table(rng, 4, 2)
+    before = make_pools(rng, pages, ps, sb, H, D)
+    before[2][:] = rng.integers(0, 256, before[2].shape)  # bytes outside [27, 247] count as the nearest
+    k, v = (bf16_round(rng.standard_normal((4, T, H, D)) * 2.0 ** rng.integers(-3, 8, (4, T, 1, 1))) for _ in range(2))
+    start, n_new, lens = [-3, 24, 26, 25], [6, 5, 6, 0], [32, 32, 32, 32]
+    _, pools, _ = eight.paged_append8(k, k, v, before, table, start, n_new, theta=0, lens=lens)
+    got = on_gpu(before)
+    tsp.device_status()
+    tsp.paged_append8(bf(k), bf(v), *got, i32(table), i32(start), n_new=i32(n_new), rope_theta=0.0, lens=i32(lens))
+    assert tsp.device_status() == tsp.DEV_BAD_LENGTH and same(got, pools)
