@@ -509,7 +509,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged8_attn_kernel(Paged8Att
 // A long call is bound by the products and the vector instructions beside them (4 x 512 tokens, 32 over 8 heads, 4096 keys:
 // 251 us = 0.82 PFLOP/s with both parts of the weights); a short one by the latency of one wave a SIMD: 2.2 us a stage (2.5
 // the first) and 4.2 before it (the range from the lengths 1.3, queries 1.5, the first stage's loads 1.4).  With a stamp
-// behind every part, which costs a fifth more, a stage is scores 0.45, weights 0.8, values 0.75, to LDS 0.35, next loads 0.25,
+// behind every part, which costs a third more, a stage is scores 0.45, weights 0.8, values 0.75, to LDS 0.35, next loads 0.25,
 // what is visible 0.2.  The states go to memory from the registers, 64 bytes of a row at once, in 1.9 us; in whole rows,
 // through LDS, 4 us.
 //   MI355X: 8 blocks of 32 tokens, 28 over 4 heads, up to 2048 keys 28.1 us (30.1 through LDS and with rounded weights); a
